@@ -234,6 +234,99 @@ kd_status kd_loss_fwd_bwd_multi(const kd_loss_params* params, int n_teachers,
                                 float* loss, float* per_token_loss, void* grad_h_s, void* grad_W_s,
                                 void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Losses over one output head.
+ *
+ * What a distillation program computes beside the divergence of two models: the cross entropy of the labels
+ * (kd_ce_*), and the divergence from a teacher of which only the largest logits were kept (kd_topk_*).  Same
+ * conventions as above: plain C ABI, every buffer the caller's, no allocation, no synchronisation, only kernels
+ * enqueued, nothing kept from call to call, results bitwise reproducible, all checks on the host before anything is
+ * enqueued.  z = h W, logits produced tile by tile (twice with gradients), never stored; tokens that do not count are
+ * compacted away.
+ *
+ *  h       [T, H] device, in_dtype;  W: head in the order w_layout, in_dtype
+ *  mask    [T] uint8 device, non-zero = token may count; NULL = every token may
+ *  loss    device, one float: the mean over the n tokens that count, times loss_scale (0 when n == 0)
+ *  per_token_loss  device, [T] floats (0 for tokens that do not count) or NULL
+ *  grad_h [T, H], grad_W (order of W) device, grad_dtype; either may be NULL and is then not computed.  Rows of grad_h
+ *          of tokens that do not count are exactly 0; grad_W is overwritten, or added to with accumulate_grad_W
+ *  workspace  device, 256-byte aligned, workspace_bytes >= the size query
+ * h, W, grad_h, grad_W must be 16-byte aligned, the other arrays to their elements.  Inputs must not alias outputs or
+ * the workspace.
+ *
+ * fp32 operands are multiplied as three bf16 parts each (six products, 24 bits), and fp32 gradients are fp32 sums of
+ * products in which dL/dz is held in three parts: fp32 results are as exact as fp32 arithmetic gives them.  For bf16
+ * gradients dL/dz is rounded to bf16 once, without the factor loss_scale / n that all its entries share, and the sums
+ * once more. */
+
+/* Type of labels and of vocabulary rows. */
+typedef enum { KD_I32 = 0, KD_I64 = 1 } kd_index_dtype;
+
+/* Cross entropy with labels:
+ *   l_t = lse_t - (1-e) z[t, y_t] - (e / V) sum_v z[t, v] + z_loss lse_t^2,    lse_t = log sum_v exp(z[t, v])
+ * with label smoothing e.  A token counts if the mask says so and its label is not negative (-100, say); a label of V or
+ * more is never read: its token's loss, the loss and the gradients are NaN. */
+typedef struct {
+  int64_t T, H, V;            /* H and V multiples of 8                                          */
+  int32_t in_dtype;           /* kd_dtype of h and W                                             */
+  int32_t grad_dtype;         /* kd_dtype of grad_h and grad_W                                   */
+  int32_t w_layout;           /* kd_wlayout                                                      */
+  int32_t index_dtype;        /* kd_index_dtype of the labels                                    */
+  float label_smoothing;      /* e, 0 <= e < 1                                                   */
+  float z_loss;               /* >= 0, finite: weight of the squared log-sum-exp                 */
+  float loss_scale;           /* finite, non-zero: factor on losses and gradients                */
+  int32_t accumulate_grad_W;  /* 0 or 1                                                          */
+  int32_t vocab_chunk;        /* as in kd_loss_params                                            */
+  int32_t reserved;           /* must be 0                                                       */
+} kd_ce_params;
+
+kd_status kd_ce_workspace_size(const kd_ce_params* params, size_t* bytes);
+kd_status kd_ce_fwd_bwd(const kd_ce_params* params, const void* h, const void* W, const void* labels,
+                        const uint8_t* mask, float* loss, float* per_token_loss, void* grad_h, void* grad_W,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+/* ... without gradients: -per_token_loss (loss_scale 1, no smoothing) are the labels' log-probabilities. */
+kd_status kd_ce_fwd(const kd_ce_params* params, const void* h, const void* W, const void* labels, const uint8_t* mask,
+                    float* loss, float* per_token_loss, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits.  Per token K vocabulary rows top_index[t, k] and the teacher's logits
+ * top_logits[t, k] there, in any order; a negative row, or a logit of minus infinity, is an entry that is not there (lists
+ * shorter than K); entries of the same row add up.  With p = softmax(z / tau) and
+ *   KD_TAIL_RENORM  q_k = softmax over the list of top_logits / tau             (lse is not read, may be NULL)
+ *   KD_TAIL_REST    q_k = exp(top_logits[t, k] / tau - lse[t]),  lse[t] = log sum_v exp(z_t[t, v] / tau) over the teacher's
+ *                   whole vocabulary; what the list does not hold, r = max(0, 1 - sum q), is one more category, which is
+ *                   compared with the student's mass beside the list
+ *   KD_TAIL_DROP    the same q without the rest (also for importance weights: top_logits = tau log w, lse = 0)
+ * the loss of a token is  sum_k q_k (log q_k - log p_k)  (+ r (log r - log (1 - sum p_k)) with KD_TAIL_REST).
+ * A token counts if the mask says so and its list is not empty; a row of V or more is never read: its token's loss, the
+ * loss and the gradients are NaN, as for a logit of NaN. */
+typedef enum { KD_TAIL_RENORM = 0, KD_TAIL_REST = 1, KD_TAIL_DROP = 2 } kd_tail;
+#define KD_TOPK_MAX 1024
+
+typedef struct {
+  int64_t T, H, V;            /* H and V multiples of 8                                          */
+  int32_t K;                  /* entries per token, 1 .. KD_TOPK_MAX, at most V (KD_TAIL_REST: V - 1) */
+  int32_t in_dtype;           /* kd_dtype of h_s and W_s                                         */
+  int32_t grad_dtype;         /* kd_dtype of grad_h_s and grad_W_s                               */
+  int32_t w_layout;           /* kd_wlayout                                                      */
+  int32_t index_dtype;        /* kd_index_dtype of top_index                                     */
+  int32_t top_dtype;          /* kd_dtype of top_logits                                          */
+  int32_t tail;               /* kd_tail                                                         */
+  float tau;                  /* temperature, 1e-6 <= tau <= 1e6                                 */
+  float loss_scale;           /* finite, non-zero: factor on losses and gradients                */
+  int32_t accumulate_grad_W;  /* 0 or 1                                                          */
+  int32_t flags;              /* KD_FLAG_TAU2 or 0                                               */
+  int32_t vocab_chunk;        /* as in kd_loss_params                                            */
+  int32_t reserved[2];        /* must be 0                                                       */
+} kd_topk_params;
+
+kd_status kd_topk_workspace_size(const kd_topk_params* params, size_t* bytes);
+kd_status kd_topk_fwd_bwd(const kd_topk_params* params, const void* top_logits, const void* top_index, const float* lse,
+                          const void* h_s, const void* W_s, const uint8_t* mask, float* loss, float* per_token_loss,
+                          void* grad_h_s, void* grad_W_s, void* workspace, size_t workspace_bytes, void* hip_stream);
+kd_status kd_topk_fwd(const kd_topk_params* params, const void* top_logits, const void* top_index, const float* lse,
+                      const void* h_s, const void* W_s, const uint8_t* mask, float* loss, float* per_token_loss,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static, NUL-terminated description of a status code (error reporting of this boundary; nothing of
  * the paper's). */
 const char* kd_status_string(kd_status status);

@@ -1,7 +1,7 @@
-"""torch.autograd front end of the library: the distillation loss as a differentiable scalar.
+"""torch.autograd front end of the library: the losses as differentiable scalars.
 
 The forward call runs the whole fused path (loss AND both gradients come out of one
-kd_loss_fwd_bwd); backward only scales the stored gradients by the incoming scalar (the one
+call of the library); backward only scales the stored gradients by the incoming scalar (the one
 PyTorch op here: the chain rule through whatever the caller does with the loss).  No step of the
 method runs in PyTorch: this module is argument marshalling, like kdloss.py.
 """
@@ -38,3 +38,45 @@ def kd_loss(h_s, W_s, h_t, W_t, mask=None, tau=1.0, kind=K.FKL, beta=0.5, w_layo
     gradients (they are formed in forward, before that factor exists)."""
     return _KDLossFn.apply(h_s, W_s, h_t, W_t, mask, float(tau), int(kind), float(beta), int(w_layout),
                            int(flags), float(teacher_scale), workspace, float(loss_scale))
+
+
+class _HeadLossFn(torch.autograd.Function):
+    """A one-head loss: `call(want_grad_h, want_grad_W)` gives the dict of a *_fwd_bwd call.  Only the gradients that are asked
+    for are computed."""
+
+    @staticmethod
+    def forward(ctx, h, W, call, names):
+        out = call(ctx.needs_input_grad[0], ctx.needs_input_grad[1])
+        ctx.save_for_backward(out[names[0]], out[names[1]])
+        return out["loss"].reshape(())
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        return tuple(None if x is None else x * g.to(x.dtype) for x in ctx.saved_tensors) + (None, None)
+
+
+def cross_entropy(h, W, labels, mask=None, label_smoothing=0.0, z_loss=0.0, w_layout=K.W_VH, workspace=None,
+                  loss_scale=1.0):
+    """Cross entropy of `labels` (negative: ignored) under softmax(h W) as a scalar tensor, the mean over the tokens that
+    count; gradients flow to h and W.  Arguments as in kdloss.kd_ce_fwd_bwd; loss_scale as in kd_loss.  Where no gradient is
+    asked for, none is computed."""
+    kw = dict(label_smoothing=float(label_smoothing), z_loss=float(z_loss), w_layout=int(w_layout), workspace=workspace,
+              loss_scale=float(loss_scale))
+    if not (torch.is_grad_enabled() and (h.requires_grad or W.requires_grad)):
+        return K.kd_ce_fwd(h.detach(), W.detach(), labels, mask, **kw)["loss"].reshape(())
+    return _HeadLossFn.apply(h, W, lambda gh, gW: K.kd_ce_fwd_bwd(h.detach(), W.detach(), labels, mask, want_grad_h=gh,
+                                                                  want_grad_W=gW, **kw), ("grad_h", "grad_W"))
+
+
+def topk_loss(h_s, W_s, top_logits, top_index, lse=None, mask=None, tau=1.0, tail=K.TAIL_RENORM, w_layout=K.W_VH, flags=0,
+              workspace=None, loss_scale=1.0):
+    """Divergence of softmax(h_s W_s / tau) from a teacher's top logits as a scalar tensor; gradients flow to h_s and W_s.
+    Arguments as in kdloss.kd_topk_fwd_bwd; loss_scale as in kd_loss.  Where no gradient is asked for, none is computed."""
+    kw = dict(lse=lse, mask=mask, tau=float(tau), tail=int(tail), w_layout=int(w_layout), flags=int(flags),
+              workspace=workspace, loss_scale=float(loss_scale))
+    if not (torch.is_grad_enabled() and (h_s.requires_grad or W_s.requires_grad)):
+        return K.kd_topk_fwd(top_logits, top_index, h_s.detach(), W_s.detach(), **kw)["loss"].reshape(())
+    return _HeadLossFn.apply(h_s, W_s, lambda gh, gW: K.kd_topk_fwd_bwd(top_logits, top_index, h_s.detach(), W_s.detach(),
+                                                                        want_grad_h=gh, want_grad_W=gW, **kw),
+                             ("grad_h_s", "grad_W_s"))

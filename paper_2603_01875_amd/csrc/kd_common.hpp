@@ -53,6 +53,43 @@ __device__ __forceinline__ int dz_column(int i, int row) {
   return 32 * (i >> 1) + 16 * ((row >> 2) & 1) + 8 * (i & 1) + 4 * (row >> 3) + (row & 3);
 }
 
+// Merging the partial sums.  Every workgroup (one per token tile and vocabulary range) leaves its values as [range][value][T_pad], and
+// with few tokens there are many ranges (256 at T <= 256; the eight-wave loop's four lanes of a token put theirs
+// together first: a step of T = 200, H = 2048 / 512, V = 32000 148 -> 133 us, AKL at T = 150, H = 1024 / 512 347 -> 291).  A merge is bound by the latency of its loads:
+// one thread walking all the parts of a token took 658 us at T = 256 and 47 us at T = 4096.  So a workgroup owns TX
+// tokens and NT / TX threads share the parts of each: lanes run along the tokens (TX = 8: 32-byte runs, TX = 32:
+// whole lines), the rest of the lanes and the waves along the parts; partial results meet by shuffles, then through
+// LDS, in a fixed order.  Measured: combine_kernel 658 -> 23 us at T = 256, 47 -> 9 us at 128 parts, 6 us at 32 (T = 4096),
+// one search merge of AKL 536 -> 15 us at T = 2048.
+struct MergeSum {
+  static __device__ __forceinline__ float op(float a, float b) { return a + b; }
+};
+struct MergeMax {
+  static __device__ __forceinline__ float op(float a, float b) { return fmaxf(a, b); }
+};
+// v[i] of every thread -> the merged value of the thread's token, in every thread of that token
+template <int TX, int NT, int NV, class Op>
+__device__ __forceinline__ void merge_parts(float (&v)[NV], float* lds) {
+  constexpr int NW = NT / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tx = lane % TX;
+#pragma unroll
+  for (int off = TX; off < 64; off <<= 1)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = Op::op(v[i], __shfl_xor(v[i], off, 64));
+  __syncthreads();                       // the values of an earlier merge have been read
+  if (lane < TX)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) lds[(wave * NV + i) * TX + tx] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float r = lds[i * TX + tx];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) r = Op::op(r, lds[(w * NV + i) * TX + tx]);
+    v[i] = r;
+  }
+}
+
 #define KD_STRIP_KERNEL __global__ __launch_bounds__(StripCfg::NT, 1) __attribute__((amdgpu_waves_per_eu(1, 1)))
 
 // Launch of a kernel that needs more dynamic LDS than the default limit.  The limit is a property of

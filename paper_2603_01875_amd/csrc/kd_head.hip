@@ -1,0 +1,413 @@
+// The one-head losses: cross entropy with labels, and distillation from a teacher's top logits.  One call:
+//   targets  : the caller's labels or top logits -> per token a sorted list of entries with their probabilities, and whether it counts
+//   (row map and operand copies: operands_kernel, kd_kernels.hip)
+//   stats    : logit tiles -> running max and sum beside the lists, the logits on them (kd_head.hpp)
+//   combine  : log-sum-exp, the token's loss, the coefficients of its gradient
+//   finalize : n, loss, the gradients' common factor, h transposed for grad_W
+//   per chunk of the vocabulary:
+//     grad   : logit tiles again -> dL/dz in the order of dz_chunk;  listed: its entries on the lists
+//     the backward products (kd_products.hpp)
+//   gradh_finish
+#include "kd_head.hpp"
+
+namespace kd {
+
+// ------------------------------------------------------------------------------------------
+// targets
+// ------------------------------------------------------------------------------------------
+struct TargetArgs {
+  Targets t;
+  int T, V;
+  double inv_tau;
+};
+
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
+  return x;
+}
+__device__ __forceinline__ double wave_max(double x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x = fmax(x, __shfl_xor(x, off, 64));
+  return x;
+}
+
+// An entry past the vocabulary makes its token NaN: it is never read, and the loss says so.
+__global__ __launch_bounds__(256) void label_targets_kernel(const TargetArgs a) {
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= a.T) return;
+  const int64_t y = a.t.index64 ? ((const int64_t*)a.t.index)[t] : (int64_t)((const int*)a.t.index)[t];
+  const bool out = y >= a.V;
+  a.t.valid[t] = y >= 0 && (!a.t.mask || a.t.mask[t]);
+  a.t.list[t] = y >= 0 && !out ? (int)y : kNoEntry;
+  a.t.q[t] = 1.f - a.t.smoothing;
+  double* const info = a.t.info + (int64_t)t * kTargetInfo;
+  info[0] = out ? __builtin_nan("") : 1.0;
+  info[1] = info[2] = 0.0;
+}
+
+// One wave per token.  The entries (absent: a negative row, or a logit of minus infinity) are put in ascending order by counting, for
+// each, how many come before it; those of the same row add up.  K^2 comparisons out of LDS: for K = 64 a wave's 64 reads.  All sums in
+// 64 bits: the mass beside the list is a difference from 1.
+__global__ __launch_bounds__(256) void top_targets_kernel(const TargetArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int K = a.t.K, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, t = blockIdx.x * 4 + wave;
+  double* const q = (double*)smem + wave * K;
+  int* const row = (int*)(smem + 4 * K * 8) + wave * 2 * K;
+  int* const once = row + K;
+  const bool there = t < a.T;
+  const int64_t at = (int64_t)t * K;
+  bool bad = false;
+  double top = -INFINITY;
+  if (there)
+    for (int k = lane; k < K; k += 64) {
+      const int64_t v = a.t.index64 ? ((const int64_t*)a.t.index)[at + k] : (int64_t)((const int*)a.t.index)[at + k];
+      const float z = a.t.top_f32 ? ((const float*)a.t.top)[at + k] : (float)((const bf16_t*)a.t.top)[at + k];
+      const bool in = v >= 0 && z != -INFINITY;
+      bad = bad || (in && (v >= a.V || z != z));
+      row[k] = in && v < a.V ? (int)v : kNoEntry;
+      q[k] = (double)z * a.inv_tau;
+      if (in) top = fmax(top, q[k]);
+    }
+  __syncthreads();
+  top = wave_max(top);
+  double mass = 0.0;
+  if (there)
+    for (int k = lane; k < K; k += 64) mass += row[k] != kNoEntry ? exp(q[k] - top) : 0.0;
+  mass = wave_sum(mass);
+  const double norm = !there ? 0.0 : a.t.tail == 0 ? top + log(mass) : (double)a.t.lse[t];
+  if (there)
+    for (int k = lane; k < K; k += 64) q[k] = row[k] != kNoEntry ? exp(q[k] - norm) : 0.0;
+  __syncthreads();
+  if (there)
+    for (int k = lane; k < K; k += 64) {
+      const int v = row[k];
+      bool first = v != kNoEntry;
+      for (int j = 0; j < k && first; ++j) first = row[j] != v;
+      once[k] = first ? v : kNoEntry;
+    }
+  __syncthreads();
+  if (!there) return;
+  double held = 0.0, ent = 0.0;
+  int n = 0;
+  for (int k = lane; k < K; k += 64) {
+    const int v = once[k];
+    if (v == kNoEntry) continue;
+    int rank = 0;
+    double sum = 0.0;
+    for (int j = 0; j < K; ++j) {
+      rank += once[j] < v;
+      sum += row[j] == v ? q[j] : 0.0;
+    }
+    a.t.list[at + rank] = v;
+    a.t.q[at + rank] = (float)sum;
+    held += sum;
+    ent += sum > 0.0 ? sum * log(sum) : 0.0;
+    ++n;
+  }
+  held = wave_sum(held);
+  ent = wave_sum(ent);
+  n = (int)wave_sum((double)n);
+  bad = __any(bad);
+  for (int k = n + lane; k < K; k += 64) a.t.list[at + k] = kNoEntry;
+  if (lane) return;
+  const double rest = a.t.tail == 1 ? fmax(1.0 - held, 0.0) : 0.0;
+  double* const info = a.t.info + (int64_t)t * kTargetInfo;
+  info[0] = bad || held != held ? __builtin_nan("") : held + rest;
+  info[1] = rest;
+  info[2] = ent + (rest > 0.0 ? rest * log(rest) : 0.0);
+  a.t.valid[t] = (n > 0 || bad) && (!a.t.mask || a.t.mask[t]);
+}
+
+hipError_t launch_targets(const HeadProblem& h, hipStream_t st) {
+  const TargetArgs a{h.t, h.p.T, h.p.V, 1.0 / (double)h.p.tau};
+  if (h.t.ce) hipLaunchKernelGGL(label_targets_kernel, dim3((h.p.T + 255) / 256), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(top_targets_kernel, dim3((h.p.T + 3) / 4), dim3(256), 64 * h.t.K, st, a);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------
+// combine
+// ------------------------------------------------------------------------------------------
+struct HeadCombineArgs {
+  const float* partials;
+  const int* meta;
+  const int* rowmap;
+  int T_pad, nv, K, n_parts;           // n_parts: 0 = the device's plan
+  float c, uniform, z_loss;            // uniform: U
+  const int* list;
+  const float* q;
+  const float* z;
+  const double* info;
+  f32x4* rowinfo;
+  float* row_loss;
+};
+
+// Merges a token's partial sums and its listed logits.  Logarithms in base 2; what is a difference of large quantities in double.
+template <int TX, int NT>
+__global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs a) {
+  __shared__ float lds[NT / 64 * 5 * TX];
+  const int t = blockIdx.x * TX + threadIdx.x % TX, g = threadIdx.x / TX, G = NT / TX;
+  const int n_valid = a.meta[META_N_VALID], n_parts = a.n_parts ? a.n_parts : a.meta[META_N_SPLIT];
+  if (t >= n_valid && g == 0) {        // padding rows: everything evaluates to 0
+    a.rowinfo[t] = f32x4{1.0e30f, 0.f, 0.f, 0.f};
+    a.row_loss[t] = 0.f;
+  }
+  if ((int)(blockIdx.x * TX) >= n_valid) return;
+  const int64_t stride = (int64_t)a.nv * a.T_pad;
+  const float* const q0 = a.partials + t;              // t < T_pad: allocated, whatever the row holds
+  const int64_t token = a.rowmap[t];
+  const int* const list = a.list + token * a.K;
+  const float* const prob = a.q + token * a.K;
+  const float* const z = a.z + (int64_t)t * a.K;
+  float m[2] = {M_FLOOR, M_FLOOR};
+#pragma unroll 4
+  for (int p = g; p < n_parts; p += G) m[0] = fmaxf(m[0], q0[p * stride]);
+  for (int k = g; k < a.K && list[k] != kNoEntry; k += G) m[1] = fmaxf(m[1], z[k] * a.c);
+  merge_parts<TX, NT, 2, MergeMax>(m, lds);
+  float v[5] = {0.f, 0.f, 0.f, 0.f, 0.f};              // sum beside the list, on it, sum of logits, sum q (z - max), entries
+#pragma unroll 4
+  for (int p = g; p < n_parts; p += G) {
+    const float* const q = q0 + p * stride;
+    v[0] = fmaf(q[a.T_pad], fexp2(q[0] - m[0]), v[0]);
+    if (a.nv == 3) v[2] += q[2 * a.T_pad];
+  }
+  for (int k = g; k < a.K && list[k] != kNoEntry; k += G) {
+    const float d = fmaf(z[k], a.c, -m[1]);
+    v[1] += fexp2(d);
+    v[2] += z[k];
+    v[3] = fmaf(prob[k], d, v[3]);
+    v[4] += prob[k];
+  }
+  merge_parts<TX, NT, 5, MergeSum>(v, lds);
+  if (g != 0 || t >= n_valid) return;
+  const double ln2 = 0.6931471805599453;
+  const double* const info = a.info + token * kTargetInfo;
+  const double mass = info[0], rest = info[1], ent = info[2];
+  const double lo = v[0] == 0.f ? -INFINITY : (double)m[0] + log2((double)v[0]);     // beside the list
+  const double ll = v[1] == 0.f ? -INFINITY : (double)m[1] + log2((double)v[1]);
+  const double big = fmax(lo, ll), lse = v[0] != v[0] || v[1] != v[1] ? __builtin_nan("") : big + log2(exp2(lo - big) + exp2(ll - big));
+  const double nat = lse * ln2;
+  const double on = v[4] != 0.f ? (double)v[3] + (double)m[1] * (double)v[4] : 0.0;   // sum q z in base 2
+  double loss = ent + mass * nat - ln2 * on - (double)a.uniform * (double)v[2] + (double)a.z_loss * nat * nat;
+  const double in = mass + 2.0 * (double)a.z_loss * nat;
+  double out = in;
+  if (rest > 0.0) {
+    loss -= rest * lo * ln2;
+    out -= rest * exp2(lse - lo);
+  }
+  // (the log-sum-exp as a float is up to 1e-6 off, the same way for all of a token's entries: that goes into the coefficients)
+  const float high = (float)lse;
+  const double corr = exp2((double)high - lse);
+  a.rowinfo[t] = f32x4{high, (float)(out * corr), a.uniform, (float)(in * corr)};
+  a.row_loss[t] = (float)loss;
+}
+
+hipError_t launch_head_combine(const HeadProblem& h, hipStream_t st) {
+  const Problem& p = h.p;
+  const HeadCombineArgs a{p.partials, p.meta, p.rowmap, p.T_pad, h.t.smoothing > 0.f ? 3 : 2, h.t.K, h.few ? h.parts : 0, 1.4426950408889634f / p.tau,
+                          h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.t.info, (f32x4*)p.rowinfo, p.row_loss};
+  if ((h.few ? h.parts : p.n_split) >= 128) hipLaunchKernelGGL((head_combine_kernel<8, 1024>), dim3(p.T_pad / 8), dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((head_combine_kernel<32, 256>), dim3(p.T_pad / 32), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------
+// finalize
+// ------------------------------------------------------------------------------------------
+struct HeadFinalizeArgs {
+  const int *meta, *inv, *rowmap;
+  const float* row_loss;
+  int T, T_pad;
+  float tau, weight;
+  float *loss, *per_token, *scale;
+  const void* src;         // h, for grad_W: its columns packed (see pack_columns, kd_kernels.hip), `sets` copies of the token axis
+  bf16_t* dst;
+  int src_f32, C, sets;
+};
+
+// Which bf16 part of h stands against copy s of dL/dz: dz 0 0 0 1 1 2 x h 0 1 2 0 1 0, or dz 0 1 2 x h itself.
+__device__ __forceinline__ bf16_t h_part(float f, int s, int sets) {
+  const int part = sets == 6 ? 0x010210 >> (4 * s) & 15 : 0;
+  const bf16_t hi = (bf16_t)f;
+  if (part == 0) return hi;
+  const float rest = f - (float)hi;
+  const bf16_t mid = (bf16_t)rest;
+  return part == 1 ? mid : (bf16_t)(rest - (float)mid);
+}
+
+__global__ __launch_bounds__(1024) void head_finalize_kernel(const HeadFinalizeArgs a) {
+  __shared__ double s_sum[1024];
+  __shared__ float tile[64][65];
+  const int tid = threadIdx.x, n = a.meta[META_N_VALID];
+  if (flat_group() > 0) {
+    const int b = (int)(flat_group() - 1), wide = a.T_pad / 64, by = b / wide, r0 = (b - by * wide) * 64, c0 = by * 64;
+    const int eff = a.meta[META_T_EFF];
+    if (c0 >= a.C || r0 >= eff) return;
+    const int tx = tid & 63, ty = tid >> 6, c = c0 + tx, cc = min(c, a.C - 1);
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {          // (rowmap holds a valid row for every r < T_pad)
+      const int64_t at = (int64_t)a.rowmap[r0 + ty + 16 * i] * a.C + cc;
+      v[i] = a.src_f32 ? ((const float*)a.src)[at] : (float)((const bf16_t*)a.src)[at];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tile[ty + 16 * i][tx] = r0 + ty + 16 * i < n && c < a.C ? v[i] : 0.f;
+    __syncthreads();
+    const int sub = ty >> 2, blk = ty & 3;                             // a wave: 16 hidden rows x 32 tokens, 1 KiB
+    if (sub > 1 || c0 + 16 * blk >= a.C) return;
+    for (int s = 0; s < a.sets; ++s) {
+      bf16x8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = h_part(tile[32 * sub + 8 * (tx >> 4) + e][16 * blk + (tx & 15)], s, a.sets);
+      *(bf16x8*)(a.dst + ((int64_t)(c0 / 16 + blk) * (a.T_pad / 32 * a.sets) + (s * eff + r0) / 32 + sub) * 512 + tx * 8) = o;
+    }
+    return;
+  }
+  double acc = 0.0;
+  for (int j = tid; j < n; j += 1024) acc += (double)a.row_loss[j];
+  s_sum[tid] = acc;
+  __syncthreads();
+  for (int s = 512; s > 0; s >>= 1) {
+    if (tid < s) s_sum[tid] += s_sum[tid + s];
+    __syncthreads();
+  }
+  if (tid == 0) {
+    *a.loss = n > 0 ? a.weight * (float)(s_sum[0] / (double)n) : 0.f;
+    *a.scale = n > 0 ? a.weight / ((float)n * a.tau) : 0.f;
+  }
+  if (a.per_token)
+    for (int t = tid; t < a.T; t += 1024) {
+      const int j = a.inv[t];
+      a.per_token[t] = j >= 0 ? a.weight * a.row_loss[j] : 0.f;
+    }
+}
+
+hipError_t launch_head_finalize(const HeadProblem& h, bool pack_h, hipStream_t st) {
+  const Problem& p = h.p;
+  const HeadFinalizeArgs a{p.meta, p.inv, p.rowmap, p.row_loss, p.T, p.T_pad, p.tau, p.out_weight, p.loss, p.per_token_loss, h.t.scale,
+                           p.user_h_s, (bf16_t*)p.h_sT, p.in_f32, p.H_s, p.dz_sets};
+  const FlatGrid g = flat_grid(1 + (pack_h ? (int64_t)(p.T_pad / 64) * ((p.H_s + 63) / 64) : 0));
+  hipLaunchKernelGGL(head_finalize_kernel, dim3(g.x, g.y), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------
+// logit tiles
+// ------------------------------------------------------------------------------------------
+HeadArgs head_args(const HeadProblem& h) {
+  const Problem& p = h.p;
+  HeadArgs a{};
+  a.W = (const bf16_t*)p.W_s; a.h = (const bf16_t*)p.h_s;
+  a.V = p.V; a.K = p.K_s;
+  a.ld = p.w_hv_inplace ? p.V : p.prep_Ws ? p.K_s : p.H_s;
+  a.meta = p.meta;
+  a.T_pad = p.T_pad;
+  a.c = 1.4426950408889634f / p.tau;
+  a.partials = p.partials;
+  a.rowmap = p.rowmap;
+  a.list = h.t.list; a.n_list = h.t.K; a.z = h.t.z;
+  a.rowinfo = (const f32x4*)p.rowinfo;
+  a.kept = h.kept;
+  a.dz = (bf16_t*)p.dz; a.ldz = p.V_c; a.sets = p.dz_sets;
+  return a;
+}
+
+hipError_t launch_head_stats(const HeadProblem& h, hipStream_t st) {
+  HeadArgs a = head_args(h);
+  a.v_end = h.p.V;
+  const int grid = h.p.n_tt * h.p.n_split;
+  const bool hv = h.p.w_hv_inplace, smooth = h.t.smoothing > 0.f;
+#define KD_HS(HV, S) launch_big<head_stats_kernel<HV, S>>(grid, HeadCfg::NT, HeadCfg::STATE_SMEM_BYTES, st, &a)
+  return hv ? (smooth ? KD_HS(true, true) : KD_HS(true, false)) : (smooth ? KD_HS(false, true) : KD_HS(false, false));
+#undef KD_HS
+}
+
+// dL/dz of a chunk on the lists: A_in p - q - U, where the tile kernel has written what it would be beside them.  One thread per entry.
+struct ListedArgs {
+  const int *meta, *rowmap, *list;
+  const float *q, *z;
+  const f32x4* rowinfo;
+  int K, v0, v_end, ldz, sets;
+  float c;
+  bf16_t* dz;
+};
+__global__ __launch_bounds__(256) void head_listed_kernel(const ListedArgs a) {
+  const int64_t i = flat_group() * 256 + threadIdx.x;
+  const int j = (int)(i / a.K), k = (int)(i - (int64_t)j * a.K);
+  if (j >= a.meta[META_N_VALID]) return;
+  const int64_t at = (int64_t)a.rowmap[j] * a.K + k;
+  const int v = a.list[at];
+  if (v < a.v0 || v >= a.v_end) return;
+  const f32x4 ri = a.rowinfo[j];
+  float x = fmaf(ri[3], fexp2(fmaxf(fmaf(a.z[(int64_t)j * a.K + k], a.c, -ri[0]), -1.0e38f)), -a.q[at]) - ri[2];
+  const int col = v - a.v0, c = col & 31, half = c >> 4, g = (c & 15) >> 2;
+  const int64_t to = dz_chunk(a.ldz, j >> 6, col >> 5, (j >> 4) & 3, 16 * g + (j & 15)) + 4 * half + (c & 3);
+  if (a.sets == 1) {
+    a.dz[to] = (bf16_t)x;
+    return;
+  }
+  const int64_t stride = (int64_t)a.meta[META_T_EFF] * a.ldz;
+  for (int p = 0; p < 3; ++p) {
+    const bf16_t o = (bf16_t)x;
+    x -= (float)o;
+    const int first = a.sets == 3 ? p : p == 0 ? 0 : p == 1 ? 3 : 5, n = a.sets == 3 ? 1 : 3 - p;
+    for (int s = 0; s < n; ++s) a.dz[to + (first + s) * stride] = o;
+  }
+}
+
+// The same from kept logits (the whole vocabulary is one chunk).  A workgroup makes 256 columns of a panel of 64 tokens, 4 KiB of
+// each 32; bound by memory, 6 bytes a logit.
+template <int PARTS>
+__global__ __launch_bounds__(256) void head_dz_kernel(const HeadArgs a) {
+  const int panel = blockIdx.y, panels = a.meta[META_T_EFF] >> 6;
+  if (panel >= panels) return;
+  const int lane = threadIdx.x & 63, blk = threadIdx.x >> 6, g = lane >> 4;
+  const int j = panel * 64 + 16 * blk + (lane & 15);
+  const bool token = j < a.meta[META_N_VALID];                           // (of others there may be no logits)
+  const f32x4 ri = a.rowinfo[j];
+  const int sub0 = blockIdx.x * 8, subs = (a.V + 63) / 64 * 2;
+  const int64_t stride = (int64_t)panels * 64 * a.ldz;
+#pragma unroll 4
+  for (int s = sub0; s < min(sub0 + 8, subs); ++s) {
+    const int64_t at = dz_chunk(a.ldz, panel, s, blk, lane);
+    const f32x4 lo = *(const f32x4*)(a.kept + at), hi = *(const f32x4*)(a.kept + at + 4);
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool there = token && s * 32 + 4 * g + (e < 4 ? 0 : 16) < a.V;       // (V is a multiple of 8)
+      const float d = unlisted_dz(ri, e < 4 ? lo[e & 3] : hi[e & 3], a.c, -ri[2]);
+      x[e] = there ? d : 0.f;
+    }
+    store_dz<PARTS>(x, a.dz + at, stride, a.sets);
+  }
+}
+
+hipError_t launch_head_grad(const HeadProblem& h, int v0, int width, hipStream_t st) {
+  const Problem& p = h.p;
+  HeadArgs a = head_args(h);
+  a.v0 = v0; a.v_end = v0 + width;
+  a.last_chunk = v0 + width >= p.V;
+  const int grid = p.n_tt * p.g_split;
+  const bool hv = p.w_hv_inplace, smooth = h.t.smoothing > 0.f, parts = p.dz_sets > 1;
+#define KD_HG(HV, S) (parts ? launch_big<head_grad_kernel<HV, S, 3>>(grid, HeadCfg::NT, HeadCfg::STATE_SMEM_BYTES, st, &a) \
+                            : launch_big<head_grad_kernel<HV, S, 1>>(grid, HeadCfg::NT, HeadCfg::STATE_SMEM_BYTES, st, &a))
+  hipError_t e = hipSuccess;
+  if (h.kept) {
+    const dim3 blocks((p.V + 255) / 256, p.T_pad / 64);
+    if (parts) hipLaunchKernelGGL(head_dz_kernel<3>, blocks, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(head_dz_kernel<1>, blocks, dim3(256), 0, st, a);
+    e = hipGetLastError();
+  } else {
+    e = hv ? (smooth ? KD_HG(true, true) : KD_HG(true, false)) : (smooth ? KD_HG(false, true) : KD_HG(false, false));
+  }
+#undef KD_HG
+  if (e != hipSuccess) return e;
+  const ListedArgs l{p.meta, p.rowmap, h.t.list, h.t.q, h.t.z, (const f32x4*)p.rowinfo, h.t.K, v0, v0 + width, p.V_c, p.dz_sets,
+                     1.4426950408889634f / p.tau, (bf16_t*)p.dz};
+  const FlatGrid g = flat_grid(((int64_t)p.T * h.t.K + 255) / 256);
+  hipLaunchKernelGGL(head_listed_kernel, dim3(g.x, g.y), dim3(256), 0, st, l);
+  return hipGetLastError();
+}
+
+}  // namespace kd

@@ -1,0 +1,37 @@
+// grad_W of the one-head losses: the kernels of kd_products.hpp with a scaled product.  dL/dz is kept without its factor
+// loss_scale / (n tau): that is one number for all tokens, and rounded into every entry it would shift all of them the same way (a label's
+// entry is near -1 for every token), so it multiplies the fp32 sums.  fp32 gradients contract several copies of the token axis (dz_sets).
+#include "kd_products.hpp"
+
+namespace kd {
+
+template <int NB, bool HV, bool F32, bool ADD>
+KD_STRIP_KERNEL void head_gw_kernel(const GradWArgs a) { grad_w<NB, HV, F32, ADD, true>(a); }
+template <bool HV, bool ADD>
+__global__ __launch_bounds__(256, 2) void head_gw_few_kernel(const GradWArgs a) { grad_w_few<HV, false, ADD, true>(a); }
+
+hipError_t launch_grad_W_scaled(const Problem& p, int v0, int width, hipStream_t st) {
+  const int nb = grad_W_tile(p.H_s, width, p.n_cu) / 64;
+  GradWArgs a = grad_w_args(p, v0, width, nb);
+  const bool add = p.accumulate_grad_W != 0;
+  if (p.n_tt == 1 && a.sets == 1) {
+    grad_w_few_args(p, width, a);
+#define KD_GF(HV, ADD) launch_big<head_gw_few_kernel<HV, ADD>>(a.n_vt * a.n_ht, 256, GradWFew::SMEM_BYTES, st, &a)
+    return p.w_hv ? (add ? KD_GF(true, true) : KD_GF(true, false)) : (add ? KD_GF(false, true) : KD_GF(false, false));
+#undef KD_GF
+  }
+  const int tiles = a.n_vt * a.n_ht, grid = tiles < p.n_cu ? tiles : p.n_cu;
+#define KD_GW3(N, HV, F32) (add ? launch_big<head_gw_kernel<N, HV, F32, true>>(grid, 256, StripShape<16, N>::SMEM_BYTES, st, &a) \
+                                : launch_big<head_gw_kernel<N, HV, F32, false>>(grid, 256, StripShape<16, N>::SMEM_BYTES, st, &a))
+#define KD_GW(N) (p.w_hv ? (p.grad_f32 ? KD_GW3(N, true, true) : KD_GW3(N, true, false)) \
+                         : (p.grad_f32 ? KD_GW3(N, false, true) : KD_GW3(N, false, false)))
+  switch (nb) {
+    case 2: return KD_GW(2);
+    case 3: return KD_GW(3);
+    default: return KD_GW(4);
+  }
+#undef KD_GW3
+#undef KD_GW
+}
+
+}  // namespace kd

@@ -162,43 +162,6 @@ __device__ __forceinline__ void make_rowmap(const RowmapArgs& a) {
   }
 }
 
-// Merging the partial sums.  Every workgroup (one per token tile and vocabulary range) leaves its values as [range][value][T_pad], and
-// with few tokens there are many ranges (256 at T <= 256; the eight-wave loop's four lanes of a token put theirs
-// together first: a step of T = 200, H = 2048 / 512, V = 32000 148 -> 133 us, AKL at T = 150, H = 1024 / 512 347 -> 291).  A merge is bound by the latency of its loads:
-// one thread walking all the parts of a token took 658 us at T = 256 and 47 us at T = 4096.  So a workgroup owns TX
-// tokens and NT / TX threads share the parts of each: lanes run along the tokens (TX = 8: 32-byte runs, TX = 32:
-// whole lines), the rest of the lanes and the waves along the parts; partial results meet by shuffles, then through
-// LDS, in a fixed order.  Measured: combine_kernel 658 -> 23 us at T = 256, 47 -> 9 us at 128 parts, 6 us at 32 (T = 4096),
-// one search merge of AKL 536 -> 15 us at T = 2048.
-struct MergeSum {
-  static __device__ __forceinline__ float op(float a, float b) { return a + b; }
-};
-struct MergeMax {
-  static __device__ __forceinline__ float op(float a, float b) { return fmaxf(a, b); }
-};
-// v[i] of every thread -> the merged value of the thread's token, in every thread of that token
-template <int TX, int NT, int NV, class Op>
-__device__ __forceinline__ void merge_parts(float (&v)[NV], float* lds) {
-  constexpr int NW = NT / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tx = lane % TX;
-#pragma unroll
-  for (int off = TX; off < 64; off <<= 1)
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = Op::op(v[i], __shfl_xor(v[i], off, 64));
-  __syncthreads();                       // the values of an earlier merge have been read
-  if (lane < TX)
-#pragma unroll
-    for (int i = 0; i < NV; ++i) lds[(wave * NV + i) * TX + tx] = v[i];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    float r = lds[i * TX + tx];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) r = Op::op(r, lds[(w * NV + i) * TX + tx]);
-    v[i] = r;
-  }
-}
-
 // Merge the partial statistics of one (compacted) token; write log-sum-exps and, for FKL / RKL, the
 // row loss.
 template <int TX, int NT>
@@ -502,6 +465,18 @@ __global__ void transpose_kernel(const E* src, int64_t ld_src, int R, int C, E* 
   }
 }
 
+// fp32 operands as bf16 parts laid side by side along K.  src_f32 == 1, the two-model losses: two parts, three products (see prepare);
+// src_f32 == 2, the one-head losses: three parts, f = f0 + f1 + f2 to 24 bits, and the six products of them that are not below
+// those bits, the head as [0 0 0 1 1 2], the hidden states as [0 1 2 0 1 0].
+__device__ __forceinline__ int part_of_six(int place, bool head) { return (head ? 0x211000 : 0x010210) >> (4 * place) & 15; }
+__device__ __forceinline__ bf16_t part_of(float f, int part) {
+  const bf16_t hi = (bf16_t)f;
+  if (part == 0) return hi;
+  const float rest = f - (float)hi;
+  const bf16_t mid = (bf16_t)rest;
+  return part == 1 ? mid : (bf16_t)(rest - (float)mid);
+}
+
 // The token operand of the strip loop: the compacted rows (row j = row rowmap[j] of src for j < n_valid, zero
 // beyond) in the order in which its waves load them: [64-token panel][32-element sub-step][16-token block][lane][8],
 // lane l holding elements 8 (l / 16) .. + 7 of token l mod 16.  fp32 rows become [hi | lo | hi] (see
@@ -527,15 +502,11 @@ __device__ __forceinline__ void pack_rows(int block, int tid, const void* src, i
       } else if (k0 < H) {
         v = *(const bf16x8*)((const bf16_t*)src + row + k0);
       }
-    } else if (k0 < 3 * H) {
-      const int part = k0 / H;                     // H is a multiple of 8: the eight values are of one part
-      const f32x4* x = (const f32x4*)((const float*)src + row + (k0 - part * H));
+    } else if (k0 < (src_f32 == 2 ? 6 : 3) * H) {
+      const int place = k0 / H, part = src_f32 == 2 ? part_of_six(place, false) : place == 1;      // H is a multiple of 8: the eight values are of one part
+      const f32x4* x = (const f32x4*)((const float*)src + row + (k0 - place * H));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float f = x[i >> 2][i & 3];
-        const bf16_t hi = (bf16_t)f;
-        v[i] = part == 1 ? (bf16_t)(f - (float)hi) : hi;
-      }
+      for (int i = 0; i < 8; ++i) v[i] = part_of(x[i >> 2][i & 3], part);
     }
   }
   *(bf16x8*)(dst + ((((int64_t)panel * (K / 32) + kb) * 4 + blk) * 64 + lane) * 8) = v;
@@ -556,9 +527,9 @@ __device__ __forceinline__ void prepare(int block, int tid, const void* src, int
   const int wide = (R + 15) / 16, by = block / wide, bx = block - by * wide;
   const int k0 = (by * 64 + (tid & 63)) * 8;
   if (k0 >= K) return;
-  const int part = src_f32 ? k0 / H : 0, col = k0 - part * H;      // H is a multiple of 8: eight values of one part
-  const bool lo = (split_mode == 1 && part == 2) || (split_mode == 2 && part == 1);
-  const bool pad = src_f32 ? part > 2 : k0 >= H;
+  const int place = src_f32 ? k0 / H : 0, col = k0 - place * H;      // H is a multiple of 8: eight values of one part
+  const int part = src_f32 == 2 ? part_of_six(place < 6 ? place : 0, split_mode == 1) : (split_mode == 1 && place == 2) || (split_mode == 2 && place == 1);
+  const bool pad = src_f32 ? place > (src_f32 == 2 ? 5 : 2) : k0 >= H;
   const int n = rowmap ? meta[META_N_VALID] : R;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -576,9 +547,7 @@ __device__ __forceinline__ void prepare(int block, int tid, const void* src, int
         const f32x4 x0 = x[0], x1 = x[1];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float f = e < 4 ? x0[e & 3] : x1[e & 3];
-          const bf16_t hi = (bf16_t)f;
-          v[e] = lo ? (bf16_t)(f - (float)hi) : hi;
+          v[e] = part_of(e < 4 ? x0[e & 3] : x1[e & 3], part);
         }
       }
     }
@@ -609,12 +578,11 @@ __global__ __launch_bounds__(256) void prepare_transposed_kernel(const void* src
     if (!src_f32) {
       if (c < K) row[c] = c < H ? hi : (bf16_t)0.f;
     } else {
-      if (c < H) {                     // [hi | hi | lo]
-        row[c] = hi;
-        row[H + c] = hi;
-        row[2 * H + c] = (bf16_t)(x - (float)hi);
+      const int parts = src_f32 == 2 ? 6 : 3;
+      if (c < H) {                     // [hi | hi | lo], or six
+        for (int place = 0; place < parts; ++place) row[place * H + c] = part_of(x, src_f32 == 2 ? part_of_six(place, true) : place == 2);
       }
-      if (3 * H + c < K && c < K - 3 * H) row[3 * H + c] = (bf16_t)0.f;      // the padding is shorter than 64
+      if (parts * H + c < K && c < K - parts * H) row[parts * H + c] = (bf16_t)0.f;      // the padding is shorter than 64
     }
   }
 }
@@ -839,7 +807,7 @@ static RowmapArgs rowmap_args(const Problem& p) {
   const int last = p.V - (p.V - 1) / p.V_c * p.V_c;      // width of the last chunk
   SplitChoice stats{p.n_vt, 1, 0, p.n_split, 0}, grad{1, 1, 0, 1, 0}, grad_last = grad;
   if (p.strip) {
-    const int per = StripCfg::BM / 64, sh = StripCfg::SHORT / 64, full = p.V < p.V_c ? p.V : p.V_c;
+    const int per = (p.head_rows ? p.head_rows : StripCfg::BM) / 64, sh = StripCfg::SHORT / 64, full = p.V < p.V_c ? p.V : p.V_c;
     auto choice = [&](int rows, int most, int short_units, int strided) {
       const int units = (rows + 63) / 64;
       return SplitChoice{units, per, short_units, most < units ? most : units, strided};
@@ -865,7 +833,7 @@ hipError_t launch_operands(const Problem& p, bool rowmap, bool student, bool tea
   // hidden states: packed for the strip loop; else copied where they are gathered, split or padded
   auto hidden = [&](const void* src, int H, void* dst, int K, bool fp8) {
     OperandJob j{};
-    j.src = src; j.dst = (bf16_t*)dst; j.src_f32 = p.in_f32 && !fp8;
+    j.src = src; j.dst = (bf16_t*)dst; j.src_f32 = p.in_f32 && !fp8 ? (p.f32_parts ? 2 : 1) : 0;
     j.R = p.T; j.H = H; j.K = K;
     if (fp8) { j.H /= 2; j.K /= 2; }      // rows of bytes as rows of two-byte words
     j.rowmap = p.mask ? p.rowmap : nullptr;
@@ -882,7 +850,7 @@ hipError_t launch_operands(const Problem& p, bool rowmap, bool student, bool tea
   };
   auto head = [&](const void* src, int H, void* dst, int K) {
     OperandJob j{};
-    j.src = src; j.dst = (bf16_t*)dst; j.src_f32 = p.in_f32;
+    j.src = src; j.dst = (bf16_t*)dst; j.src_f32 = p.in_f32 ? (p.f32_parts ? 2 : 1) : 0;
     j.R = p.V; j.H = H; j.K = K; j.mode = 1;
     add(false, j, (int64_t)((j.R + 15) / 16) * ((j.K + 511) / 512));
   };
@@ -901,7 +869,7 @@ hipError_t launch_operands(const Problem& p, bool rowmap, bool student, bool tea
   // heads kept as [H][V] that are not read in place: transposed copies
   auto turned = [&](const void* src, int H, void* dst, int K) {
     hipLaunchKernelGGL(prepare_transposed_kernel, dim3((p.V + 63) / 64, ((p.in_f32 ? H : K) + 63) / 64), dim3(256), 0, st, src,
-                       p.in_f32, p.V, H, (bf16_t*)dst, K);
+                       p.in_f32 ? (p.f32_parts ? 2 : 1) : 0, p.V, H, (bf16_t*)dst, K);
   };
   if (teacher && p.prep_Wt && p.t_fp8)      // e4m3 bytes
     hipLaunchKernelGGL(transpose_kernel<uint8_t>, dim3((p.K_t + 63) / 64, (p.V + 63) / 64), dim3(256), 0, st,

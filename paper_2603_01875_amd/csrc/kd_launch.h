@@ -75,7 +75,46 @@ struct Problem {
   void* h_sT;          // bf16, T_pad tokens x H_s rounded up to 16, packed (pack_columns)
   void* dz;            // bf16, T_pad x V_c, in the order of dz_chunk (kd_common.hpp)
   float* gh32;         // [n_ksplit_h][T][H_s]
+  // the one-head losses only (kd_head_api.hip), 0 otherwise
+  int head_rows;       // vocabulary rows per tile of their strip loop
+  int dz_sets;         // copies of the token axis in dz and h_sT (parts of fp32 factors); 0: one
+  int f32_parts;       // fp32 operands as six products of three bf16 parts instead of three of two
+  const float* out_scale;   // one device float that both gradients are multiplied by in fp32
 };
+
+// The one-head losses (kd_head_api.hip): cross entropy with labels and distillation from a teacher's top logits are one loss, the
+// divergence of the student from a distribution that is given on a list of entries per token (one for a label).
+struct Targets {
+  int ce;                  // labels: a list of one entry
+  int K;                   // entries per token
+  int index64, top_f32;    // types of the caller's arrays
+  int tail;                // kd_tail
+  float smoothing, z_loss; // labels only
+  const void* index;       // labels, or the entries' vocabulary rows
+  const void* top;         // teacher logits of the entries
+  const float* lse;
+  const uint8_t* mask;     // the caller's
+  // workspace
+  int* list;               // [T][K] vocabulary rows in ascending order, each once; kNoEntry behind them
+  float* q;                // [T][K] their probabilities
+  double* info;            // [T][kTargetInfo]
+  uint8_t* valid;          // [T] whether the token counts: the row map's mask
+  float* z;                // [T_pad][K] the student's logits of the entries, by compacted token
+  float* scale;            // loss_scale tau^2 / (n tau), what both gradients are multiplied by
+};
+constexpr int kNoEntry = 0x7fffffff;
+constexpr int kTargetInfo = 3;         // mass (of the list and of what stands for the rest), mass of the rest, sum q log q over both
+constexpr int kHeadRows = 256;         // vocabulary rows per tile
+// few: at most kFewHeadTokens tokens and [V][K] rows of whole k-steps, the head streams past tokens in LDS (kd_head_few.hip); kept: the logits are
+// kept in fp32, in dz's order, and turned into dz without multiplying again
+constexpr int kFewHeadTokens = 128;
+struct HeadProblem { Problem p; Targets t; int few, parts; float* kept; };
+hipError_t launch_targets(const HeadProblem& h, hipStream_t st);
+hipError_t launch_head_stats(const HeadProblem& h, hipStream_t st);
+hipError_t launch_head_few(const HeadProblem& h, hipStream_t st);
+hipError_t launch_head_combine(const HeadProblem& h, hipStream_t st);
+hipError_t launch_head_finalize(const HeadProblem& h, bool pack_h, hipStream_t st);
+hipError_t launch_head_grad(const HeadProblem& h, int v0, int width, hipStream_t st);
 
 // the row map (first teacher of a call), and the operand copies of the student and of the teacher that the call needs
 hipError_t launch_operands(const Problem& p, bool rowmap, bool student, bool teacher, hipStream_t st);
@@ -101,7 +140,10 @@ hipError_t launch_finalize(const Problem& p, bool pack_h_s, hipStream_t st);
 hipError_t launch_grad_chunk(const Problem& p, int v0, int width, bool accumulate, hipStream_t st);
 // the backward products on the chunk of `width` columns from v0; `first`: grad_h_s's parts are written, not added to
 hipError_t launch_grad_W(const Problem& p, int v0, int width, hipStream_t st);
-hipError_t launch_grad_h(const Problem& p, int v0, int width, bool first, hipStream_t st);
+// (set, W_offset: which copy of dz, and elements in front of the part of the head's rows that it is multiplied by)
+hipError_t launch_grad_h(const Problem& p, int v0, int width, bool first, hipStream_t st, int set = 0, int64_t W_offset = 0);
+// ... with the product times *p.out_scale, in front of the only rounding (kd_head_products.hip)
+hipError_t launch_grad_W_scaled(const Problem& p, int v0, int width, hipStream_t st);
 hipError_t launch_gradh_finish(const Problem& p, hipStream_t st);
 const char* build_info();     // compile-time configuration of the kernels (tile shapes)
 }  // namespace kd

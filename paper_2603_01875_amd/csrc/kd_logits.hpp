@@ -2,6 +2,7 @@
 // statistics, row sums or dL/dz_s, on either tile loop.  The kernels are in kd_kernels.hip and kd_strip_hv.hip.
 #pragma once
 #include "kd_common.hpp"
+#include "kd_logit_math.hpp"
 
 // tile configurations (overridable for tuning experiments)
 #ifndef KD_LOGIT_CFG
@@ -209,13 +210,6 @@ struct ChunkWork : ChunkMap {
 // ------------------------------------------------------------------------------------------
 // epilogues of the logit tiles
 // ------------------------------------------------------------------------------------------
-constexpr float NEG_BIG = -1.0e30f;   // logit given to vocabulary rows beyond V: every exp of it is 0
-// Running maxima start here, far below any real scaled logit and far above NEG_BIG * c (the host
-// bounds tau so that c > 1e-9): a lane that has seen only masked rows keeps this maximum, so the
-// exponent of a masked entry stays hugely negative instead of cancelling to a rounding residual.
-constexpr float M_FLOOR = -1.0e20f;
-constexpr float LN2 = 0.6931471805599453f;
-
 // Adaptive KL: per-token values kept between its passes, [AKL_ROWS][T_pad] floats.
 enum { AKL_FKL = 0, AKL_RKL = 1,   // the token's forward / reverse KL
        AKL_LO = 2, AKL_HI = 3,     // search interval of the head threshold (base-2 teacher log-probability):
@@ -233,9 +227,6 @@ constexpr int AKL_BINS = kAklBins;      // bins of a search pass of the strip lo
 __device__ __forceinline__ float akl_cell(float low, float ltmax) { return (ltmax + 1.0e-3f - low) * (1.f / kAklCells); }
 __device__ __forceinline__ float akl_edge(float j, float low, float cell) { return fmaf(j, cell, low); }
 constexpr float AKL_TOP_EPS = 1.0e-4f;   // entries this close (base-2 log) to the token's largest one count as "the top entry"
-
-__device__ __forceinline__ float fexp2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float flog2(float x) { return __builtin_amdgcn_logf(x); }
 
 // How a lane sees a finished tile: NC token columns of (up to) NE vocabulary entries each, entry e of the lane's
 // share lying at vocabulary row m(e) of the tile (four consecutive e are four consecutive rows), column j at
@@ -453,18 +444,6 @@ struct StatsEpi {
 // [token][8], one copy for the four lanes of a token, which merge what a tile adds to them; a token belongs to one wave, so there is
 // no barrier.  T = 4096, V = 151936, H = 4096 / 1024: statistics 4.33 -> 4.16 ms; with the gradient kernels' rows there, too, a step of
 // T = 4096 1.057 -> 1.062 (JSD 1.070) times the speed of the same earlier state, forward pass alone at T = 1003 1.004 -> 1.022.
-__device__ __forceinline__ float quad_max(float x) {          // over the lanes of a token, 16 and 32 apart
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
-}
-__device__ __forceinline__ float quad_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
-}
 template <int KIND>
 struct StripStatsEpi {
   static constexpr int NV = KIND == 6 ? 6 : 5;

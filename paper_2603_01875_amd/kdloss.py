@@ -13,6 +13,9 @@ import os
 FKL, RKL, JSD, TVD, SKEW_FKL, SKEW_RKL, AKL = 0, 1, 2, 3, 4, 5, 6
 BF16, F32 = 0, 1
 W_HV, W_VH = 0, 1
+I32, I64 = 0, 1
+TAIL_RENORM, TAIL_REST, TAIL_DROP = 0, 1, 2
+TOPK_MAX = 1024
 
 KD_OK = 0
 STATUS_NAMES = {0: "KD_OK", 1: "KD_ERR_NULL", 2: "KD_ERR_SHAPE", 3: "KD_ERR_ALIGN", 4: "KD_ERR_PARAM",
@@ -33,6 +36,24 @@ class KdLossParams(ctypes.Structure):
                 ("accumulate_grad_W", ctypes.c_int32), ("flags", ctypes.c_int32),
                 ("teacher_scale", ctypes.c_float), ("vocab_chunk", ctypes.c_int32),
                 ("loss_scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class KdCeParams(ctypes.Structure):
+    """kd_ce_params of the C header."""
+    _fields_ = [("T", ctypes.c_int64), ("H", ctypes.c_int64), ("V", ctypes.c_int64),
+                ("in_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("w_layout", ctypes.c_int32),
+                ("index_dtype", ctypes.c_int32), ("label_smoothing", ctypes.c_float), ("z_loss", ctypes.c_float),
+                ("loss_scale", ctypes.c_float), ("accumulate_grad_W", ctypes.c_int32), ("vocab_chunk", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class KdTopkParams(ctypes.Structure):
+    """kd_topk_params of the C header."""
+    _fields_ = [("T", ctypes.c_int64), ("H", ctypes.c_int64), ("V", ctypes.c_int64), ("K", ctypes.c_int32),
+                ("in_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("w_layout", ctypes.c_int32),
+                ("index_dtype", ctypes.c_int32), ("top_dtype", ctypes.c_int32), ("tail", ctypes.c_int32),
+                ("tau", ctypes.c_float), ("loss_scale", ctypes.c_float), ("accumulate_grad_W", ctypes.c_int32),
+                ("flags", ctypes.c_int32), ("vocab_chunk", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2)]
 
 
 class KdLossError(RuntimeError):
@@ -80,6 +101,16 @@ def lib():
                                             ctypes.POINTER(ctypes.c_float),
                                             vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.kd_loss_fwd_bwd_multi.restype = ctypes.c_int
+        C, Q = ctypes.POINTER(KdCeParams), ctypes.POINTER(KdTopkParams)
+        for size, params in ((L.kd_ce_workspace_size, C), (L.kd_topk_workspace_size, Q)):
+            size.argtypes = [params, ctypes.POINTER(ctypes.c_size_t)]
+            size.restype = ctypes.c_int
+        L.kd_ce_fwd.argtypes = [C] + [vp] * 7 + [ctypes.c_size_t, vp]
+        L.kd_ce_fwd_bwd.argtypes = [C] + [vp] * 9 + [ctypes.c_size_t, vp]
+        L.kd_topk_fwd.argtypes = [Q] + [vp] * 9 + [ctypes.c_size_t, vp]
+        L.kd_topk_fwd_bwd.argtypes = [Q] + [vp] * 11 + [ctypes.c_size_t, vp]
+        for call in (L.kd_ce_fwd, L.kd_ce_fwd_bwd, L.kd_topk_fwd, L.kd_topk_fwd_bwd):
+            call.restype = ctypes.c_int
         L.kd_quantize_e4m3.argtypes = [vp, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, vp, vp]
         L.kd_quantize_e4m3.restype = ctypes.c_int
         L.kd_loss_profile_clock.argtypes = [vp]
@@ -131,9 +162,12 @@ def quantize_e4m3(x, scale, out=None):
     return out
 
 
-def kd_loss_workspace_size(params: KdLossParams) -> int:
+def kd_loss_workspace_size(params) -> int:
+    """Workspace bytes of a call with this parameter block (KdLossParams, KdCeParams or KdTopkParams)."""
     n = ctypes.c_size_t(0)
-    st = lib().kd_loss_workspace_size(ctypes.byref(params), ctypes.byref(n))
+    query = {KdLossParams: lib().kd_loss_workspace_size, KdCeParams: lib().kd_ce_workspace_size,
+             KdTopkParams: lib().kd_topk_workspace_size}[type(params)]
+    st = query(ctypes.byref(params), ctypes.byref(n))
     if st != KD_OK:
         raise KdLossError(st)
     return int(n.value)
@@ -462,4 +496,214 @@ def kd_loss_fwd(h_t, W_t, h_s, W_s, mask=None, tau=1.0, kind=FKL, beta=0.5, w_la
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     ptl = torch.empty(T, dtype=torch.float32, device=dev)
     kd_loss_fwd_raw(p, h_t, W_t, h_s, W_s, mask, loss, ptl, workspace)
+    return dict(loss=loss, per_token_loss=ptl)
+
+
+# ------------------------------------------------------------------------------------------------
+# losses over one output head
+# ------------------------------------------------------------------------------------------------
+def make_ce_params(T, H, V, label_smoothing=0.0, z_loss=0.0, in_dtype=BF16, grad_dtype=None, w_layout=W_VH,
+                   index_dtype=I64, accumulate_grad_W=False, vocab_chunk=0, loss_scale=1.0):
+    return KdCeParams(int(T), int(H), int(V), int(in_dtype), int(in_dtype if grad_dtype is None else grad_dtype),
+                      int(w_layout), int(index_dtype), float(label_smoothing), float(z_loss), float(loss_scale),
+                      int(bool(accumulate_grad_W)), int(vocab_chunk), 0)
+
+
+def make_topk_params(T, H, V, K, tau=1.0, tail=TAIL_RENORM, in_dtype=BF16, grad_dtype=None, w_layout=W_VH,
+                     index_dtype=I64, top_dtype=F32, accumulate_grad_W=False, flags=0, vocab_chunk=0, loss_scale=1.0):
+    return KdTopkParams(int(T), int(H), int(V), int(K), int(in_dtype),
+                        int(in_dtype if grad_dtype is None else grad_dtype), int(w_layout), int(index_dtype),
+                        int(top_dtype), int(tail), float(tau), float(loss_scale), int(bool(accumulate_grad_W)),
+                        int(flags), int(vocab_chunk))
+
+
+def _float_dtype(t, name):
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    return BF16 if t.dtype == torch.bfloat16 else F32
+
+
+def _index_dtype(t, name):
+    import torch
+    if t.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"{name} must be int32 or int64, got {t.dtype}")
+    return I32 if t.dtype == torch.int32 else I64
+
+
+def _check_head(h, W, w_layout):
+    """Hidden states and head of the one-head losses: (T, H, V, in_dtype)."""
+    import torch
+    for n, t in (("h", h), ("W", W)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+            raise ValueError(f"{n} must be a 2-dimensional torch tensor")
+    if w_layout not in (W_HV, W_VH):
+        raise ValueError("unknown w_layout")
+    in_dtype = _float_dtype(h, "h")
+    if W.dtype != h.dtype:
+        raise ValueError(f"W is {W.dtype}, h is {h.dtype}")
+    T, H = h.shape
+    V, H_w = W.shape if w_layout == W_VH else (W.shape[1], W.shape[0])
+    if H_w != H:
+        raise ValueError(f"W has shape {tuple(W.shape)}, expected {'[V, H]' if w_layout == W_VH else '[H, V]'} with H = {H}")
+    return int(T), int(H), int(V), in_dtype
+
+
+def _check_tensors(need, dev):
+    """need: (name, tensor or None, dtypes, elements, may be None)."""
+    for n, t, dtypes, count, optional in need:
+        if t is None:
+            if optional:
+                continue
+            raise ValueError(f"{n} is needed")
+        if t.device != dev or not t.is_cuda:
+            raise ValueError(f"{n} must be a CUDA (HIP) tensor on {dev}, got {t.device}")
+        if not t.is_contiguous():
+            raise ValueError(f"{n} must be contiguous")
+        if t.dtype not in dtypes:
+            raise ValueError(f"{n} must be {' or '.join(map(str, dtypes))} here, got {t.dtype}")
+        if t.numel() != count:
+            raise ValueError(f"{n} has {t.numel()} elements, expected {count}")
+
+
+def _head_call(name, p, inputs, h, W, mask, loss, per_token_loss, grads, workspace, stream):
+    """Checks what a call of the one-head losses is given against its parameter block and makes it.
+    inputs: (name, tensor, dtypes, elements, optional) in front of h / behind W, with their place; grads: None or a pair."""
+    import torch
+    before, behind = inputs
+    fdt = (torch.bfloat16 if p.in_dtype == BF16 else torch.float32,)
+    gdt = (torch.bfloat16 if p.grad_dtype == BF16 else torch.float32,)
+    T, H, V = p.T, p.H, p.V
+    need = before + [("h", h, fdt, T * H, False), ("W", W, fdt, V * H, False)] + behind
+    need += [("mask", mask, (torch.uint8, torch.bool), T, True), ("loss", loss, (torch.float32,), 1, False),
+             ("per_token_loss", per_token_loss, (torch.float32,), T, True)]
+    if grads is not None:
+        need += [("grad_h", grads[0], gdt, T * H, True), ("grad_W", grads[1], gdt, V * H, True)]
+    dev = h.device
+    _check_tensors(need, dev)
+    if workspace is None or not workspace.is_cuda or workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA (HIP) tensor on the operands' device")
+    args = [_ptr(t) for _, t, *_ in before] + [_ptr(h), _ptr(W)] + [_ptr(t) for _, t, *_ in behind]
+    args += [_ptr(mask), _ptr(loss), _ptr(per_token_loss)] + ([] if grads is None else [_ptr(g) for g in grads])
+    with torch.cuda.device(dev):                   # the launches go to the operands' device, whatever the current one is
+        s = torch.cuda.current_stream().cuda_stream if stream is None else stream
+        st = getattr(lib(), name)(ctypes.byref(p), *args, _ptr(workspace), ctypes.c_size_t(_nbytes(workspace)),
+                                  ctypes.c_void_p(s))
+    if st != KD_OK:
+        raise KdLossError(st)
+
+
+def _label_inputs(p, labels):
+    import torch
+    return [], [("labels", labels, (torch.int32 if p.index_dtype == I32 else torch.int64,), p.T, False)]
+
+
+def _top_inputs(p, top_logits, top_index, lse):
+    import torch
+    return [("top_logits", top_logits, (torch.bfloat16 if p.top_dtype == BF16 else torch.float32,), p.T * p.K, False),
+            ("top_index", top_index, (torch.int32 if p.index_dtype == I32 else torch.int64,), p.T * p.K, False),
+            ("lse", lse, (torch.float32,), p.T, p.tail == TAIL_RENORM)], []
+
+
+def kd_ce_fwd_raw(params, h, W, labels, mask, loss, per_token_loss, workspace, stream=None):
+    """Thin call: all tensors are the caller's (mask and per_token_loss may be None)."""
+    _head_call("kd_ce_fwd", params, _label_inputs(params, labels), h, W, mask, loss, per_token_loss, None, workspace, stream)
+
+
+def kd_ce_fwd_bwd_raw(params, h, W, labels, mask, loss, per_token_loss, grad_h, grad_W, workspace, stream=None):
+    """Thin call: all tensors are the caller's (mask, per_token_loss and one of the gradients may be None)."""
+    _head_call("kd_ce_fwd_bwd", params, _label_inputs(params, labels), h, W, mask, loss, per_token_loss, (grad_h, grad_W),
+               workspace, stream)
+
+
+def kd_topk_fwd_raw(params, top_logits, top_index, lse, h_s, W_s, mask, loss, per_token_loss, workspace, stream=None):
+    """Thin call: all tensors are the caller's (mask and per_token_loss may be None, lse with TAIL_RENORM)."""
+    _head_call("kd_topk_fwd", params, _top_inputs(params, top_logits, top_index, lse), h_s, W_s, mask, loss, per_token_loss,
+               None, workspace, stream)
+
+
+def kd_topk_fwd_bwd_raw(params, top_logits, top_index, lse, h_s, W_s, mask, loss, per_token_loss, grad_h_s, grad_W_s,
+                        workspace, stream=None):
+    """Thin call: all tensors are the caller's (mask, per_token_loss and one of the gradients may be None, lse with
+    TAIL_RENORM)."""
+    _head_call("kd_topk_fwd_bwd", params, _top_inputs(params, top_logits, top_index, lse), h_s, W_s, mask, loss,
+               per_token_loss, (grad_h_s, grad_W_s), workspace, stream)
+
+
+def _head_outputs(p, h, W, workspace, grads, grad_W, want):
+    """Outputs (and the workspace unless given) of a convenience call."""
+    import torch
+    dev = h.device
+    if workspace is None:
+        workspace = alloc_workspace(p, dev)
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    ptl = torch.empty(p.T, dtype=torch.float32, device=dev)
+    if not grads:
+        return loss, ptl, None, None, workspace
+    tdt = torch.bfloat16 if p.grad_dtype == BF16 else torch.float32
+    grad_h = torch.empty(h.shape, dtype=tdt, device=dev) if want[0] else None
+    if grad_W is None and want[1]:
+        grad_W = torch.empty(W.shape, dtype=tdt, device=dev)
+    return loss, ptl, grad_h, grad_W, workspace
+
+
+def kd_ce_fwd_bwd(h, W, labels, mask=None, label_smoothing=0.0, z_loss=0.0, w_layout=W_VH, grad_dtype=None,
+                  workspace=None, grad_W=None, accumulate_grad_W=False, vocab_chunk=0, loss_scale=1.0,
+                  want_grad_h=True, want_grad_W=True):
+    """Cross entropy of `labels` ([T] int32 or int64; negative: the token does not count) under softmax(h W), and its
+    gradients.  h [T,H]; W in `w_layout`.  Allocates outputs (and the workspace unless given); returns a dict of tensors."""
+    T, H, V, in_dtype = _check_head(h, W, w_layout)
+    p = make_ce_params(T, H, V, label_smoothing, z_loss, in_dtype, grad_dtype, w_layout, _index_dtype(labels, "labels"),
+                       accumulate_grad_W, vocab_chunk, loss_scale)
+    if accumulate_grad_W and grad_W is None:
+        raise ValueError("accumulate_grad_W needs the grad_W to add to")
+    loss, ptl, gh, gW, ws = _head_outputs(p, h, W, workspace, True, grad_W, (want_grad_h, want_grad_W))
+    kd_ce_fwd_bwd_raw(p, h, W, labels, mask, loss, ptl, gh, gW, ws)
+    return dict(loss=loss, per_token_loss=ptl, grad_h=gh, grad_W=gW, workspace=ws)
+
+
+def kd_ce_fwd(h, W, labels, mask=None, label_smoothing=0.0, z_loss=0.0, w_layout=W_VH, workspace=None, loss_scale=1.0):
+    """The same without gradients."""
+    T, H, V, in_dtype = _check_head(h, W, w_layout)
+    p = make_ce_params(T, H, V, label_smoothing, z_loss, in_dtype, None, w_layout, _index_dtype(labels, "labels"),
+                       loss_scale=loss_scale)
+    loss, ptl, _, _, ws = _head_outputs(p, h, W, workspace, False, None, None)
+    kd_ce_fwd_raw(p, h, W, labels, mask, loss, ptl, ws)
+    return dict(loss=loss, per_token_loss=ptl)
+
+
+def _check_top(T, top_logits, top_index):
+    if top_index.dim() != 2 or top_index.shape[0] != T or top_logits.shape != top_index.shape:
+        raise ValueError(f"top_logits and top_index must be [T, K] with T = {T}, got {tuple(top_logits.shape)} and "
+                         f"{tuple(top_index.shape)}")
+    return int(top_index.shape[1]), _float_dtype(top_logits, "top_logits"), _index_dtype(top_index, "top_index")
+
+
+def kd_topk_fwd_bwd(top_logits, top_index, h_s, W_s, lse=None, mask=None, tau=1.0, tail=TAIL_RENORM, w_layout=W_VH,
+                    grad_dtype=None, workspace=None, grad_W_s=None, accumulate_grad_W=False, flags=0, vocab_chunk=0,
+                    loss_scale=1.0, want_grad_h=True, want_grad_W=True):
+    """Divergence of softmax(h_s W_s / tau) from the teacher's top logits ([T,K], with their vocabulary rows top_index, as
+    torch.topk returns them; negative rows are entries that are not there), and its gradients.  `tail` says what stands for
+    the rest of the teacher's vocabulary; lse [T] is the teacher's log-sum-exp of its logits over tau (not with
+    TAIL_RENORM).  Allocates outputs (and the workspace unless given); returns a dict of tensors."""
+    T, H, V, in_dtype = _check_head(h_s, W_s, w_layout)
+    K, top_dtype, index_dtype = _check_top(T, top_logits, top_index)
+    p = make_topk_params(T, H, V, K, tau, tail, in_dtype, grad_dtype, w_layout, index_dtype, top_dtype, accumulate_grad_W,
+                         flags, vocab_chunk, loss_scale)
+    if accumulate_grad_W and grad_W_s is None:
+        raise ValueError("accumulate_grad_W needs the grad_W_s to add to")
+    loss, ptl, gh, gW, ws = _head_outputs(p, h_s, W_s, workspace, True, grad_W_s, (want_grad_h, want_grad_W))
+    kd_topk_fwd_bwd_raw(p, top_logits, top_index, lse, h_s, W_s, mask, loss, ptl, gh, gW, ws)
+    return dict(loss=loss, per_token_loss=ptl, grad_h_s=gh, grad_W_s=gW, workspace=ws)
+
+
+def kd_topk_fwd(top_logits, top_index, h_s, W_s, lse=None, mask=None, tau=1.0, tail=TAIL_RENORM, w_layout=W_VH,
+                workspace=None, flags=0, loss_scale=1.0):
+    """The same without gradients."""
+    T, H, V, in_dtype = _check_head(h_s, W_s, w_layout)
+    K, top_dtype, index_dtype = _check_top(T, top_logits, top_index)
+    p = make_topk_params(T, H, V, K, tau, tail, in_dtype, None, w_layout, index_dtype, top_dtype, flags=flags,
+                         loss_scale=loss_scale)
+    loss, ptl, _, _, ws = _head_outputs(p, h_s, W_s, workspace, False, None, None)
+    kd_topk_fwd_raw(p, top_logits, top_index, lse, h_s, W_s, mask, loss, ptl, ws)
     return dict(loss=loss, per_token_loss=ptl)
