@@ -2,12 +2,14 @@
 //   targets  : the caller's labels or top logits -> per token a sorted list of entries with their probabilities, and whether it counts
 //   (row map and operand copies: operands_kernel, kd_kernels.hip)
 //   stats    : logit tiles -> running max and sum beside the lists, the logits on them (kd_head.hpp)
-//   combine  : log-sum-exp, the token's loss, the coefficients of its gradient
-//   finalize : n, loss, the gradients' common factor, h transposed for grad_W
+//   combine  : log-sum-exp, the token's loss, the coefficients of its gradient, n, loss, the gradients' common factor; beside it h
+//              transposed for grad_W
 //   per chunk of the vocabulary:
 //     grad   : logit tiles again -> dL/dz in the order of dz_chunk;  listed: its entries on the lists
+//              (few enough logits are kept and read instead: dz)
 //     the backward products (kd_products.hpp)
 //   gradh_finish
+// With few tokens (kd_head_few.hip) nothing is compacted: tokens that do not count are multiplied with the others, their results dropped.
 #include "kd_head.hpp"
 
 namespace kd {
@@ -15,12 +17,6 @@ namespace kd {
 // ------------------------------------------------------------------------------------------
 // targets
 // ------------------------------------------------------------------------------------------
-struct TargetArgs {
-  Targets t;
-  int T, V;
-  double inv_tau;
-};
-
 __device__ __forceinline__ double wave_sum(double x) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
@@ -32,18 +28,9 @@ __device__ __forceinline__ double wave_max(double x) {
   return x;
 }
 
-// An entry past the vocabulary makes its token NaN: it is never read, and the loss says so.
 __global__ __launch_bounds__(256) void label_targets_kernel(const TargetArgs a) {
   const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= a.T) return;
-  const int64_t y = a.t.index64 ? ((const int64_t*)a.t.index)[t] : (int64_t)((const int*)a.t.index)[t];
-  const bool out = y >= a.V;
-  a.t.valid[t] = y >= 0 && (!a.t.mask || a.t.mask[t]);
-  a.t.list[t] = y >= 0 && !out ? (int)y : kNoEntry;
-  a.t.q[t] = 1.f - a.t.smoothing;
-  double* const info = a.t.info + (int64_t)t * kTargetInfo;
-  info[0] = out ? __builtin_nan("") : 1.0;
-  info[1] = info[2] = 0.0;
+  if (t < a.T) (void)label_target(a, t);
 }
 
 // One wave per token.  The entries (absent: a negative row, or a logit of minus infinity) are put in ascending order by counting, for
@@ -116,11 +103,17 @@ __global__ __launch_bounds__(256) void top_targets_kernel(const TargetArgs a) {
   info[0] = bad || held != held ? __builtin_nan("") : held + rest;
   info[1] = rest;
   info[2] = ent + (rest > 0.0 ? rest * log(rest) : 0.0);
-  a.t.valid[t] = (n > 0 || bad) && (!a.t.mask || a.t.mask[t]);
+  const bool counts = (n > 0 || bad) && (!a.t.mask || a.t.mask[t]);
+  a.t.valid[t] = counts;
+  keep_places(a, t, counts);
+}
+
+TargetArgs target_args(const HeadProblem& h) {
+  return TargetArgs{h.t, h.p.T, h.p.V, 1.0 / (double)h.p.tau, h.few, h.p.meta, h.p.rowmap, h.p.inv};
 }
 
 hipError_t launch_targets(const HeadProblem& h, hipStream_t st) {
-  const TargetArgs a{h.t, h.p.T, h.p.V, 1.0 / (double)h.p.tau};
+  const TargetArgs a = target_args(h);
   if (h.t.ce) hipLaunchKernelGGL(label_targets_kernel, dim3((h.p.T + 255) / 256), dim3(256), 0, st, a);
   else hipLaunchKernelGGL(top_targets_kernel, dim3((h.p.T + 3) / 4), dim3(256), 64 * h.t.K, st, a);
   return hipGetLastError();
@@ -129,11 +122,23 @@ hipError_t launch_targets(const HeadProblem& h, hipStream_t st) {
 // ------------------------------------------------------------------------------------------
 // combine
 // ------------------------------------------------------------------------------------------
+struct PackHArgs {         // h transposed for grad_W: see pack_columns (kd_kernels.hip), `sets` copies of the token axis
+  const void* src;
+  bf16_t* dst;
+  int src_f32, C, sets, T_pad;
+  const int *meta, *rowmap, *inv;
+};
+struct LossSumArgs {
+  const int *meta, *rowmap, *inv;
+  const float* row_loss;
+  float tau, weight;
+  float *loss, *scale;
+};
 struct HeadCombineArgs {
   const float* partials;
   const int* meta;
-  const int* rowmap;
-  int T_pad, nv, K, n_parts;           // n_parts: 0 = the device's plan
+  const int *rowmap, *inv;
+  int T, T_pad, nv, K, n_parts;        // n_parts: 0 = the device's plan
   float c, uniform, z_loss;            // uniform: U
   const int* list;
   const float* q;
@@ -141,89 +146,11 @@ struct HeadCombineArgs {
   const double* info;
   f32x4* rowinfo;
   float* row_loss;
-};
-
-// Merges a token's partial sums and its listed logits.  Logarithms in base 2; what is a difference of large quantities in double.
-template <int TX, int NT>
-__global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs a) {
-  __shared__ float lds[NT / 64 * 5 * TX];
-  const int t = blockIdx.x * TX + threadIdx.x % TX, g = threadIdx.x / TX, G = NT / TX;
-  const int n_valid = a.meta[META_N_VALID], n_parts = a.n_parts ? a.n_parts : a.meta[META_N_SPLIT];
-  if (t >= n_valid && g == 0) {        // padding rows: everything evaluates to 0
-    a.rowinfo[t] = f32x4{1.0e30f, 0.f, 0.f, 0.f};
-    a.row_loss[t] = 0.f;
-  }
-  if ((int)(blockIdx.x * TX) >= n_valid) return;
-  const int64_t stride = (int64_t)a.nv * a.T_pad;
-  const float* const q0 = a.partials + t;              // t < T_pad: allocated, whatever the row holds
-  const int64_t token = a.rowmap[t];
-  const int* const list = a.list + token * a.K;
-  const float* const prob = a.q + token * a.K;
-  const float* const z = a.z + (int64_t)t * a.K;
-  float m[2] = {M_FLOOR, M_FLOOR};
-#pragma unroll 4
-  for (int p = g; p < n_parts; p += G) m[0] = fmaxf(m[0], q0[p * stride]);
-  for (int k = g; k < a.K && list[k] != kNoEntry; k += G) m[1] = fmaxf(m[1], z[k] * a.c);
-  merge_parts<TX, NT, 2, MergeMax>(m, lds);
-  float v[5] = {0.f, 0.f, 0.f, 0.f, 0.f};              // sum beside the list, on it, sum of logits, sum q (z - max), entries
-#pragma unroll 4
-  for (int p = g; p < n_parts; p += G) {
-    const float* const q = q0 + p * stride;
-    v[0] = fmaf(q[a.T_pad], fexp2(q[0] - m[0]), v[0]);
-    if (a.nv == 3) v[2] += q[2 * a.T_pad];
-  }
-  for (int k = g; k < a.K && list[k] != kNoEntry; k += G) {
-    const float d = fmaf(z[k], a.c, -m[1]);
-    v[1] += fexp2(d);
-    v[2] += z[k];
-    v[3] = fmaf(prob[k], d, v[3]);
-    v[4] += prob[k];
-  }
-  merge_parts<TX, NT, 5, MergeSum>(v, lds);
-  if (g != 0 || t >= n_valid) return;
-  const double ln2 = 0.6931471805599453;
-  const double* const info = a.info + token * kTargetInfo;
-  const double mass = info[0], rest = info[1], ent = info[2];
-  const double lo = v[0] == 0.f ? -INFINITY : (double)m[0] + log2((double)v[0]);     // beside the list
-  const double ll = v[1] == 0.f ? -INFINITY : (double)m[1] + log2((double)v[1]);
-  const double big = fmax(lo, ll), lse = v[0] != v[0] || v[1] != v[1] ? __builtin_nan("") : big + log2(exp2(lo - big) + exp2(ll - big));
-  const double nat = lse * ln2;
-  const double on = v[4] != 0.f ? (double)v[3] + (double)m[1] * (double)v[4] : 0.0;   // sum q z in base 2
-  double loss = ent + mass * nat - ln2 * on - (double)a.uniform * (double)v[2] + (double)a.z_loss * nat * nat;
-  const double in = mass + 2.0 * (double)a.z_loss * nat;
-  double out = in;
-  if (rest > 0.0) {
-    loss -= rest * lo * ln2;
-    out -= rest * exp2(lse - lo);
-  }
-  // (the log-sum-exp as a float is up to 1e-6 off, the same way for all of a token's entries: that goes into the coefficients)
-  const float high = (float)lse;
-  const double corr = exp2((double)high - lse);
-  a.rowinfo[t] = f32x4{high, (float)(out * corr), a.uniform, (float)(in * corr)};
-  a.row_loss[t] = (float)loss;
-}
-
-hipError_t launch_head_combine(const HeadProblem& h, hipStream_t st) {
-  const Problem& p = h.p;
-  const HeadCombineArgs a{p.partials, p.meta, p.rowmap, p.T_pad, h.t.smoothing > 0.f ? 3 : 2, h.t.K, h.few ? h.parts : 0, 1.4426950408889634f / p.tau,
-                          h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.t.info, (f32x4*)p.rowinfo, p.row_loss};
-  if ((h.few ? h.parts : p.n_split) >= 128) hipLaunchKernelGGL((head_combine_kernel<8, 1024>), dim3(p.T_pad / 8), dim3(1024), 0, st, a);
-  else hipLaunchKernelGGL((head_combine_kernel<32, 256>), dim3(p.T_pad / 32), dim3(256), 0, st, a);
-  return hipGetLastError();
-}
-
-// ------------------------------------------------------------------------------------------
-// finalize
-// ------------------------------------------------------------------------------------------
-struct HeadFinalizeArgs {
-  const int *meta, *inv, *rowmap;
-  const float* row_loss;
-  int T, T_pad;
-  float tau, weight;
-  float *loss, *per_token, *scale;
-  const void* src;         // h, for grad_W: its columns packed (see pack_columns, kd_kernels.hip), `sets` copies of the token axis
-  bf16_t* dst;
-  int src_f32, C, sets;
+  float weight;
+  float* per_token;
+  int groups;              // workgroups that combine; those behind them pack h
+  LossSumArgs sum;
+  PackHArgs pack;
 };
 
 // Which bf16 part of h stands against copy s of dL/dz: dz 0 0 0 1 1 2 x h 0 1 2 0 1 0, or dz 0 1 2 x h itself.
@@ -236,59 +163,173 @@ __device__ __forceinline__ bf16_t h_part(float f, int s, int sets) {
   return part == 1 ? mid : (bf16_t)(rest - (float)mid);
 }
 
-__global__ __launch_bounds__(1024) void head_finalize_kernel(const HeadFinalizeArgs a) {
-  __shared__ double s_sum[1024];
-  __shared__ float tile[64][65];
-  const int tid = threadIdx.x, n = a.meta[META_N_VALID];
-  if (flat_group() > 0) {
-    const int b = (int)(flat_group() - 1), wide = a.T_pad / 64, by = b / wide, r0 = (b - by * wide) * 64, c0 = by * 64;
-    const int eff = a.meta[META_T_EFF];
-    if (c0 >= a.C || r0 >= eff) return;
-    const int tx = tid & 63, ty = tid >> 6, c = c0 + tx, cc = min(c, a.C - 1);
-    float v[4];
+// Block b of 64 tokens x 64 hidden rows, by NT threads.
+template <int NT>
+__device__ __forceinline__ void pack_h(const PackHArgs& a, int b, float (*tile)[65]) {
+  const int wide = a.T_pad / 64, by = b / wide, r0 = (b - by * wide) * 64, c0 = by * 64;
+  const int eff = a.meta[META_T_EFF], n = a.meta[META_N_VALID];
+  if (c0 >= a.C || r0 >= eff) return;
+  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6, c = c0 + tx, cc = min(c, a.C - 1);
+  constexpr int ROWS = 4096 / NT;
+  float v[ROWS];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {          // (rowmap holds a valid row for every r < T_pad)
-      const int64_t at = (int64_t)a.rowmap[r0 + ty + 16 * i] * a.C + cc;
-      v[i] = a.src_f32 ? ((const float*)a.src)[at] : (float)((const bf16_t*)a.src)[at];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) tile[ty + 16 * i][tx] = r0 + ty + 16 * i < n && c < a.C ? v[i] : 0.f;
-    __syncthreads();
-    const int sub = ty >> 2, blk = ty & 3;                             // a wave: 16 hidden rows x 32 tokens, 1 KiB
-    if (sub > 1 || c0 + 16 * blk >= a.C) return;
-    for (int s = 0; s < a.sets; ++s) {
-      bf16x8 o;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = h_part(tile[32 * sub + 8 * (tx >> 4) + e][16 * blk + (tx & 15)], s, a.sets);
-      *(bf16x8*)(a.dst + ((int64_t)(c0 / 16 + blk) * (a.T_pad / 32 * a.sets) + (s * eff + r0) / 32 + sub) * 512 + tx * 8) = o;
-    }
-    return;
+  for (int i = 0; i < ROWS; ++i) {         // (rowmap holds a token for every r < T_pad)
+    const int r = r0 + ty + NT / 64 * i, token = a.rowmap[r];
+    const int64_t at = (int64_t)token * a.C + cc;
+    v[i] = a.src_f32 ? ((const float*)a.src)[at] : (float)((const bf16_t*)a.src)[at];
+    if (r >= n || c >= a.C || a.inv[token] < 0) v[i] = 0.f;
   }
-  double acc = 0.0;
-  for (int j = tid; j < n; j += 1024) acc += (double)a.row_loss[j];
-  s_sum[tid] = acc;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) tile[ty + NT / 64 * i][tx] = v[i];
   __syncthreads();
-  for (int s = 512; s > 0; s >>= 1) {
-    if (tid < s) s_sum[tid] += s_sum[tid + s];
-    __syncthreads();
+  for (int p = ty; p < 8 * a.sets; p += NT / 64) {                     // a wave: 16 hidden rows x 32 tokens, 1 KiB
+    const int s = p >> 3, sub = (p >> 2) & 1, blk = p & 3;
+    if (c0 + 16 * blk >= a.C) continue;
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = h_part(tile[32 * sub + 8 * (tx >> 4) + e][16 * blk + (tx & 15)], s, a.sets);
+    *(bf16x8*)(a.dst + ((int64_t)(c0 / 16 + blk) * (a.T_pad / 32 * a.sets) + (s * eff + r0) / 32 + sub) * 512 + tx * 8) = o;
   }
-  if (tid == 0) {
-    *a.loss = n > 0 ? a.weight * (float)(s_sum[0] / (double)n) : 0.f;
-    *a.scale = n > 0 ? a.weight / ((float)n * a.tau) : 0.f;
-  }
-  if (a.per_token)
-    for (int t = tid; t < a.T; t += 1024) {
-      const int j = a.inv[t];
-      a.per_token[t] = j >= 0 ? a.weight * a.row_loss[j] : 0.f;
-    }
 }
 
-hipError_t launch_head_finalize(const HeadProblem& h, bool pack_h, hipStream_t st) {
+// The mean of the losses of the tokens that count, summed in a fixed order, and the gradients' common factor.
+template <int NT>
+__device__ __forceinline__ void sum_losses(const LossSumArgs& a, double* sums) {
+  const int n_valid = a.meta[META_N_VALID];
+  double acc = 0.0;
+  int n = 0;
+  for (int j = threadIdx.x; j < n_valid; j += NT) {
+    acc += (double)a.row_loss[j];
+    n += a.inv[a.rowmap[j]] >= 0;
+  }
+  double total = 0.0;
+  for (int pass = 0; pass < 2; ++pass) {
+    sums[threadIdx.x] = pass ? (double)n : acc;
+    __syncthreads();
+    for (int s = NT / 2; s > 0; s >>= 1) {
+      if ((int)threadIdx.x < s) sums[threadIdx.x] += sums[threadIdx.x + s];
+      __syncthreads();
+    }
+    if (pass == 0) {
+      total = sums[0];
+      __syncthreads();
+    }
+  }
+  if (threadIdx.x == 0) {
+    const double count = sums[0];
+    *a.loss = count > 0.0 ? a.weight * (float)(total / count) : 0.f;
+    *a.scale = count > 0.0 ? a.weight / ((float)count * a.tau) : 0.f;
+  }
+}
+
+// Merges a token's partial sums and its listed logits.  Logarithms in base 2; what is a difference of large quantities in double.
+template <int TX, int NT>
+__global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs a) {
+  constexpr int BYTES = sizeof(float) * 64 * 65;
+  __shared__ __attribute__((aligned(16))) char shared[BYTES];
+  if (flat_group() >= a.groups) {
+    if (a.pack.src) pack_h<NT>(a.pack, (int)(flat_group() - a.groups), (float(*)[65])shared);
+    return;
+  }
+  float* const lds = (float*)shared;
+  static_assert(NT / 64 * 5 * TX * 4 <= BYTES && NT * 8 <= BYTES, "the merges' and the sum's share");
+  const int t = blockIdx.x * TX + threadIdx.x % TX, g = threadIdx.x / TX, G = NT / TX;
+  const int n_valid = a.meta[META_N_VALID], n_parts = a.n_parts ? a.n_parts : a.meta[META_N_SPLIT];
+  const int64_t token = a.rowmap[t];
+  const bool counts = t < n_valid && a.inv[token] >= 0;
+  if (a.groups == 1)                     // (rows behind the workgroup's)
+    for (int j = TX + threadIdx.x; j < a.T_pad; j += NT) a.rowinfo[j] = f32x4{1.0e30f, 0.f, 0.f, 0.f};
+  if (!counts && g == 0) {             // everything evaluates to 0
+    a.rowinfo[t] = f32x4{1.0e30f, 0.f, 0.f, 0.f};
+    a.row_loss[t] = 0.f;
+  }
+  if (g == 0 && t < a.T && a.per_token && a.inv[t] < 0) a.per_token[t] = 0.f;
+  if ((int)(blockIdx.x * TX) < n_valid) {
+    const int64_t stride = (int64_t)a.nv * a.T_pad;
+    const float* const q0 = a.partials + t;            // t < T_pad: allocated, whatever the row holds
+    const int* const list = a.list + token * a.K;
+    const float* const prob = a.q + token * a.K;
+    const float* const z = a.z + (int64_t)t * a.K;
+    float m[2] = {M_FLOOR, M_FLOOR};
+#pragma unroll 4
+    for (int p = g; p < n_parts; p += G) m[0] = fmaxf(m[0], q0[p * stride]);
+    for (int k = g; k < a.K && list[k] != kNoEntry; k += G) m[1] = fmaxf(m[1], z[k] * a.c);
+    merge_parts<TX, NT, 2, MergeMax>(m, lds);
+    float v[5] = {0.f, 0.f, 0.f, 0.f, 0.f};            // sum beside the list, on it, sum of logits, sum q (z - max), sum q
+#pragma unroll 4
+    for (int p = g; p < n_parts; p += G) {
+      const float* const q = q0 + p * stride;
+      v[0] = fmaf(q[a.T_pad], fexp2(q[0] - m[0]), v[0]);
+      if (a.nv == 3) v[2] += q[2 * a.T_pad];
+    }
+    for (int k = g; k < a.K && list[k] != kNoEntry; k += G) {
+      const float d = fmaf(z[k], a.c, -m[1]);
+      v[1] += fexp2(d);
+      v[2] += z[k];
+      v[3] = fmaf(prob[k], d, v[3]);
+      v[4] += prob[k];
+    }
+    merge_parts<TX, NT, 5, MergeSum>(v, lds);
+    if (g == 0 && counts) {
+      const double ln2 = 0.6931471805599453;
+      const double* const info = a.info + token * kTargetInfo;
+      const double mass = info[0], rest = info[1], ent = info[2];
+      const double lo = v[0] == 0.f ? -INFINITY : (double)m[0] + log2((double)v[0]);     // beside the list
+      const double ll = v[1] == 0.f ? -INFINITY : (double)m[1] + log2((double)v[1]);
+      const double big = fmax(lo, ll), lse = v[0] != v[0] || v[1] != v[1] ? __builtin_nan("") : big + log2(exp2(lo - big) + exp2(ll - big));
+      const double nat = lse * ln2;
+      const double on = v[4] != 0.f ? (double)v[3] + (double)m[1] * (double)v[4] : 0.0;   // sum q z in base 2
+      double loss = ent + mass * nat - ln2 * on - (double)a.uniform * (double)v[2] + (double)a.z_loss * nat * nat;
+      const double in = mass + 2.0 * (double)a.z_loss * nat;
+      double out = in;
+      if (rest > 0.0) {
+        loss -= rest * lo * ln2;
+        out -= rest * exp2(lse - lo);
+      }
+      // (the log-sum-exp as a float is up to 1e-6 off, the same way for all of a token's entries: that goes into the coefficients)
+      const float high = (float)lse;
+      const double corr = exp2((double)high - lse);
+      a.rowinfo[t] = f32x4{high, (float)(out * corr), a.uniform, (float)(in * corr)};
+      a.row_loss[t] = (float)loss;
+      if (a.per_token) a.per_token[token] = a.weight * (float)loss;
+    }
+  }
+  if (a.groups == 1) {
+    __syncthreads();                     // (one workgroup has written all the losses)
+    sum_losses<NT>(a.sum, (double*)shared);
+  }
+}
+
+// ... of more workgroups than one, in a launch of its own unless the gradients' first launch does it.  (The combining workgroup that is
+// done last can not do it cheaply: what it needs is in eight L2 caches, and a fence that writes one back took 10 us and more.)
+__global__ __launch_bounds__(1024) void head_sum_kernel(const LossSumArgs a) {
+  __shared__ double sums[1024];
+  sum_losses<1024>(a, sums);
+}
+
+static LossSumArgs loss_sum_args(const HeadProblem& h) {
   const Problem& p = h.p;
-  const HeadFinalizeArgs a{p.meta, p.inv, p.rowmap, p.row_loss, p.T, p.T_pad, p.tau, p.out_weight, p.loss, p.per_token_loss, h.t.scale,
-                           p.user_h_s, (bf16_t*)p.h_sT, p.in_f32, p.H_s, p.dz_sets};
-  const FlatGrid g = flat_grid(1 + (pack_h ? (int64_t)(p.T_pad / 64) * ((p.H_s + 63) / 64) : 0));
-  hipLaunchKernelGGL(head_finalize_kernel, dim3(g.x, g.y), dim3(1024), 0, st, a);
+  return LossSumArgs{p.meta, p.rowmap, p.inv, p.row_loss, p.tau, p.out_weight, p.loss, h.t.scale};
+}
+
+hipError_t launch_head_combine(const HeadProblem& h, bool backward, bool pack_h, hipStream_t st) {
+  const Problem& p = h.p;
+  // 8 tokens x 128 threads where a token has many parts, 32 x 8 else (see merge_parts); 32 x 32 where that is all the tokens
+  const bool all = p.T <= 32, many = !all && (h.few ? h.parts : p.n_split) >= 128;
+  HeadCombineArgs a{p.partials, p.meta, p.rowmap, p.inv, p.T, p.T_pad, h.t.smoothing > 0.f ? 3 : 2, h.t.K, h.few ? h.parts : 0,
+                    1.4426950408889634f / p.tau, h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.t.info,
+                    (f32x4*)p.rowinfo, p.row_loss, p.out_weight, p.per_token_loss, all ? 1 : many ? p.T_pad / 8 : p.T_pad / 32,
+                    loss_sum_args(h), {}};
+  int64_t groups = a.groups;
+  if (pack_h) {
+    a.pack = PackHArgs{p.user_h_s, (bf16_t*)p.h_sT, p.in_f32, p.H_s, p.dz_sets, p.T_pad, p.meta, p.rowmap, p.inv};
+    groups += (int64_t)(p.T_pad / 64) * ((p.H_s + 63) / 64);
+  }
+  const FlatGrid g = flat_grid(groups);
+  if (all) hipLaunchKernelGGL((head_combine_kernel<32, 1024>), dim3(g.x, g.y), dim3(1024), 0, st, a);
+  else if (many) hipLaunchKernelGGL((head_combine_kernel<8, 1024>), dim3(g.x, g.y), dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((head_combine_kernel<32, 256>), dim3(g.x, g.y), dim3(256), 0, st, a);
+  if (!all && !(h.kept && backward)) hipLaunchKernelGGL(head_sum_kernel, dim3(1), dim3(1024), 0, st, a.sum);
   return hipGetLastError();
 }
 
@@ -340,7 +381,7 @@ __global__ __launch_bounds__(256) void head_listed_kernel(const ListedArgs a) {
   const int v = a.list[at];
   if (v < a.v0 || v >= a.v_end) return;
   const f32x4 ri = a.rowinfo[j];
-  float x = fmaf(ri[3], fexp2(fmaxf(fmaf(a.z[(int64_t)j * a.K + k], a.c, -ri[0]), -1.0e38f)), -a.q[at]) - ri[2];
+  float x = listed_dz(ri, a.z[(int64_t)j * a.K + k], a.c, a.q[at]);
   const int col = v - a.v0, c = col & 31, half = c >> 4, g = (c & 15) >> 2;
   const int64_t to = dz_chunk(a.ldz, j >> 6, col >> 5, (j >> 4) & 3, 16 * g + (j & 15)) + 4 * half + (c & 3);
   if (a.sets == 1) {
@@ -356,28 +397,80 @@ __global__ __launch_bounds__(256) void head_listed_kernel(const ListedArgs a) {
   }
 }
 
-// The same from kept logits (the whole vocabulary is one chunk).  A workgroup makes 256 columns of a panel of 64 tokens, 4 KiB of
-// each 32; bound by memory, 6 bytes a logit.
+// All of it from kept logits (the whole vocabulary is one chunk).  A workgroup makes 256 columns of a panel of 64 tokens, 4 KiB of
+// each 32; bound by memory, 6 bytes a logit.  Which of them are listed stands in LDS, a word per token and 32 columns.
+struct KeptArgs {
+  HeadArgs h;
+  const int* inv;
+  const float* q;
+  LossSumArgs sum;         // (if the merge has not done it: loss not null)
+};
 template <int PARTS>
-__global__ __launch_bounds__(256) void head_dz_kernel(const HeadArgs a) {
-  const int panel = blockIdx.y, panels = a.meta[META_T_EFF] >> 6;
+__global__ __launch_bounds__(256) void head_dz_kernel(const KeptArgs k) {
+  __shared__ uint32_t listed[64][8];
+  __shared__ int first[64], whose[64];
+  const HeadArgs& a = k.h;
+  __shared__ double sums[256];
+  if (blockIdx.y == 0) {
+    if (blockIdx.x == 0 && k.sum.loss) sum_losses<256>(k.sum, sums);
+    return;
+  }
+  const int panel = blockIdx.y - 1, panels = a.meta[META_T_EFF] >> 6;
   if (panel >= panels) return;
-  const int lane = threadIdx.x & 63, blk = threadIdx.x >> 6, g = lane >> 4;
-  const int j = panel * 64 + 16 * blk + (lane & 15);
-  const bool token = j < a.meta[META_N_VALID];                           // (of others there may be no logits)
-  const f32x4 ri = a.rowinfo[j];
-  const int sub0 = blockIdx.x * 8, subs = (a.V + 63) / 64 * 2;
+  const int sub0 = blockIdx.x * 8, subs = min((a.V + 63) / 64 * 2 - sub0, 8);
+  const int lane = threadIdx.x & 63, blk = threadIdx.x >> 6, g = lane >> 4, i = 16 * blk + (lane & 15);
+  f32x4 z[8][2];                             // (all on their way before the lists are looked at; behind the last sub-step the last again)
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    const float* const from = a.kept + dz_chunk(a.ldz, panel, sub0 + min(s, subs - 1), blk, lane);
+    z[s][0] = *(const f32x4*)from;
+    z[s][1] = *(const f32x4*)(from + 4);
+  }
+  const f32x4 ri = a.rowinfo[panel * 64 + i];
+  if (threadIdx.x < 64) {
+    const int i = threadIdx.x, j = panel * 64 + i;
+    const int token = j < a.meta[META_N_VALID] ? a.rowmap[j] : -1;
+    const bool counts = token >= 0 && k.inv[token] >= 0;
+    *(u32x4*)listed[i] = u32x4{0u, 0u, 0u, 0u};
+    *(u32x4*)(listed[i] + 4) = u32x4{0u, 0u, 0u, 0u};
+    whose[i] = counts ? token : -1;
+    if (counts) {
+      const int* const list = a.list + (int64_t)token * a.n_list;
+      int at = first_entry(list, a.n_list, 32 * sub0);
+      first[i] = at;
+      for (; at < a.n_list; ++at) {
+        const int col = list[at] - 32 * sub0;
+        if (col >= 256) break;
+        listed[i][col >> 5] |= 1u << (col & 31);
+      }
+    }
+  }
+  __syncthreads();
+  const int token = whose[i];                                              // (of tokens that do not count there may be no logits)
   const int64_t stride = (int64_t)panels * 64 * a.ldz;
-#pragma unroll 4
-  for (int s = sub0; s < min(sub0 + 8, subs); ++s) {
-    const int64_t at = dz_chunk(a.ldz, panel, s, blk, lane);
-    const f32x4 lo = *(const f32x4*)(a.kept + at), hi = *(const f32x4*)(a.kept + at + 4);
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    if (s >= subs) break;
+    const int64_t at = dz_chunk(a.ldz, panel, sub0 + s, blk, lane);
+    const uint32_t word = listed[i][s], mine = (word >> (4 * g)) & 0x000f000fu;
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const bool there = token && s * 32 + 4 * g + (e < 4 ? 0 : 16) < a.V;       // (V is a multiple of 8)
-      const float d = unlisted_dz(ri, e < 4 ? lo[e & 3] : hi[e & 3], a.c, -ri[2]);
+      const bool there = token >= 0 && (sub0 + s) * 32 + 4 * g + (e < 4 ? 0 : 16) < a.V;       // (V is a multiple of 8)
+      const float d = unlisted_dz(ri, z[s][e >> 2][e & 3], a.c, -ri[2]);
       x[e] = there ? d : 0.f;
+    }
+    if (mine) {
+      int rank = first[i];
+      for (int w = 0; w < s; ++w) rank += __popc(listed[i][w]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int bit = (e < 4 ? 0 : 16) + (e & 3);
+        if (mine >> bit & 1) {
+          const int n = rank + __popc(word & ((1u << (bit + 4 * g)) - 1));
+          x[e] = listed_dz(ri, a.z[(int64_t)(panel * 64 + i) * a.n_list + n], a.c, k.q[(int64_t)token * a.n_list + n]);
+        }
+      }
     }
     store_dz<PARTS>(x, a.dz + at, stride, a.sets);
   }
@@ -394,10 +487,12 @@ hipError_t launch_head_grad(const HeadProblem& h, int v0, int width, hipStream_t
                             : launch_big<head_grad_kernel<HV, S, 1>>(grid, HeadCfg::NT, HeadCfg::STATE_SMEM_BYTES, st, &a))
   hipError_t e = hipSuccess;
   if (h.kept) {
-    const dim3 blocks((p.V + 255) / 256, p.T_pad / 64);
-    if (parts) hipLaunchKernelGGL(head_dz_kernel<3>, blocks, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(head_dz_kernel<1>, blocks, dim3(256), 0, st, a);
-    e = hipGetLastError();
+    const dim3 blocks((p.V + 255) / 256, p.T_pad / 64 + 1);
+    KeptArgs k{a, p.inv, h.t.q, loss_sum_args(h)};
+    if (p.T <= 32) k.sum.loss = nullptr;
+    if (parts) hipLaunchKernelGGL(head_dz_kernel<3>, blocks, dim3(256), 0, st, k);
+    else hipLaunchKernelGGL(head_dz_kernel<1>, blocks, dim3(256), 0, st, k);
+    return hipGetLastError();
   } else {
     e = hv ? (smooth ? KD_HG(true, true) : KD_HG(true, false)) : (smooth ? KD_HG(false, true) : KD_HG(false, false));
   }

@@ -18,7 +18,10 @@ struct HeadCfg : StripShape<kHeadRows / 16, 4> {
   static constexpr int HELD_V = 16, HELD_A = 12;     // (of two accumulators: unused)
   static constexpr int SHORT = 64;                   // a workgroup's last tile, if it has at most so many rows: see StripCfg
   // behind the stages: 32 bytes per token of what lasts from tile to tile, and 32 bytes per token of which rows of the tile are listed
-  static constexpr int STATE_AT = SMEM_BYTES, LISTED_AT = STATE_AT + 32 * BN, STATE_SMEM_BYTES = LISTED_AT + 32 * BN;
+  // ... and the entries of its list that come next
+  static constexpr int AHEAD = 16;
+  static constexpr int STATE_AT = SMEM_BYTES, LISTED_AT = STATE_AT + 32 * BN, NEXT_AT = LISTED_AT + 32 * BN;
+  static constexpr int STATE_SMEM_BYTES = NEXT_AT + 4 * (AHEAD + 1) * BN;
   static_assert(STATE_SMEM_BYTES <= 160 * 1024, "LDS of a gfx950 CU");
 };
 
@@ -42,6 +45,52 @@ struct HeadArgs {
   bf16_t* dz;
   int ldz, sets;
 };
+
+struct TargetArgs {
+  Targets t;
+  int T, V;
+  double inv_tau;
+  int identity;            // few tokens: there is no row map; this launch writes that every token is its own row
+  int *meta, *rowmap, *inv;
+};
+
+// What the row map leaves behind (make_rowmap, kd_kernels.hip), for tokens that all keep their places: inv says which count.
+__device__ __forceinline__ void keep_places(const TargetArgs& a, int t, bool counts) {
+  if (!a.identity) return;
+  a.rowmap[t] = t;
+  a.inv[t] = counts ? t : -1;
+  if (t == 0) {
+    a.meta[META_N_VALID] = a.T;
+    a.meta[META_N_TT] = 1;
+    a.meta[META_T_EFF] = (a.T + 63) / 64 * 64;
+    a.meta[META_N_SPLIT] = a.meta[META_G_SPLIT] = a.meta[META_G_SPLIT_LAST] = 1;
+  }
+  for (int i = a.T + t; i < kTileN; i += a.T) a.rowmap[i] = a.T - 1;
+}
+
+// A label's entry, kNoEntry where there is none.  One past the vocabulary makes its token NaN: it is never read, and the loss says so.
+__device__ __forceinline__ int64_t label_of(const TargetArgs& a, int t) {
+  return a.t.index64 ? ((const int64_t*)a.t.index)[t] : (int64_t)((const int*)a.t.index)[t];
+}
+__device__ __forceinline__ int label_row(const TargetArgs& a, int t) {
+  const int64_t y = label_of(a, t);
+  return y >= 0 && y < a.V ? (int)y : kNoEntry;
+}
+// ... written down as what later kernels take
+__device__ __forceinline__ int label_target(const TargetArgs& a, int t) {
+  const int64_t y = label_of(a, t);
+  const bool out = y >= a.V, counts = y >= 0 && (!a.t.mask || a.t.mask[t]);
+  const int row = y >= 0 && !out ? (int)y : kNoEntry;
+  a.t.valid[t] = counts;
+  keep_places(a, t, counts);
+  a.t.list[t] = row;
+  a.t.q[t] = 1.f - a.t.smoothing;
+  double* const info = a.t.info + (int64_t)t * kTargetInfo;
+  info[0] = out ? __builtin_nan("") : 1.0;
+  info[1] = info[2] = 0.0;
+  return row;
+}
+TargetArgs target_args(const HeadProblem& h);  // kd_head.hip
 
 // One workgroup: see StripWork (kd_logits.hpp), with tiles of four units.
 template <bool HV>
@@ -129,9 +178,11 @@ struct HeadStatsEpi {
   const HeadArgs& a;
   float* all;
   uint64_t* listed;
+  int* ahead;              // [AHEAD][token]: entry k of the list in row k mod AHEAD; behind them the first that is not there
   __device__ HeadStatsEpi(const HeadArgs& a_, char* smem, int tt, int row0) : a(a_) {
     all = (float*)(smem + HeadCfg::STATE_AT);
     listed = (uint64_t*)(smem + HeadCfg::LISTED_AT);
+    ahead = (int*)(smem + HeadCfg::NEXT_AT) + threadIdx.x;
     float* const own = all + threadIdx.x * 8;
     int* const owni = (int*)own;
     *(f32x4*)own = f32x4{M_FLOOR, 0.f, 0.f, 0.f};
@@ -141,9 +192,20 @@ struct HeadStatsEpi {
       token = a.rowmap[j];
       const int* const list = a.list + (int64_t)token * a.n_list;
       at = first_entry(list, a.n_list, row0);
-      if (at < a.n_list) next = list[at];
+      next = fetch(list, at);
     }
     owni[4] = next; owni[5] = owni[6] = at; owni[7] = token;
+  }
+  // Entries at .. of the list into the ring; the first of them.  (Read when it is needed, an entry costs a tile the time of a load and of
+  // all that are in flight.)
+  __device__ __forceinline__ int fetch(const int* list, int at) const {
+    int v[HeadCfg::AHEAD];
+#pragma unroll
+    for (int i = 0; i < HeadCfg::AHEAD; ++i) v[i] = list[min(at + i, a.n_list - 1)];
+#pragma unroll
+    for (int i = 0; i < HeadCfg::AHEAD; ++i) ahead[((at + i) % HeadCfg::AHEAD) * HeadCfg::BN] = at + i < a.n_list ? v[i] : kNoEntry;
+    ahead[HeadCfg::AHEAD * HeadCfg::BN] = at + HeadCfg::AHEAD;
+    return at < a.n_list ? v[0] : kNoEntry;
   }
   __device__ __forceinline__ void begin_item(const StripItem& it) {
     int* const own = (int*)(all + threadIdx.x * 8);
@@ -154,12 +216,12 @@ struct HeadStatsEpi {
     own[6] = at;
     const int end = it.m0 + it.a_rows;
     if (next < end) {
-      const int* const list = a.list + (int64_t)own[7] * a.n_list;
       do {
         const int row = next - it.m0, e = 4 * (row >> 4) + (row & 3), g = (row >> 2) & 3;
         bits[2 * g + (e >> 5)] |= 1u << (e & 31);
         ++at;
-        next = at < a.n_list ? list[at] : kNoEntry;
+        next = at < ahead[HeadCfg::AHEAD * HeadCfg::BN] ? ahead[(at % HeadCfg::AHEAD) * HeadCfg::BN]
+                                                        : fetch(a.list + (int64_t)own[7] * a.n_list, at);
       } while (next < end);
       own[4] = next; own[5] = at;
     }
@@ -172,11 +234,14 @@ struct HeadStatsEpi {
       const int e = mine ? __builtin_ctzll(mine) : 4096, block = e >> 2, r = e & 3;
       float v = 0.f;
 #pragma unroll
-      for (int i = 0; i < NE / 4; ++i)
-        if (__any(block == i)) {
+      for (int q = 0; q < NE / 16; ++q)
+        if (__any((e >> 4) == q)) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (block == i && r == k) { v = T[4 * i + k]; T[4 * i + k] = NEG_BIG; }
+          for (int k = 0; k < 16; ++k) {
+            const bool it = e == 16 * q + k;
+            v = it ? T[16 * q + k] : v;
+            T[16 * q + k] = it ? NEG_BIG : T[16 * q + k];
+          }
         }
       if (mine) {
         int rank = ((const int*)all)[n * 8 + 6];       // entries of the list in front of this row
@@ -253,6 +318,10 @@ __device__ __forceinline__ void store_dz(float (&x)[8], bf16_t* to, int64_t stri
 // keeps its NaN through A_out.)
 __device__ __forceinline__ float unlisted_dz(const f32x4& ri, float z, float c, float u) {
   return fmaf(ri[1], fexp2(fmaxf(fmaf(z, c, -ri[0]), -1.0e38f)), u);
+}
+
+__device__ __forceinline__ float listed_dz(const f32x4& ri, float z, float c, float q) {
+  return fmaf(ri[3], fexp2(fmaxf(fmaf(z, c, -ri[0]), -1.0e38f)), -q) - ri[2];
 }
 
 // dL/dz of a tile, without its common factor (Targets::scale): A_out p - U, in bf16 (PARTS 1), or as three bf16 parts that hold 24 bits,

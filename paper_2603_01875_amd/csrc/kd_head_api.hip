@@ -19,6 +19,9 @@ using kd::round_up;
 // Most bytes of logits that a call with gradients keeps in its workspace, in fp32, instead of making them twice.
 constexpr int64_t kKept = 160ll << 20;
 
+// Most bytes of grad_h's partial sums for which the products of its parts get sums of their own.
+constexpr int64_t kPartialSums = 128ll << 20;
+
 struct HeadLayout {
   size_t meta, rowmap, inv, row_loss, rowinfo, scale, valid, list, q, info, z;
   size_t prep_h, prep_W, partials, h_sT, dz, gh32, kept;
@@ -108,18 +111,36 @@ void plan(const Call& c, HeadProblem& h, HeadLayout& L, bool backward) {
   const int64_t v_all = round_up(q.V, 256);
   int64_t vc = c.vocab_chunk;
   if (vc == 0) {
-    vc = kd::choose_chunk(q, v_all, q.K_s);
+    // From 4096 tokens on 32768 columns, twice what the two-model losses take: a chunk's ends weigh more beside one model's products.
+    // (T = 4096, H = 1024, V = 151936 3908 -> 3860 us, H = 2048, V = 128256 6503 -> 6432, T = 8192, H = 2048 13956 -> 13676.)
+    vc = q.T_pad >= 4096 ? 32768 : kd::choose_chunk(q, v_all, q.K_s);
     while (vc > 1024 && (int64_t)q.T_pad * q.dz_sets * vc * 2 > (512ll << 20)) vc = round_up(vc / 2, 256);
   }
   q.V_c = (int)(vc < v_all ? vc : v_all);
-  kd::plan_grad_h(q, false);
+  q.gh_pairs = q.dz_sets;
+  if (q.T <= kd::kFewHeadTokens) {                     // parts that fill all places for workgroups, of at least eight k-steps
+    const int steps = ((q.V < q.V_c ? q.V : q.V_c) + 63) / 64, tiles = (q.H_s + 127) / 128 * q.dz_sets;
+    int parts = kd::kFewGradHGroups / tiles;
+    if (parts > steps / 8) parts = steps / 8;
+    if (parts < 1) parts = 1;
+    q.gh_rows = 128;
+    q.ksteps_h = (steps + parts - 1) / parts;
+    q.n_ksplit_h = (steps + q.ksteps_h - 1) / q.ksteps_h;
+  } else {
+    kd::plan_grad_h(q, false, q.dz_sets);
+    if (q.dz_sets > 1 && (int64_t)q.n_ksplit_h * q.dz_sets * q.T * q.H_s * 4 > kPartialSums) {
+      q.gh_pairs = 1;
+      kd::plan_grad_h(q, false);
+    }
+  }
 
   const bool keeps = backward && q.V_c == v_all && (int64_t)q.T_pad * v_all * 4 <= kKept;
   h.few = q.T <= kd::kFewHeadTokens && !q.w_hv_inplace && q.K_s == (q.prep_Ws ? q.K_s : q.H_s) && (keeps || !backward);
   if (h.few) {
     const int units32 = (q.V + 31) / 32;
     h.parts = units32 < q.n_cu ? units32 : q.n_cu;
-    q.strip = 0;                                       // (tokens as rows)
+    q.strip = 0;                                       // (tokens as rows, where they lie if they are whole k-steps of bf16)
+    q.prep_hs = q.in_f32 || q.K_s != q.H_s;
   }
 
   t.ce = c.ce; t.K = c.K; t.index64 = c.index_dtype == KD_I64; t.top_f32 = c.top_dtype == KD_F32; t.tail = c.tail;
@@ -138,16 +159,16 @@ void plan(const Call& c, HeadProblem& h, HeadLayout& L, bool backward) {
   L.q = take((size_t)q.T * t.K * 4);
   L.info = take((size_t)q.T * kd::kTargetInfo * 8);
   L.z = take((size_t)q.T_pad * t.K * 4);
-  L.prep_h = take((size_t)q.T_pad * q.K_s * 2);
+  L.prep_h = q.prep_hs ? take((size_t)q.T_pad * q.K_s * 2) : 0;
   L.prep_W = q.prep_Ws ? take((size_t)q.V * q.K_s * 2) : 0;
   const size_t partial_bytes = (size_t)(h.few ? h.parts : q.n_split) * (c.smoothing > 0.f ? 3 : 2) * q.T_pad * 4;
-  L.partials = off;                                    // read for the last time before the backward pass writes its first byte
+  L.h_sT = backward ? take((size_t)round_up(q.H_s, 16) * q.T_pad * q.dz_sets * 2) : 0;      // (packed beside the merge of the partials)
+  L.partials = off;                                    // read for the last time before the backward pass writes what lies there
   if (backward) {
-    L.h_sT = take((size_t)round_up(q.H_s, 16) * q.T_pad * q.dz_sets * 2);
     L.dz = take((size_t)q.T_pad * q.dz_sets * q.V_c * 2);
-    L.gh32 = take((size_t)q.n_ksplit_h * q.T * q.H_s * 4);
+    L.gh32 = take((size_t)q.n_ksplit_h * q.gh_pairs * q.T * q.H_s * 4);
   } else {
-    L.h_sT = L.dz = L.gh32 = off;
+    L.dz = L.gh32 = off;
   }
   const size_t end = (size_t)round_up((int64_t)(L.partials + partial_bytes), 256);
   if (off < end) off = end;
@@ -178,9 +199,9 @@ void carve(HeadProblem& h, const HeadLayout& L, void* ws) {
   t.info = reinterpret_cast<double*>(b + L.info);
   t.z = reinterpret_cast<float*>(b + L.z);
   if (h.kept) h.kept = reinterpret_cast<float*>(b + L.kept);
-  q.mask = t.valid;                                    // which tokens the row map keeps
+  q.mask = h.few ? nullptr : t.valid;                  // which tokens the row map keeps
   q.user_h_s = q.h_s; q.user_W_s = q.W_s;
-  q.h_s = b + L.prep_h;
+  if (q.prep_hs) q.h_s = b + L.prep_h;
   if (q.prep_Ws) q.W_s = b + L.prep_W;
 }
 
@@ -189,29 +210,39 @@ void carve(HeadProblem& h, const HeadLayout& L, void* ws) {
     if ((expr) != hipSuccess) return KD_ERR_LAUNCH; \
   } while (0)
 
-// The pairs of parts whose products make grad_h: copy of dL/dz, part of W's rows (places of the prepared head: part 0 first, part 1
-// fourth, part 2 sixth).
-struct PartPair { int set, place; };
-constexpr PartPair kPairs6[6] = {{0, 0}, {0, 3}, {3, 0}, {0, 5}, {5, 0}, {3, 3}}, kPairs3[3] = {{0, 0}, {1, 0}, {2, 0}};
+// The products that make grad_h: a copy of dL/dz by a part of W's rows (places of the prepared head: part 0 first, part 1 fourth,
+// part 2 sixth).
+constexpr int kPairSet6[6] = {0, 0, 3, 0, 5, 3}, kPairPlace6[6] = {0, 3, 0, 5, 0, 3};
+
+kd::GradHPairs grad_h_pairs(const Problem& q) {
+  kd::GradHPairs pairs{q.dz_sets, {}, {}};
+  for (int i = 0; i < pairs.n; ++i) {
+    pairs.set[i] = pairs.n == 6 ? kPairSet6[i] : i;
+    pairs.at[i] = pairs.n == 6 ? kPairPlace6[i] * q.H_s : 0;
+  }
+  return pairs;
+}
 
 kd_status run(const HeadProblem& h, bool backward, hipStream_t st) {
   const Problem& q = h.p;
-  KD_TRY(kd::launch_targets(h, st));
-  KD_TRY(kd::launch_operands(q, true, true, false, st));
+  if (!(h.few && h.t.ce)) KD_TRY(kd::launch_targets(h, st));
+  KD_TRY(kd::launch_operands(q, !h.few, true, false, st));
   KD_TRY(h.few ? kd::launch_head_few(h, st) : kd::launch_head_stats(h, st));
-  KD_TRY(kd::launch_head_combine(h, st));
-  KD_TRY(kd::launch_head_finalize(h, backward && q.grad_W_s, st));
+  KD_TRY(kd::launch_head_combine(h, backward, backward && q.grad_W_s, st));
   if (!backward) return KD_OK;
   for (int64_t v0 = 0; v0 < q.V; v0 += q.V_c) {
     const int width = (int)((q.V - v0 < q.V_c) ? q.V - v0 : q.V_c);
     KD_TRY(kd::launch_head_grad(h, (int)v0, width, st));
     if (q.grad_W_s) KD_TRY(kd::launch_grad_W_scaled(q, (int)v0, width, st));
     if (q.grad_h_s) {
-      const int n = q.dz_sets;
-      for (int i = 0; i < n; ++i) {
-        const PartPair pair = n == 6 ? kPairs6[i] : n == 3 ? kPairs3[i] : PartPair{0, 0};
-        KD_TRY(kd::launch_grad_h(q, (int)v0, width, v0 == 0 && i == 0, st, pair.set, (int64_t)pair.place * q.H_s));
-      }
+      // all products in one launch, or, where their partial sums would take too much memory, each adding to those of the one before
+      const kd::GradHPairs all = grad_h_pairs(q);
+      if (q.gh_pairs > 1) KD_TRY(kd::launch_head_grad_h(q, (int)v0, width, v0 == 0, st, &all));
+      else
+        for (int i = 0; i < all.n; ++i) {
+          const kd::GradHPairs one{1, {all.set[i]}, {all.at[i]}};
+          KD_TRY(kd::launch_head_grad_h(q, (int)v0, width, v0 == 0 && i == 0, st, &one));
+        }
     }
   }
   if (q.grad_h_s) KD_TRY(kd::launch_gradh_finish(q, st));

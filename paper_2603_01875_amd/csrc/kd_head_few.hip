@@ -19,6 +19,11 @@ struct FewCfg {
   static_assert(ALL_SMEM_BYTES <= 160 * 1024, "LDS of a gfx950 CU");
 };
 
+struct FewArgs {
+  HeadArgs h;
+  TargetArgs t;            // labels are taken as they are, lists have been made of top logits
+};
+
 // A range of the vocabulary, in units of 32 rows, in tiles of 256.
 struct FewItem { int n0, rows; };                      // first row, rows that exist
 struct FewWork {
@@ -134,18 +139,23 @@ struct FewEpi {
   const HeadArgs& a;
   char* const smem;
   int lane, wave, flip, n_valid, panels;
-  __device__ FewEpi(const HeadArgs& a_, char* s, int row0) : a(a_), smem(s), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), flip(1) {
-    n_valid = meta_get(a.meta, META_N_VALID);
-    panels = meta_get(a.meta, META_T_EFF) >> 6;
+  __device__ FewEpi(const FewArgs& k, char* s, int row0) : a(k.h), smem(s), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), flip(1) {
+    n_valid = a.T;
+    panels = (a.T + 63) >> 6;
     for (int i = threadIdx.x; i < 4 * C::BM; i += 256) *(f32x4*)(smem + C::SUMS_AT + 16 * i) = f32x4{M_FLOOR, 0.f, 0.f, 0.f};
     const int j = threadIdx.x;
     if (j >= C::BM) return;
     int next = kNoEntry, at = 0, token = 0;
     if (j < n_valid) {
-      token = a.rowmap[j];
-      const int* const list = a.list + (int64_t)token * a.n_list;
-      at = first_entry(list, a.n_list, row0);
-      if (at < a.n_list) next = list[at];
+      token = j;
+      if (k.t.t.ce) {                        // (the first workgroup writes lists of them, for what comes later)
+        const int y = blockIdx.x == 0 ? label_target(k.t, j) : label_row(k.t, j);
+        if (y >= row0) next = y;
+      } else {
+        const int* const list = a.list + (int64_t)token * a.n_list;
+        at = first_entry(list, a.n_list, row0);
+        if (at < a.n_list) next = list[at];
+      }
     }
     int* const own = (int*)(smem + C::LIST_AT) + 4 * j;
     own[0] = next; own[1] = at; own[2] = token;
@@ -263,16 +273,17 @@ struct FewEpi {
 };
 
 template <int MB, bool SMOOTH>
-KD_STRIP_KERNEL void head_few_kernel(const HeadArgs a) {
+KD_STRIP_KERNEL void head_few_kernel(const FewArgs k) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  FewWork work(a);
-  FewEpi<MB, SMOOTH> epi(a, smem, work.row0);
-  few_loop<MB>(a, work, epi, smem);
+  FewWork work(k.h);
+  FewEpi<MB, SMOOTH> epi(k, smem, work.row0);
+  few_loop<MB>(k.h, work, epi, smem);
   epi.write(blockIdx.x);
 }
+
 hipError_t launch_head_few(const HeadProblem& h, hipStream_t st) {
-  HeadArgs a = head_args(h);
-  a.T = h.p.T;
+  FewArgs a{head_args(h), target_args(h)};
+  a.h.T = h.p.T;
   const bool smooth = h.t.smoothing > 0.f;
 #define KD_FEW(MB) (smooth ? launch_big<head_few_kernel<MB, true>>(h.parts, 256, FewCfg<MB>::ALL_SMEM_BYTES, st, &a) \
                            : launch_big<head_few_kernel<MB, false>>(h.parts, 256, FewCfg<MB>::ALL_SMEM_BYTES, st, &a))

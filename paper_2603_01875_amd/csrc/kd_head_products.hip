@@ -10,6 +10,25 @@ KD_STRIP_KERNEL void head_gw_kernel(const GradWArgs a) { grad_w<NB, HV, F32, ADD
 template <bool HV, bool ADD>
 __global__ __launch_bounds__(256, 2) void head_gw_few_kernel(const GradWArgs a) { grad_w_few<HV, false, ADD, true>(a); }
 
+// grad_h with few tokens: bound by the head, which streams through once, so by how much of it is in flight.  The accumulator of 64 NB
+// tokens leaves room for two workgroups a CU, 32 KiB each on their way (and the stores of one under the products of the other).
+template <int NB, bool HV>
+__global__ __launch_bounds__(256, 2) void head_gh_few_kernel(const GradHArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  GradHWork<8, HV, NB> work(a);
+  GradHEpi<8, NB> epi(a);
+  strip_loop<1, false, StripShape<8, NB>, HV ? A_ROWS_DZ : A_KMAJOR_DZ>(work, epi, smem);
+}
+
+hipError_t launch_head_grad_h(const Problem& p, int v0, int width, bool first, hipStream_t st, const GradHPairs* pairs) {
+  if (p.T > kFewHeadTokens) return launch_grad_h(p, v0, width, first, st, pairs);
+  const GradHArgs a = grad_h_args(p, v0, width, first, pairs);
+  const int tiles = a.n_ht * a.n_split * a.n_pairs, grid = tiles < kFewGradHGroups ? tiles : kFewGradHGroups;
+#define KD_GHF(NB, HV) launch_big<head_gh_few_kernel<NB, HV>>(grid, 256, StripShape<8, NB>::SMEM_BYTES, st, &a)
+  return p.T <= 64 ? (p.w_hv_inplace ? KD_GHF(1, true) : KD_GHF(1, false)) : (p.w_hv_inplace ? KD_GHF(2, true) : KD_GHF(2, false));
+#undef KD_GHF
+}
+
 hipError_t launch_grad_W_scaled(const Problem& p, int v0, int width, hipStream_t st) {
   const int nb = grad_W_tile(p.H_s, width, p.n_cu) / 64;
   GradWArgs a = grad_w_args(p, v0, width, nb);

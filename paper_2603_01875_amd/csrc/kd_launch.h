@@ -26,6 +26,10 @@ inline int grad_W_tile(int64_t H_s, int64_t width, int n_cu) {
   return best;
 }
 
+// The one-head losses take kernels of their own with at most so many tokens; grad_h_s then has so many workgroups at a time.
+constexpr int kFewHeadTokens = 128;
+constexpr int kFewGradHGroups = 2 * kNumCU;
+
 // Shape of a grid of `groups` workgroups of up to 1024 threads that are numbered in a row (kernels: flat_group).  A grid has fewer
 // than 2^32 threads along one axis, so beyond 2^21 workgroups it takes a second one, and the last row has some too many.
 struct FlatGrid { uint32_t x, y; };
@@ -78,6 +82,7 @@ struct Problem {
   // the one-head losses only (kd_head_api.hip), 0 otherwise
   int head_rows;       // vocabulary rows per tile of their strip loop
   int dz_sets;         // copies of the token axis in dz and h_sT (parts of fp32 factors); 0: one
+  int gh_pairs;        // products that have partial sums of grad_h_s of their own; 0: one
   int f32_parts;       // fp32 operands as six products of three bf16 parts instead of three of two
   const float* out_scale;   // one device float that both gradients are multiplied by in fp32
 };
@@ -107,13 +112,12 @@ constexpr int kTargetInfo = 3;         // mass (of the list and of what stands f
 constexpr int kHeadRows = 256;         // vocabulary rows per tile
 // few: at most kFewHeadTokens tokens and [V][K] rows of whole k-steps, the head streams past tokens in LDS (kd_head_few.hip); kept: the logits are
 // kept in fp32, in dz's order, and turned into dz without multiplying again
-constexpr int kFewHeadTokens = 128;
 struct HeadProblem { Problem p; Targets t; int few, parts; float* kept; };
 hipError_t launch_targets(const HeadProblem& h, hipStream_t st);
 hipError_t launch_head_stats(const HeadProblem& h, hipStream_t st);
 hipError_t launch_head_few(const HeadProblem& h, hipStream_t st);
-hipError_t launch_head_combine(const HeadProblem& h, hipStream_t st);
-hipError_t launch_head_finalize(const HeadProblem& h, bool pack_h, hipStream_t st);
+// (with the losses' sum, unless a backward pass on kept logits does it)
+hipError_t launch_head_combine(const HeadProblem& h, bool backward, bool pack_h, hipStream_t st);
 hipError_t launch_head_grad(const HeadProblem& h, int v0, int width, hipStream_t st);
 
 // the row map (first teacher of a call), and the operand copies of the student and of the teacher that the call needs
@@ -140,9 +144,12 @@ hipError_t launch_finalize(const Problem& p, bool pack_h_s, hipStream_t st);
 hipError_t launch_grad_chunk(const Problem& p, int v0, int width, bool accumulate, hipStream_t st);
 // the backward products on the chunk of `width` columns from v0; `first`: grad_h_s's parts are written, not added to
 hipError_t launch_grad_W(const Problem& p, int v0, int width, hipStream_t st);
-// (set, W_offset: which copy of dz, and elements in front of the part of the head's rows that it is multiplied by)
-hipError_t launch_grad_h(const Problem& p, int v0, int width, bool first, hipStream_t st, int set = 0, int64_t W_offset = 0);
-// ... with the product times *p.out_scale, in front of the only rounding (kd_head_products.hip)
+// (pairs: products of copies of dz with parts of the head's rows, `at` elements into them; null: dz by the head)
+struct GradHPairs { int n; int set[6], at[6]; };
+hipError_t launch_grad_h(const Problem& p, int v0, int width, bool first, hipStream_t st, const GradHPairs* pairs = nullptr);
+// ... of the one-head losses (kd_head_products.hip): grad_h_s with few tokens by tiles of its own; grad_W_s times *p.out_scale, in front of the
+// only rounding
+hipError_t launch_head_grad_h(const Problem& p, int v0, int width, bool first, hipStream_t st, const GradHPairs* pairs);
 hipError_t launch_grad_W_scaled(const Problem& p, int v0, int width, hipStream_t st);
 hipError_t launch_gradh_finish(const Problem& p, hipStream_t st);
 const char* build_info();     // compile-time configuration of the kernels (tile shapes)

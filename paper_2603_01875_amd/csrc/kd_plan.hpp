@@ -70,7 +70,8 @@ inline int64_t choose_chunk(const Problem& q, int64_t v_all, int64_t logit_k) {
 // with up to 18 tiles and splits (product and gradh_finish), and 180 more: 0.6 % behind the best one of each on average (2.5 % and more
 // with the last chunk and the cache left out).  T = 4096, H_s = 1024, V = 151936 128 rows x 2 parts 1123 us a call, 256 x 4 1213; T = 1024 256 x 16 353 us,
 // 128 x 8 372, 128 x 16 312; T = 512 256 x 32 142 us, 128 x 16 159.
-inline void plan_grad_h(Problem& q, bool lean) {
+// `products`: so many that are summed, each with parts of its own (GradHPairs).
+inline void plan_grad_h(Problem& q, bool lean, int products = 1) {
   const int first_width = (int)(q.V < q.V_c ? q.V : q.V_c), steps_first = (first_width + 63) / 64;
   const int full_chunks = q.V / first_width, last_width = q.V - full_chunks * first_width;
   double least = 1e300;
@@ -80,7 +81,7 @@ inline void plan_grad_h(Problem& q, bool lean) {
     const int i = rows / 64 - 1;
     const double in_cache[] = {0.62, 0.85, 1.19, 1.47}, from_memory[] = {0.82, 0.98, 1.26, 1.47};
     const double ends = 1.7 + rows / 256. * (q.V > q.V_c ? 24. : 8.5);
-    const int64_t h_tiles = (q.H_s + rows - 1) / rows, tiles = h_tiles * q.n_tt, masked_tiles = h_tiles * ((q.n_tt * 7 + 7) / 8);
+    const int64_t h_tiles = (q.H_s + rows - 1) / rows * products, tiles = h_tiles * q.n_tt, masked_tiles = h_tiles * ((q.n_tt * 7 + 7) / 8);
     auto rounds = [&](int64_t n) { return (double)((n + q.n_cu - 1) / q.n_cu); };
     for (int s = 1; s <= 32 && (s == 1 || q.V_c / s >= 512) && s <= steps_first; ++s) {
       if (lean && s > 1 && s * tiles > q.n_cu) break;
@@ -91,7 +92,7 @@ inline void plan_grad_h(Problem& q, bool lean) {
         return 0.5 * (rounds(tiles * parts) + rounds(masked_tiles * parts)) * ((steps < n ? steps : n) * step + ends);
       };
       const double t = full_chunks * chunk(first_width) + (last_width > 0 ? chunk(last_width) : 0.) +
-                       (double)((steps_first + steps - 1) / steps) * q.T * q.H_s * 1.17e-6;
+                       (double)((steps_first + steps - 1) / steps) * q.T * q.H_s * products * 1.17e-6;
       if (t < least) { least = t; q.gh_rows = rows; sk = s; }
     }
   }

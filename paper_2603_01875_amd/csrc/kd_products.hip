@@ -61,23 +61,10 @@ hipError_t launch_grad_W(const Problem& p, int v0, int width, hipStream_t st) {
 #undef KD_GW
 }
 
-hipError_t launch_grad_h(const Problem& p, int v0, int width, bool first, hipStream_t st, int set, int64_t W_offset) {
+hipError_t launch_grad_h(const Problem& p, int v0, int width, bool first, hipStream_t st, const GradHPairs* pairs) {
   const int mb = p.gh_rows / 16;
-  GradHArgs a{};
-  a.dz = (const char*)p.dz;
-  const int64_t ld = p.w_hv_inplace ? p.V : p.prep_Ws ? p.K_s : p.H_s;
-  a.W = (const char*)p.W_s + ((size_t)v0 * (p.w_hv_inplace ? 1 : ld) + W_offset) * 2;
-  a.out = p.gh32; a.part_stride = (int64_t)p.T * p.H_s;
-  a.width = width; a.H_s = p.H_s;
-  a.n_ht = (p.H_s + 16 * mb - 1) / (16 * mb);
-  a.ksteps = p.ksteps_h;
-  a.n_split = ((width + 63) / 64 + a.ksteps - 1) / a.ksteps;       // every part has at least one k-step
-  a.accumulate = first ? 0 : 1;
-  a.set = set;
-  a.lda = 2u * (uint32_t)ld;
-  a.ldb = (uint32_t)p.V_c * 128;
-  a.meta = p.meta;
-  const int tiles = a.n_ht * p.n_tt * a.n_split, grid = tiles < p.n_cu ? tiles : p.n_cu;   // worst case: no token masked
+  const GradHArgs a = grad_h_args(p, v0, width, first, pairs);
+  const int tiles = a.n_ht * p.n_tt * a.n_split * a.n_pairs, grid = tiles < p.n_cu ? tiles : p.n_cu;   // worst case: no token masked
 #define KD_GH(N) (p.w_hv_inplace ? launch_big<grad_h_kernel<N, true>>(grid, 256, StripShape<N, 4>::SMEM_BYTES, st, &a) \
                                  : launch_big<grad_h_kernel<N, false>>(grid, 256, StripShape<N, 4>::SMEM_BYTES, st, &a))
   switch (mb) {
@@ -93,7 +80,7 @@ hipError_t launch_gradh_finish(const Problem& p, hipStream_t st) {
   const int64_t n = (int64_t)p.T * p.H_s;
   const FlatGrid g = flat_grid(((n + 3) / 4 + 255) / 256);
   hipLaunchKernelGGL(gradh_finish_kernel, dim3(g.x, g.y), dim3(256), 0, st, p.gh32,
-                     p.n_ksplit_h, p.T, p.H_s, p.inv, p.out_scale, p.grad_f32, p.grad_h_s);
+                     p.n_ksplit_h * (p.gh_pairs ? p.gh_pairs : 1), p.T, p.H_s, p.inv, p.out_scale, p.grad_f32, p.grad_h_s);
   return hipGetLastError();
 }
 

@@ -394,15 +394,18 @@ struct GradHArgs {
   int width, H_s;
   int n_ht, n_split, ksteps;   // hidden tiles; parts of ksteps k-steps of 64 columns
   int accumulate;
-  int set;                 // which of the copies of the token axis (GradWArgs::sets) is multiplied
+  // Products that are summed, each with parts of its own (n_ksplit behind one another): which copy of the token axis (GradWArgs::sets)
+  // by which part of the head's rows, in elements from W.  One product: copy 0 by the rows themselves.
+  int n_pairs, n_ksplit;
+  int pair_set[6], pair_at[6];
   uint32_t lda, ldb;
   const int* meta;
 };
 
-// 16 MB hidden rows (LDS) x 256 tokens; HV: the head is [H][V]
-template <int MB, bool HV>
+// 16 MB hidden rows (LDS) x 64 NB tokens; HV: the head is [H][V]
+template <int MB, bool HV, int NB = 4>
 struct GradHWork {
-  typedef StripShape<MB, 4> C;
+  typedef StripShape<MB, NB> C;
   const GradHArgs& a;
   int L, G, n_tt;
   __device__ GradHWork(const GradHArgs& a_) : a(a_) {
@@ -410,59 +413,66 @@ struct GradHWork {
     L = xcd_logical_id(blockIdx.x, G);
     n_tt = meta_get(a.meta, META_N_TT);
   }
-  __device__ int n_items() const { const int n = a.n_ht * n_tt * a.n_split; return L < n ? (n - L + G - 1) / G : 0; }
+  __device__ int n_items() const { const int n = a.n_ht * n_tt * a.n_split * a.n_pairs; return L < n ? (n - L + G - 1) / G : 0; }
   __device__ StripItem item(int i) const {
     const auto p = kernel_args<GradHArgs>();
-    const int q = i * G + L, per = p->n_ht * n_tt, part = q / per;
+    const int q = i * G + L, per = p->n_ht * n_tt;
+    int part = q / per, pair = 0, set;
     int ht, tt;
     group_decode(q - part * per, p->n_ht, n_tt, ht, tt);
+    if (p->n_pairs > 1) {
+      pair = part / p->n_split;
+      part -= pair * p->n_split;
+    }
+    set = p->pair_set[pair];
+    const char* const W = p->W + (int64_t)p->pair_at[pair] * 2;
     const int k0 = part * p->ksteps * 64;
     StripItem it;
     it.m0 = ht * C::BM;
     it.n0 = tt * 256;
     it.lda0 = it.lda1 = p->lda;
     it.ldb0 = it.ldb1 = p->ldb;
-    it.A0 = it.A1 = HV ? p->W + (int64_t)it.m0 * it.lda1 + k0 * 2 : p->W + (int64_t)k0 * it.lda1 + it.m0 * 2;
-    const int panel = (it.n0 >> 6) + (p->set ? p->set * (meta_get(p->meta, META_T_EFF) >> 6) : 0);
+    it.A0 = it.A1 = HV ? W + (int64_t)it.m0 * it.lda1 + k0 * 2 : W + (int64_t)k0 * it.lda1 + it.m0 * 2;
+    const int panel = (it.n0 >> 6) + (set ? set * (meta_get(p->meta, META_T_EFF) >> 6) : 0);
     it.B0 = it.B1 = p->dz + (int64_t)panel * it.ldb1 + (int64_t)k0 * 128;
     it.k0 = it.k1 = min(p->ksteps * 64, p->width - k0);
     it.a_rows = it.out_rows = min(C::BM, p->H_s - it.m0);
     it.b_blocks = 0;
-    it.aux = part;
+    it.aux = part + pair * p->n_ksplit;
     return it;
   }
 };
 
-template <int MB>
+template <int MB, int NB = 4>
 struct GradHEpi {
   static constexpr bool WHOLE = true;
-  static constexpr int STORES = 4 * MB;
+  static constexpr int STORES = NB * MB;
   const GradHArgs& a;
   int lane, wave, n_valid;
   __device__ GradHEpi(const GradHArgs& a_) : a(a_), lane(threadIdx.x & 63), wave(threadIdx.x >> 6), n_valid(meta_get(a_.meta, META_N_VALID)) {}
   __device__ void begin_item(const StripItem&) {}
   // the tile's valid tokens of its part
   __device__ __forceinline__ rsrc_t buffer(const StripItem& it, bool exists) const {
-    const int rows = exists ? max(min(n_valid - it.n0, 256), 0) : 0;
+    const int rows = exists ? max(min(n_valid - it.n0, 64 * NB), 0) : 0;
     return make_rsrc(a.out + (int64_t)it.aux * a.part_stride + (int64_t)it.n0 * a.H_s, (uint32_t)rows * (uint32_t)a.H_s * 4u);
   }
   __device__ __forceinline__ uint32_t place(const StripItem& it, int ln, int i, int j) const {
     const int h = 16 * i + 4 * (ln >> 4);
-    return h < it.a_rows ? ((uint32_t)(64 * wave + 16 * j + (ln & 15)) * (uint32_t)a.H_s + it.m0 + h) * 4u : NOWHERE;
+    return h < it.a_rows ? ((uint32_t)(16 * NB * wave + 16 * j + (ln & 15)) * (uint32_t)a.H_s + it.m0 + h) * 4u : NOWHERE;
   }
-  __device__ __forceinline__ void start(const StripItem& it, f32x4 (&T)[MB * 4]) const {
+  __device__ __forceinline__ void start(const StripItem& it, f32x4 (&T)[MB * NB]) const {
     const rsrc_t r = buffer(it, a.accumulate);
     const int ln = fresh(lane);
-    static_for<0, 4 * MB>([&](auto nc) {
+    static_for<0, NB * MB>([&](auto nc) {
       constexpr int n = decltype(nc)::value;
       T[n] = load4<true>(r, place(it, ln, n % MB, n / MB));
       if constexpr (n % 16 == 15) __builtin_amdgcn_sched_barrier(0);
     });
   }
-  __device__ __forceinline__ void tile(const StripItem& it, f32x4 (&T)[MB * 4]) const {
+  __device__ __forceinline__ void tile(const StripItem& it, f32x4 (&T)[MB * NB]) const {
     const rsrc_t r = buffer(it, true);
     const int ln = fresh(lane);
-    static_for<0, 4 * MB>([&](auto nc) {
+    static_for<0, NB * MB>([&](auto nc) {
       constexpr int n = decltype(nc)::value;
       store4<true>(r, place(it, ln, n % MB, n / MB), T[n]);
       if constexpr (n % 16 == 15) __builtin_amdgcn_sched_barrier(0);
@@ -478,7 +488,7 @@ KD_STRIP_KERNEL void grad_h_kernel(const GradHArgs a) {
   strip_loop<1, false, StripShape<MB, 4>, HV ? A_ROWS_DZ : A_KMAJOR_DZ>(work, epi, smem);
 }
 
-// What launch_grad_W (kd_products.hip) and launch_grad_W_scaled (kd_head_products.hip) have in common.
+// What the launchers of kd_products.hip and kd_head_products.hip have in common.
 inline GradWArgs grad_w_args(const Problem& p, int v0, int width, int nb) {
   GradWArgs a{};
   a.dz = (const char*)p.dz; a.hT = (const char*)p.h_sT;
@@ -490,6 +500,29 @@ inline GradWArgs grad_w_args(const Problem& p, int v0, int width, int nb) {
   a.scale = p.out_scale;
   a.lda = (uint32_t)p.V_c * 128; a.ldb = (uint32_t)(p.T_pad * a.sets) * 32;
   a.b_blocks = (p.H_s + 15) / 16;
+  a.meta = p.meta;
+  return a;
+}
+inline GradHArgs grad_h_args(const Problem& p, int v0, int width, bool first, const GradHPairs* pairs) {
+  const int mb = p.gh_rows / 16;
+  GradHArgs a{};
+  a.dz = (const char*)p.dz;
+  const int64_t ld = p.w_hv_inplace ? p.V : p.prep_Ws ? p.K_s : p.H_s;
+  a.W = (const char*)p.W_s + (size_t)v0 * 2 * (p.w_hv_inplace ? 1 : ld);
+  a.out = p.gh32; a.part_stride = (int64_t)p.T * p.H_s;
+  a.width = width; a.H_s = p.H_s;
+  a.n_ht = (p.H_s + 16 * mb - 1) / (16 * mb);
+  a.ksteps = p.ksteps_h;
+  a.n_split = ((width + 63) / 64 + a.ksteps - 1) / a.ksteps;       // every part has at least one k-step
+  a.accumulate = first ? 0 : 1;
+  a.n_ksplit = p.n_ksplit_h;
+  a.n_pairs = 1;
+  if (pairs) {
+    a.n_pairs = pairs->n;
+    for (int i = 0; i < pairs->n; ++i) { a.pair_set[i] = pairs->set[i]; a.pair_at[i] = pairs->at[i]; }
+  }
+  a.lda = 2u * (uint32_t)ld;
+  a.ldb = (uint32_t)p.V_c * 128;
   a.meta = p.meta;
   return a;
 }

@@ -259,7 +259,7 @@ __device__ __forceinline__ void strip_loop(const Work& work, Epi& epi, char* sme
 #pragma unroll
       for (int j = 0; j < NB; ++j) bj[j] = (uint32_t)min(j, it.b_blocks - 1 - b0) * bstride;
     } else {
-      rb = make_rsrc((l_ph ? it.B1 : it.B0) + (int64_t)wave * bstride, bstride);
+      rb = make_rsrc((l_ph ? it.B1 : it.B0) + (int64_t)(wave * NB / 4) * bstride, bstride);
     }
     set_voff(AM == A_KMAJOR_DZ && l_nk == 1 ? l_tail : 64);
   };
@@ -298,7 +298,7 @@ __device__ __forceinline__ void strip_loop(const Work& work, Epi& epi, char* sme
     __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_t*)(smem + st + wave * 1024 + j * 4096), 16,
                                              voff[j], l_a, 0, 0);
   };
-  const uint32_t boff = lane * 16;
+  const uint32_t boff = lane * 16 + (B_BLOCKS ? 0 : wave * NB % 4 * 1024);      // (fewer than four blocks: waves share a panel)
   auto load_b = [&](const rsrc_t& r, const uint32_t (&blk)[NB], int kb, int s, int j) -> u32x4 {
     if constexpr (B_BLOCKS) return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, boff, kb + s * B_SUB + blk[j], 0));
     else return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, boff + j * 1024, kb + s * B_SUB, 0));

@@ -49,6 +49,10 @@ def test_products(kernels):
     assert len(products) == 24                # tiles x order x type x add
     for name, code in products.items():
         assert hazards(code) == [] and early_uses(code) == [], name
+    grad_h = _of(kernels, "head_gh_few_kernel")
+    assert len(grad_h) == 4                   # 64, 128 tokens x order
+    for name, code in grad_h.items():
+        assert hazards(code) == [] and early_uses(code) == [], name
     few = _of(kernels, "head_gw_few_kernel")
     assert len(few) == 4                      # order x add
     for name, code in few.items():
