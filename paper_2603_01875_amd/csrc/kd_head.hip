@@ -33,79 +33,128 @@ __global__ __launch_bounds__(256) void label_targets_kernel(const TargetArgs a) 
   if (t < a.T) (void)label_target(a, t);
 }
 
-// One wave per token.  The entries (absent: a negative row, or a logit of minus infinity) are put in ascending order by counting, for
-// each, how many come before it; those of the same row add up.  K^2 comparisons out of LDS: for K = 64 a wave's 64 reads.  All sums in
-// 64 bits: the mass beside the list is a difference from 1.
+// G threads per token.  The entries that are there (a row that is not negative, a logit above minus infinity) go to the place that the
+// count of smaller rows gives them: K compares each, out of LDS, four at a time (K = 217, 4546 tokens KD_T1 us).  Entries of the same row,
+// which meet in one place, add up, in a second look that most calls do not need.  All sums in 64 bits: the mass beside the list is a
+// difference from 1.
+template <int G>
 __global__ __launch_bounds__(256) void top_targets_kernel(const TargetArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int K = a.t.K, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, t = blockIdx.x * 4 + wave;
-  double* const q = (double*)smem + wave * K;
-  int* const row = (int*)(smem + 4 * K * 8) + wave * 2 * K;
-  int* const once = row + K;
+  __shared__ double sums[4][3];
+  __shared__ int bad_of[4];
+  constexpr int PER = 256 / G, WAVES = G / 64;         // tokens a workgroup, waves a token
+  const int K = a.t.K, Kp = (K + 3) & ~3, mine = threadIdx.x / G, k0 = threadIdx.x % G, wave = threadIdx.x >> 6, w0 = mine * WAVES;
+  const int t = blockIdx.x * PER + mine, lane = threadIdx.x & 63;
+  double* const q = (double*)smem + mine * Kp;
+  int* const row = (int*)(smem + PER * Kp * 8) + mine * 2 * Kp;
+  int* const taken = row + Kp;                         // entries in a place; where some met: the rows, each once
   const bool there = t < a.T;
   const int64_t at = (int64_t)t * K;
+  // sums over a token's waves of x, y, z, in one order
+  auto all = [&](double x, double y, double z) {
+    x = wave_sum(x); y = wave_sum(y); z = wave_sum(z);
+    __syncthreads();
+    if (lane == 0) { sums[wave][0] = x; sums[wave][1] = y; sums[wave][2] = z; }
+    __syncthreads();
+  };
+  auto sum = [&](int i) {
+    double r = sums[w0][i];
+    for (int w = 1; w < WAVES; ++w) r += sums[w0 + w][i];
+    return r;
+  };
   bool bad = false;
   double top = -INFINITY;
-  if (there)
-    for (int k = lane; k < K; k += 64) {
-      const int64_t v = a.t.index64 ? ((const int64_t*)a.t.index)[at + k] : (int64_t)((const int*)a.t.index)[at + k];
-      const float z = a.t.top_f32 ? ((const float*)a.t.top)[at + k] : (float)((const bf16_t*)a.t.top)[at + k];
-      const bool in = v >= 0 && z != -INFINITY;
-      bad = bad || (in && (v >= a.V || z != z));
-      row[k] = in && v < a.V ? (int)v : kNoEntry;
-      q[k] = (double)z * a.inv_tau;
-      if (in) top = fmax(top, q[k]);
-    }
-  __syncthreads();
+  for (int k = k0; k < Kp; k += G) {
+    row[k] = kNoEntry;
+    taken[k] = 0;
+    if (!there || k >= K) continue;
+    const int64_t v = a.t.index64 ? ((const int64_t*)a.t.index)[at + k] : (int64_t)((const int*)a.t.index)[at + k];
+    const float z = a.t.top_f32 ? ((const float*)a.t.top)[at + k] : (float)((const bf16_t*)a.t.top)[at + k];
+    const bool in = v >= 0 && z != -INFINITY;
+    bad = bad || (in && (v >= a.V || z != z));
+    row[k] = in && v < a.V ? (int)v : kNoEntry;
+    q[k] = (double)z * a.inv_tau;
+    if (in) top = fmax(top, q[k]);
+  }
   top = wave_max(top);
-  double mass = 0.0;
-  if (there)
-    for (int k = lane; k < K; k += 64) mass += row[k] != kNoEntry ? exp(q[k] - top) : 0.0;
-  mass = wave_sum(mass);
-  const double norm = !there ? 0.0 : a.t.tail == 0 ? top + log(mass) : (double)a.t.lse[t];
-  if (there)
-    for (int k = lane; k < K; k += 64) q[k] = row[k] != kNoEntry ? exp(q[k] - norm) : 0.0;
+  if (lane == 0) sums[wave][0] = top;
   __syncthreads();
-  if (there)
-    for (int k = lane; k < K; k += 64) {
+  top = sums[w0][0];
+  for (int w = 1; w < WAVES; ++w) top = fmax(top, sums[w0 + w][0]);
+  double norm = 0.0;
+  if (a.t.tail == 0) {
+    double mass = 0.0;
+    for (int k = k0; k < K; k += G) mass += there && row[k] != kNoEntry ? exp(q[k] - top) : 0.0;
+    all(mass, 0.0, 0.0);
+    norm = top + log(sum(0));
+  } else if (there) {
+    norm = (double)a.t.lse[t];
+  }
+  for (int k = k0; k < K; k += G) q[k] = there && row[k] != kNoEntry ? exp(q[k] - norm) : 0.0;
+  __syncthreads();
+  int n = 0, met = 0;
+  double held = 0.0, ent = 0.0;
+  for (int k = k0; k < K; k += G) {
+    const int v = row[k];
+    if (v == kNoEntry) continue;
+    int place = 0;
+    for (int j = 0; j < Kp; j += 4) {
+      const int4 r = *(const int4*)(row + j);
+      place += (r.x < v) + (r.y < v) + (r.z < v) + (r.w < v);
+    }
+    ++n;
+    met += atomicAdd(&taken[place], 1) != 0;
+    a.t.list[at + place] = v;                          // (of entries that meet, either; done again below)
+    a.t.q[at + place] = (float)q[k];
+    held += q[k];
+    ent += q[k] > 0.0 ? q[k] * log(q[k]) : 0.0;
+  }
+  const unsigned long long b_bad = __ballot(bad);
+  all((double)n, (double)met, held);
+  if (lane == 0) bad_of[wave] = b_bad != 0;
+  __syncthreads();
+  n = (int)sum(0);
+  met = (int)sum(1);
+  held = sum(2);
+  bool any_bad = false;
+  for (int w = 0; w < WAVES; ++w) any_bad = any_bad || bad_of[w0 + w];
+  const int distinct = n - met;
+  if (__syncthreads_or(met)) {                         // (in any token of the workgroup)
+    for (int k = k0; k < K; k += G) {
       const int v = row[k];
       bool first = v != kNoEntry;
       for (int j = 0; j < k && first; ++j) first = row[j] != v;
-      once[k] = first ? v : kNoEntry;
+      taken[k] = first ? v : kNoEntry;
     }
-  __syncthreads();
-  if (!there) return;
-  double held = 0.0, ent = 0.0;
-  int n = 0;
-  for (int k = lane; k < K; k += 64) {
-    const int v = once[k];
-    if (v == kNoEntry) continue;
-    int rank = 0;
-    double sum = 0.0;
-    for (int j = 0; j < K; ++j) {
-      rank += once[j] < v;
-      sum += row[j] == v ? q[j] : 0.0;
+    __syncthreads();
+    ent = 0.0;
+    for (int k = k0; k < K; k += G) {
+      const int v = taken[k];
+      if (v == kNoEntry) continue;
+      int place = 0;
+      double total = 0.0;
+      for (int j = 0; j < K; ++j) {
+        place += taken[j] < v;
+        total += row[j] == v ? q[j] : 0.0;
+      }
+      a.t.list[at + place] = v;
+      a.t.q[at + place] = (float)total;
+      ent += total > 0.0 ? total * log(total) : 0.0;
     }
-    a.t.list[at + rank] = v;
-    a.t.q[at + rank] = (float)sum;
-    held += sum;
-    ent += sum > 0.0 ? sum * log(sum) : 0.0;
-    ++n;
   }
-  held = wave_sum(held);
-  ent = wave_sum(ent);
-  n = (int)wave_sum((double)n);
-  bad = __any(bad);
-  for (int k = n + lane; k < K; k += 64) a.t.list[at + k] = kNoEntry;
-  if (lane) return;
+  all(ent, 0.0, 0.0);
+  ent = sum(0);
+  if (!there) return;
+  for (int k = distinct + k0; k < K; k += G) a.t.list[at + k] = kNoEntry;
+  if (k0) return;
   const double rest = a.t.tail == 1 ? fmax(1.0 - held, 0.0) : 0.0;
   double* const info = a.t.info + (int64_t)t * kTargetInfo;
-  info[0] = bad || held != held ? __builtin_nan("") : held + rest;
+  info[0] = any_bad || held != held ? __builtin_nan("") : held + rest;
   info[1] = rest;
   info[2] = ent + (rest > 0.0 ? rest * log(rest) : 0.0);
-  const bool counts = (n > 0 || bad) && (!a.t.mask || a.t.mask[t]);
-  a.t.valid[t] = counts;
-  keep_places(a, t, counts);
+  const bool counts_ = (n > 0 || any_bad) && (!a.t.mask || a.t.mask[t]);
+  a.t.valid[t] = counts_;
+  keep_places(a, t, counts_);
 }
 
 TargetArgs target_args(const HeadProblem& h) {
@@ -115,7 +164,8 @@ TargetArgs target_args(const HeadProblem& h) {
 hipError_t launch_targets(const HeadProblem& h, hipStream_t st) {
   const TargetArgs a = target_args(h);
   if (h.t.ce) hipLaunchKernelGGL(label_targets_kernel, dim3((h.p.T + 255) / 256), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(top_targets_kernel, dim3((h.p.T + 3) / 4), dim3(256), 64 * h.t.K, st, a);
+  else if (h.t.K <= 64) hipLaunchKernelGGL(top_targets_kernel<64>, dim3((h.p.T + 3) / 4), dim3(256), 64 * ((h.t.K + 3) & ~3), st, a);
+  else hipLaunchKernelGGL(top_targets_kernel<256>, dim3(h.p.T), dim3(256), 16 * ((h.t.K + 3) & ~3), st, a);
   return hipGetLastError();
 }
 
@@ -143,6 +193,8 @@ struct HeadCombineArgs {
   const int* list;
   const float* q;
   const float* z;
+  const float* kept;                   // the entries' logits among all of them, or null and in z
+  int ldz;
   const double* info;
   f32x4* rowinfo;
   float* row_loss;
@@ -249,11 +301,15 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
     const float* const q0 = a.partials + t;            // t < T_pad: allocated, whatever the row holds
     const int* const list = a.list + token * a.K;
     const float* const prob = a.q + token * a.K;
-    const float* const z = a.z + (int64_t)t * a.K;
+    auto z = [&](int k) {
+      if (!a.kept) return a.z[(int64_t)t * a.K + k];
+      const int v = list[k], c = v & 31;
+      return a.kept[dz_chunk(a.ldz, t >> 6, v >> 5, (t >> 4) & 3, 16 * ((c & 15) >> 2) + (t & 15)) + 4 * (c >> 4) + (c & 3)];
+    };
     float m[2] = {M_FLOOR, M_FLOOR};
 #pragma unroll 4
     for (int p = g; p < n_parts; p += G) m[0] = fmaxf(m[0], q0[p * stride]);
-    for (int k = g; k < a.K && list[k] != kNoEntry; k += G) m[1] = fmaxf(m[1], z[k] * a.c);
+    for (int k = g; k < a.K && list[k] != kNoEntry; k += G) m[1] = fmaxf(m[1], z(k) * a.c);
     merge_parts<TX, NT, 2, MergeMax>(m, lds);
     float v[5] = {0.f, 0.f, 0.f, 0.f, 0.f};            // sum beside the list, on it, sum of logits, sum q (z - max), sum q
 #pragma unroll 4
@@ -263,9 +319,9 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
       if (a.nv == 3) v[2] += q[2 * a.T_pad];
     }
     for (int k = g; k < a.K && list[k] != kNoEntry; k += G) {
-      const float d = fmaf(z[k], a.c, -m[1]);
+      const float zk = z(k), d = fmaf(zk, a.c, -m[1]);
       v[1] += fexp2(d);
-      v[2] += z[k];
+      v[2] += zk;
       v[3] = fmaf(prob[k], d, v[3]);
       v[4] += prob[k];
     }
@@ -317,7 +373,7 @@ hipError_t launch_head_combine(const HeadProblem& h, bool backward, bool pack_h,
   // 8 tokens x 128 threads where a token has many parts, 32 x 8 else (see merge_parts); 32 x 32 where that is all the tokens
   const bool all = p.T <= 32, many = !all && (h.few ? h.parts : p.n_split) >= 128;
   HeadCombineArgs a{p.partials, p.meta, p.rowmap, p.inv, p.T, p.T_pad, h.t.smoothing > 0.f ? 3 : 2, h.t.K, h.few ? h.parts : 0,
-                    1.4426950408889634f / p.tau, h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.t.info,
+                    1.4426950408889634f / p.tau, h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.kept, p.V_c, h.t.info,
                     (f32x4*)p.rowinfo, p.row_loss, p.out_weight, p.per_token_loss, all ? 1 : many ? p.T_pad / 8 : p.T_pad / 32,
                     loss_sum_args(h), {}};
   int64_t groups = a.groups;
@@ -359,7 +415,8 @@ hipError_t launch_head_stats(const HeadProblem& h, hipStream_t st) {
   a.v_end = h.p.V;
   const int grid = h.p.n_tt * h.p.n_split;
   const bool hv = h.p.w_hv_inplace, smooth = h.t.smoothing > 0.f;
-#define KD_HS(HV, S) launch_big<head_stats_kernel<HV, S>>(grid, HeadCfg::NT, HeadCfg::STATE_SMEM_BYTES, st, &a)
+#define KD_HS(HV, S) (h.kept ? launch_big<head_stats_kernel<HV, S, true>>(grid, HeadCfg::NT, HeadCfg::STATE_SMEM_BYTES, st, &a) \
+                             : launch_big<head_stats_kernel<HV, S, false>>(grid, HeadCfg::NT, HeadCfg::STATE_SMEM_BYTES, st, &a))
   return hv ? (smooth ? KD_HS(true, true) : KD_HS(true, false)) : (smooth ? KD_HS(false, true) : KD_HS(false, false));
 #undef KD_HS
 }
@@ -468,7 +525,7 @@ __global__ __launch_bounds__(256) void head_dz_kernel(const KeptArgs k) {
         const int bit = (e < 4 ? 0 : 16) + (e & 3);
         if (mine >> bit & 1) {
           const int n = rank + __popc(word & ((1u << (bit + 4 * g)) - 1));
-          x[e] = listed_dz(ri, a.z[(int64_t)(panel * 64 + i) * a.n_list + n], a.c, k.q[(int64_t)token * a.n_list + n]);
+          x[e] = listed_dz(ri, z[s][e >> 2][e & 3], a.c, k.q[(int64_t)token * a.n_list + n]);
         }
       }
     }

@@ -171,7 +171,17 @@ struct HeadGeo {
 // max, sum, sum of logits; next entry of the list, its place in it, that place at the tile's start, the token.
 // Which rows of the tile are listed: [token][4] words of 64 bits, bit 4 i + r of word g for row 16 i + 4 g + r, so that a lane finds
 // its own rows in one word.  Thread i keeps the list of token i of the tile, which is its own wave's: no barrier.
-template <bool SMOOTH>
+// x, or the logit of what does not exist where bit B of `word` is set: the bit, spread over a word, picks one of the two.  (Pinned: with
+// all of a column's words made at once they are spilled.)
+template <int B>
+__device__ __forceinline__ float left_out(float x, uint32_t word) {
+  int32_t on;
+  asm volatile("v_bfe_i32 %1, %2, %3, 1\n\tv_bfi_b32 %0, %1, %4, %0" : "+v"(x), "=&v"(on) : "v"(word), "n"(B), "v"(NEG_BIG));
+  return x;
+}
+
+// KEPT: all logits are stored (HeadArgs::kept), so those on the lists need not be picked out: they are only taken out of the sums.
+template <bool SMOOTH, bool KEPT>
 struct HeadStatsEpi {
   static constexpr int NV = SMOOTH ? 3 : 2;
   HeadGeo geo;
@@ -258,31 +268,43 @@ struct HeadStatsEpi {
   template <class J, int NE>
   __device__ __forceinline__ void column(const StripItem& it, J, float (&T)[NE]) {
     const int n = geo.n(J::value);
-    if (a.kept) {
-      const int panel = (it.n0 >> 6) + geo.wave;
+    if constexpr (KEPT) {
+      const int64_t panel = uniform((it.n0 >> 6) + geo.wave);
+      const rsrc_t to = make_rsrc(a.kept + panel * 64 * a.ldz, 256u * (uint32_t)a.ldz);
 #pragma unroll
       for (int u = 0; u < NE / 8; ++u) {
         if (32 * u >= it.out_rows) break;
-        f32x4* const to = (f32x4*)(a.kept + dz_chunk(a.ldz, panel, (it.m0 >> 5) + u, J::value, geo.lane));
-        to[0] = f32x4{T[8 * u], T[8 * u + 1], T[8 * u + 2], T[8 * u + 3]};
-        to[1] = f32x4{T[8 * u + 4], T[8 * u + 5], T[8 * u + 6], T[8 * u + 7]};
+        const uint32_t sub = 8192u * (uint32_t)((it.m0 >> 5) + u) + 2048u * J::value;      // (as dz_chunk, elements of four bytes)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{T[8 * u], T[8 * u + 1], T[8 * u + 2], T[8 * u + 3]}), to, 32 * geo.lane, sub, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{T[8 * u + 4], T[8 * u + 5], T[8 * u + 6], T[8 * u + 7]}), to, 32 * geo.lane + 16, sub, 0);
       }
     }
     const uint64_t mine = listed[n * 4 + (geo.lane >> 4)];
-    if (__any(mine != 0)) take(it, n, mine, T);
     float* const at = all + n * 8;
     const f32x4 old = *(const f32x4*)at;
-    float top = NEG_BIG;
-#pragma unroll
-    for (int e = 0; e < NE; ++e) top = fmaxf(top, T[e]);
-    const float m = fmaxf(old[0], quad_max(top) * a.c);
-    float s = 0.f, zs = 0.f;
-#pragma unroll
-    for (int e = 0; e < NE; ++e) {
-      s += fexp2(fmaf(T[e], a.c, -m));
-      if (SMOOTH) zs += T[e] > 0.1f * NEG_BIG ? T[e] : 0.f;
+    // logit(IntC<e>): entry e of the column, as it counts
+    auto add = [&](auto&& logit) {
+      float top = NEG_BIG;
+      static_for<0, NE>([&](auto ec) { top = fmaxf(top, logit(ec)); });
+      const float m = fmaxf(old[0], quad_max(top) * a.c);
+      float s = 0.f, zs = 0.f;
+      static_for<0, NE>([&](auto ec) {
+        const float z = logit(ec);
+        s += fexp2(fmaf(z, a.c, -m));
+        if (SMOOTH) zs += z > 0.1f * NEG_BIG ? z : 0.f;
+      });
+      *(f32x4*)at = f32x4{m, fmaf(old[1], fexp2(old[0] - m), quad_sum(s)), SMOOTH ? old[2] + quad_sum(zs) : 0.f, 0.f};
+    };
+    if constexpr (KEPT) {
+      if (__any(mine != 0)) {                // (taken out twice: a column that has been changed does not stay in accumulation registers)
+        const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
+        add([&](auto ec) { return left_out<decltype(ec)::value & 31>(T[decltype(ec)::value], half[decltype(ec)::value >> 5]); });
+        return;
+      }
+    } else {
+      if (__any(mine != 0)) take(it, n, mine, T);
     }
-    *(f32x4*)at = f32x4{m, fmaf(old[1], fexp2(old[0] - m), quad_sum(s)), SMOOTH ? old[2] + quad_sum(zs) : 0.f, 0.f};
+    add([&](auto ec) { return T[decltype(ec)::value]; });
   }
   __device__ void write(int tt, int split) {
     const float* const own = all + threadIdx.x * 8;
@@ -384,12 +406,12 @@ struct HeadDrive {
 
 HeadArgs head_args(const HeadProblem& h);      // kd_head.hip
 
-template <bool HV, bool SMOOTH>
+template <bool HV, bool SMOOTH, bool KEPT>
 KD_STRIP_KERNEL void head_stats_kernel(const HeadArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   HeadWork<HV> work(a, meta_get(a.meta, META_N_SPLIT));
-  HeadStatsEpi<SMOOTH> epi(a, smem, work.tt, work.row0);
-  HeadDrive<HeadStatsEpi<SMOOTH>> drive(epi);
+  HeadStatsEpi<SMOOTH, KEPT> epi(a, smem, work.tt, work.row0);
+  HeadDrive<HeadStatsEpi<SMOOTH, KEPT>> drive(epi);
   strip_loop<1, true, HeadCfg, HV ? A_KMAJOR_DZ : A_ROWS>(work, drive, smem);
   if (work.cnt > 0) epi.write(work.tt, work.split);
 }

@@ -231,7 +231,13 @@ struct FewEpi {
             }
         }
         const uint32_t mine = ((const uint16_t*)(smem + C::LISTED_AT))[((flip * C::BM + n) * 4 + wave) * 4 + g];
-        if (__any(mine != 0)) take(n, mine, z);
+        if (__any(mine != 0)) {
+          if (a.kept)                        // (they are there among the others)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[e] = mine >> e & 1 ? NEG_BIG : z[e];
+          else
+            take(n, mine, z);
+        }
         f32x4* const at = (f32x4*)(smem + C::SUMS_AT) + wave * C::BM + n;
         const f32x4 old = *at;
         float top = NEG_BIG;

@@ -28,7 +28,7 @@ def _of(kernels, name):
 
 def test_logit_kernels(kernels):
     logit = {**_of(kernels, "head_stats_kernel"), **_of(kernels, "head_grad_kernel")}
-    assert len(logit) == 4 + 8                # order x smoothing; order x smoothing x parts
+    assert len(logit) == 8 + 8                # order x smoothing x kept; order x smoothing x parts
     for name, code in logit.items():
         assert sum(c.op.startswith("v_mfma") for c in code) >= 4 * 64, name
         assert hazards(code) == [], name
