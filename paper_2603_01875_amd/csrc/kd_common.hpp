@@ -90,6 +90,18 @@ __device__ __forceinline__ void merge_parts(float (&v)[NV], float* lds) {
   }
 }
 
+// fp32 operands as bf16 parts laid side by side along K.  src_f32 == 1, the two-model losses: two parts, three products (see prepare);
+// src_f32 == 2, the one-head losses: three parts, f = f0 + f1 + f2 to 24 bits, and the six products of them that are not below
+// those bits, the head as [0 0 0 1 1 2], the hidden states as [0 1 2 0 1 0].
+__device__ __forceinline__ int part_of_six(int place, bool head) { return (head ? 0x211000 : 0x010210) >> (4 * place) & 15; }
+__device__ __forceinline__ bf16_t part_of(float f, int part) {
+  const bf16_t hi = (bf16_t)f;
+  if (part == 0) return hi;
+  const float rest = f - (float)hi;
+  const bf16_t mid = (bf16_t)rest;
+  return part == 1 ? mid : (bf16_t)(rest - (float)mid);
+}
+
 #define KD_STRIP_KERNEL __global__ __launch_bounds__(StripCfg::NT, 1) __attribute__((amdgpu_waves_per_eu(1, 1)))
 
 // Launch of a kernel that needs more dynamic LDS than the default limit.  The limit is a property of

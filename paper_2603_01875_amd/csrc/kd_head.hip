@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256) void label_targets_kernel(const TargetArgs a) 
 }
 
 // G threads per token.  The entries that are there (a row that is not negative, a logit above minus infinity) go to the place that the
-// count of smaller rows gives them: K compares each, out of LDS, four at a time (K = 217, 4546 tokens KD_T1 us).  Entries of the same row,
+// count of smaller rows gives them: K compares each, out of LDS, four at a time (K = 217, 4546 tokens: 37.5 us).  Entries of the same row,
 // which meet in one place, add up, in a second look that most calls do not need.  All sums in 64 bits: the mass beside the list is a
 // difference from 1.
 template <int G>
@@ -170,6 +170,48 @@ hipError_t launch_targets(const HeadProblem& h, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------------------------------
+// fp32 heads
+// ------------------------------------------------------------------------------------------
+// The rows' bf16 parts side by side (part_of_six), zero from 6 H to K.  A thread reads eight values once and writes them to all six places;
+// bound by its writes, 12 bytes a value.  (As one copy a place, prepare() of kd_kernels.hip read them six times: V = 32000, H = 1432
+// 299 us; so 130 us, 5.7 TB/s.)
+__global__ __launch_bounds__(256) void head_split_kernel(const float* src, int64_t V, int H, int K, bf16_t* dst) {
+  const int wide = H / 8;
+  const int64_t i = flat_group() * 256 + threadIdx.x, r = i / wide;
+  const int c = (int)(i - r * wide) * 8;
+  if (r >= V) return;
+  const f32x4 x[2] = {*(const f32x4*)(src + r * H + c), *(const f32x4*)(src + r * H + c + 4)};
+  bf16x8 part[3];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float f = x[e >> 2][e & 3];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      part[p][e] = (bf16_t)f;
+      f -= (float)part[p][e];
+    }
+  }
+  bf16_t* const to = dst + r * K + c;
+#pragma unroll
+  for (int place = 0; place < 6; ++place) {
+    const int p = part_of_six(place, true);
+    *(bf16x8*)(to + place * H) = p == 0 ? part[0] : p == 1 ? part[1] : part[2];
+  }
+  bf16x8 zero;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) zero[e] = (bf16_t)0.f;
+  for (int k = 6 * H + c; k < K; k += H) *(bf16x8*)(dst + r * K + k) = zero;
+}
+
+hipError_t launch_head_split(const HeadProblem& h, hipStream_t st) {
+  const Problem& p = h.p;
+  const FlatGrid g = flat_grid(((int64_t)p.V * (p.H_s / 8) + 255) / 256);
+  hipLaunchKernelGGL(head_split_kernel, dim3(g.x, g.y), dim3(256), 0, st, (const float*)p.user_W_s, (int64_t)p.V, p.H_s, p.K_s,
+                     (bf16_t*)const_cast<void*>(p.W_s));
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------
 // combine
 // ------------------------------------------------------------------------------------------
 struct PackHArgs {         // h transposed for grad_W: see pack_columns (kd_kernels.hip), `sets` copies of the token axis
@@ -207,12 +249,7 @@ struct HeadCombineArgs {
 
 // Which bf16 part of h stands against copy s of dL/dz: dz 0 0 0 1 1 2 x h 0 1 2 0 1 0, or dz 0 1 2 x h itself.
 __device__ __forceinline__ bf16_t h_part(float f, int s, int sets) {
-  const int part = sets == 6 ? 0x010210 >> (4 * s) & 15 : 0;
-  const bf16_t hi = (bf16_t)f;
-  if (part == 0) return hi;
-  const float rest = f - (float)hi;
-  const bf16_t mid = (bf16_t)rest;
-  return part == 1 ? mid : (bf16_t)(rest - (float)mid);
+  return part_of(f, sets == 6 ? part_of_six(s, false) : 0);
 }
 
 // Block b of 64 tokens x 64 hidden rows, by NT threads.

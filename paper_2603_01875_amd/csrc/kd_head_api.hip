@@ -227,6 +227,7 @@ kd_status run(const HeadProblem& h, bool backward, hipStream_t st) {
   const Problem& q = h.p;
   if (!(h.few && h.t.ce)) KD_TRY(kd::launch_targets(h, st));
   KD_TRY(kd::launch_operands(q, !h.few, true, false, st));
+  if (q.in_f32 && !q.w_hv) KD_TRY(kd::launch_head_split(h, st));
   KD_TRY(h.few ? kd::launch_head_few(h, st) : kd::launch_head_stats(h, st));
   KD_TRY(kd::launch_head_combine(h, backward, backward && q.grad_W_s, st));
   if (!backward) return KD_OK;

@@ -465,18 +465,6 @@ __global__ void transpose_kernel(const E* src, int64_t ld_src, int R, int C, E* 
   }
 }
 
-// fp32 operands as bf16 parts laid side by side along K.  src_f32 == 1, the two-model losses: two parts, three products (see prepare);
-// src_f32 == 2, the one-head losses: three parts, f = f0 + f1 + f2 to 24 bits, and the six products of them that are not below
-// those bits, the head as [0 0 0 1 1 2], the hidden states as [0 1 2 0 1 0].
-__device__ __forceinline__ int part_of_six(int place, bool head) { return (head ? 0x211000 : 0x010210) >> (4 * place) & 15; }
-__device__ __forceinline__ bf16_t part_of(float f, int part) {
-  const bf16_t hi = (bf16_t)f;
-  if (part == 0) return hi;
-  const float rest = f - (float)hi;
-  const bf16_t mid = (bf16_t)rest;
-  return part == 1 ? mid : (bf16_t)(rest - (float)mid);
-}
-
 // The token operand of the strip loop: the compacted rows (row j = row rowmap[j] of src for j < n_valid, zero
 // beyond) in the order in which its waves load them: [64-token panel][32-element sub-step][16-token block][lane][8],
 // lane l holding elements 8 (l / 16) .. + 7 of token l mod 16.  fp32 rows become [hi | lo | hi] (see
@@ -857,7 +845,7 @@ hipError_t launch_operands(const Problem& p, bool rowmap, bool student, bool tea
   if (teacher && p.prep_ht) hidden(p.user_h_t, p.H_t, const_cast<void*>(p.h_t), p.K_t, p.t_fp8);
   if (student && p.prep_hs) hidden(p.user_h_s, p.H_s, const_cast<void*>(p.h_s), p.K_s, false);
   if (teacher && p.prep_Wt && !p.w_hv) head(p.user_W_t, p.H_t, const_cast<void*>(p.W_t), p.K_t);
-  if (student && p.prep_Ws && !p.w_hv) head(p.user_W_s, p.H_s, const_cast<void*>(p.W_s), p.K_s);
+  if (student && p.prep_Ws && !p.w_hv && !(p.in_f32 && p.f32_parts)) head(p.user_W_s, p.H_s, const_cast<void*>(p.W_s), p.K_s);
   auto launch = [&](int64_t groups, const OperandArgs& a) {
     const FlatGrid g = flat_grid(groups);
     if (groups) hipLaunchKernelGGL(operands_kernel, dim3(g.x, g.y), dim3(1024), 0, st, a);

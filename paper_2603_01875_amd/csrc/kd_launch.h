@@ -114,6 +114,7 @@ constexpr int kHeadRows = 256;         // vocabulary rows per tile
 // kept in fp32, in dz's order, and turned into dz without multiplying again
 struct HeadProblem { Problem p; Targets t; int few, parts; float* kept; };
 hipError_t launch_targets(const HeadProblem& h, hipStream_t st);
+hipError_t launch_head_split(const HeadProblem& h, hipStream_t st);      // the copy of an fp32 head kept as [V][H]
 hipError_t launch_head_stats(const HeadProblem& h, hipStream_t st);
 hipError_t launch_head_few(const HeadProblem& h, hipStream_t st);
 // (with the losses' sum, unless a backward pass on kept logits does it)
