@@ -255,7 +255,8 @@ kd_status kd_loss_fwd_bwd_multi(const kd_loss_params* params, int n_teachers,
  * the workspace.
  *
  * fp32 operands are multiplied as three bf16 parts each (six products, 24 bits), and fp32 gradients are fp32 sums of
- * products in which dL/dz is held in three parts: fp32 results are as exact as fp32 arithmetic gives them.  For bf16
+ * products in which dL/dz is held in three parts: fp32 results are as exact as fp32 arithmetic gives them.  (Infinite
+ * weights need bf16 operands, where a logit of minus infinity is a row of probability 0; the parts of fp32 ones give NaN.)  For bf16
  * gradients dL/dz is rounded to bf16 once, without the factor loss_scale / n that all its entries share, and the sums
  * once more. */
 

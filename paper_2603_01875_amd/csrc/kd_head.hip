@@ -358,8 +358,8 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
     for (int k = g; k < a.K && list[k] != kNoEntry; k += G) {
       const float zk = z(k), d = fmaf(zk, a.c, -m[1]);
       v[1] += fexp2(d);
-      v[2] += zk;
-      v[3] = fmaf(prob[k], d, v[3]);
+      if (a.nv == 3) v[2] += zk;
+      if (prob[k] != 0.f) v[3] = fmaf(prob[k], d, v[3]);        // (0 log 0 = 0: a logit of minus infinity)
       v[4] += prob[k];
     }
     merge_parts<TX, NT, 5, MergeSum>(v, lds);
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
       const double big = fmax(lo, ll), lse = v[0] != v[0] || v[1] != v[1] ? __builtin_nan("") : big + log2(exp2(lo - big) + exp2(ll - big));
       const double nat = lse * ln2;
       const double on = v[4] != 0.f ? (double)v[3] + (double)m[1] * (double)v[4] : 0.0;   // sum q z in base 2
-      double loss = ent + mass * nat - ln2 * on - (double)a.uniform * (double)v[2] + (double)a.z_loss * nat * nat;
+      double loss = ent + mass * nat - ln2 * on - (a.nv == 3 ? (double)a.uniform * (double)v[2] : 0.0) + (double)a.z_loss * nat * nat;
       const double in = mass + 2.0 * (double)a.z_loss * nat;
       double out = in;
       if (rest > 0.0) {

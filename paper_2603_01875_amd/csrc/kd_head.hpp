@@ -144,7 +144,7 @@ struct HeadWork {
   }
 };
 
-// First of `n` ascending entries that is not below `row`; fifteen probes a level, whose loads are in flight together.
+// First of `n` ascending entries that is not below `row`; sixteen probes a level, whose loads are in flight together.
 __device__ __forceinline__ int first_entry(const int* list, int n, int row) {
   int at = 0;
   while (n > 0) {                          // the answer lies in at .. at + n
@@ -160,6 +160,10 @@ __device__ __forceinline__ int first_entry(const int* list, int n, int row) {
   }
   return at;
 }
+
+// Whether a logit is one of a row that exists beside the list: those of others are NEG_BIG, give or take a logit (kd_strip.hpp).  (What is
+// lower still is: minus infinity counts.)
+__device__ __forceinline__ bool counts_in(float z) { return !(fabsf(z - NEG_BIG) <= -0.9f * NEG_BIG); }
 
 struct HeadGeo {
   int wave, lane;
@@ -291,7 +295,7 @@ struct HeadStatsEpi {
       static_for<0, NE>([&](auto ec) {
         const float z = logit(ec);
         s += fexp2(fmaf(z, a.c, -m));
-        if (SMOOTH) zs += z > 0.1f * NEG_BIG ? z : 0.f;
+        if (SMOOTH) zs += counts_in(z) ? z : 0.f;
       });
       *(f32x4*)at = f32x4{m, fmaf(old[1], fexp2(old[0] - m), quad_sum(s)), SMOOTH ? old[2] + quad_sum(zs) : 0.f, 0.f};
     };
@@ -378,7 +382,7 @@ struct HeadGradEpi {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float z = T[16 * p + 8 * u + e];
-          x[e] = unlisted_dz(ri, z, a.c, SMOOTH ? (z > 0.1f * NEG_BIG ? -ri[2] : 0.f) : 0.f);
+          x[e] = unlisted_dz(ri, z, a.c, SMOOTH ? (counts_in(z) ? -ri[2] : 0.f) : 0.f);
         }
         store_dz<PARTS>(x, a.dz + dz_chunk(a.ldz, panel, (m0 >> 5) + 2 * p + u, j, geo.lane), (int64_t)panels * 64 * a.ldz, a.sets);
       }

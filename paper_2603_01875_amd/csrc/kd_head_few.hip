@@ -248,7 +248,7 @@ struct FewEpi {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           s += fexp2(fmaf(z[e], a.c, -m));
-          if (SMOOTH) zs += z[e] > 0.1f * NEG_BIG ? z[e] : 0.f;
+          if (SMOOTH) zs += counts_in(z[e]) ? z[e] : 0.f;
         }
         *at = f32x4{m, fmaf(old[1], fexp2(old[0] - m), quad_sum(s)), SMOOTH ? old[2] + quad_sum(zs) : 0.f, 0.f};
       }

@@ -229,6 +229,51 @@ def test_weights_of_infinity_in_rows_of_their_own():
     assert (out["grad_W"][9] == 0).all() and not out["grad_W"].isnan().any()
 
 
+@pytest.mark.parametrize("T,chunk,layout", [(50, 0, "vh"), (50, 0, "hv"), (300, 0, "vh"), (300, 256, "vh"), (300, 256, "hv")])
+@pytest.mark.parametrize("smoothing", [0.0, 0.1])
+def test_probabilities_of_zero_where_the_target_is_not(T, chunk, layout, smoothing):
+    """A logit of minus infinity that the target gives a probability: the loss is infinite, and dL/dz = p - q still holds."""
+    H, V = 128, 1024
+    h, W, y, _ = U.make(55, T, H, V, "bf16")
+    h[:, 5] = h[:, 5].abs() + 1
+    y[y == 9] = 10
+    y[::4] = 9
+    W_inf, W_low = W.clone(), W.clone()
+    W_inf[9, 5], W_low[9, 5] = -float("inf"), -1e6
+    out = K.kd_ce_fwd_bwd(*U.device(h, W_inf, layout), y.cuda(), None, smoothing, 0.0, U.LAYOUT[layout], K.F32, vocab_chunk=chunk,
+                          want_grad_h=False)
+    low = O.cross_entropy(U.np64(h), U.np64(W_low), y.numpy(), None, smoothing)
+    rows = U.np64(out["per_token_loss"])
+    infinite = np.ones(T, bool) if smoothing else y.numpy() == 9
+    assert np.isposinf(rows[infinite]).all() and np.isposinf(out["loss"].item())
+    W[9] = 0                                               # (the row is no logit's error; its share of p, below 1 %, is the 1.01)
+    b = U.bounds(U.np64(h), U.np64(W), low, 1.0, "bf16", "f32")
+    assert (np.abs(rows - low["per_token_loss"])[~infinite] <= 1.01 * b["rows"][~infinite] + 8 * U.F32 * 40).all()
+    gW = U.np64(out["grad_W"] if layout == "vh" else out["grad_W"].T)
+    assert (np.abs(gW - low["grad_W"]) <= 1.01 * b["grad_W"]).all()
+
+
+@pytest.mark.parametrize("T", [50, 300])
+@pytest.mark.parametrize("tail", [O.RENORM, O.DROP])
+def test_entries_of_no_weight_add_nothing(T, tail):
+    """Top logits of the type's lowest value: their probability is 0, also where the student's is."""
+    H, V, k = 128, 1024, 6
+    h, W, y, rng = U.make(56, T, H, V, "bf16")
+    h[:, 5] = h[:, 5].abs() + 1
+    W[9, 5] = -float("inf")
+    a, ids = U.top_lists(rng, T, V, k, y)
+    ids[ids == 9] = 11
+    ids[:, 0], a[:, 0] = 9, torch.finfo(torch.float32).min
+    lse = torch.zeros(T) + 3.0
+    out = K.kd_topk_fwd_bwd(a.cuda(), ids.cuda(), *U.device(h, W), lse=None if tail == O.RENORM else lse.cuda(), tail=tail)
+    W[9, 5] = -1e6
+    ref = O.topk(U.np64(a), ids.numpy(), U.np64(h), U.np64(W), U.np64(lse), tail=tail)
+    W[9] = 0
+    b = U.bounds(U.np64(h), U.np64(W), ref, 1.0, "bf16", "bf16")
+    assert (np.abs(U.np64(out["per_token_loss"]) - ref["per_token_loss"]) <= 1.01 * b["rows"] + 8 * U.F32 * 40).all()
+    assert not out["grad_W_s"].isnan().any() and (out["grad_W_s"][9] == 0).all()
+
+
 @pytest.mark.parametrize("T", [50, 300])
 @pytest.mark.parametrize("grad", ["bf16", "f32"])
 def test_gradients_one_at_a_time_and_added_up(T, grad):
@@ -390,3 +435,102 @@ def test_a_head_whose_offsets_pass_32_bits():
         gW = dz[:, rows].t() @ h.double() / T
         bound = dz[:, rows].abs().t() @ h.double().abs() / T * (U.BF16 + 2e-3) + U.BF16 * gW.abs()
         assert ((out["grad_W"][rows].double() - gW).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("T", [31, 32, 33])
+@pytest.mark.parametrize("layout", ["vh", "hv"])
+def test_around_the_tokens_that_one_workgroup_merges(T, layout):
+    _ce((T, 128, 1024), 60 + T, layout=layout, smoothing=0.05)
+    _topk((T, 128, 1024), 70, O.REST, 60 + T, layout=layout)
+
+
+def test_fp32_products_whose_partial_sums_would_be_too_many():
+    """fp32 operands and gradients: six products of 2304 x 2560 sums are more than 128 MiB, so each adds to those in front of it."""
+    T, H, V = 2304, 2560, 520
+    h, W, y, rng = U.make(80, T, H, V, "f32", w_std=0.02)
+    y = _labels(y, rng, T)
+    ref = O.cross_entropy(U.np64(h), U.np64(W), y.numpy())
+    out = K.kd_ce_fwd_bwd(*U.device(h, W), y.cuda())
+    torch.cuda.synchronize()
+    U.check(out, ref, U.np64(h), U.np64(W), in_dtype="f32", grad_dtype="f32")
+
+
+@pytest.mark.parametrize("T,k", [(40, 7), (300, 70), (300, 300)])
+@pytest.mark.parametrize("tail", [O.RENORM, O.REST, O.DROP])
+def test_the_same_row_in_many_entries(T, k, tail):
+    """Lists of three rows, and of one, each many times over; importance weights that do not add up to one."""
+    H, V = 64, 520
+    h, W, y, rng = U.make(90, T, H, V, "f32")
+    a = torch.from_numpy(rng.standard_normal((T, k)).astype(np.float32))
+    ids = torch.from_numpy(np.asarray([0, 255, V - 1])[rng.integers(0, 3, (T, k))])
+    ids[::3] = 256
+    lse = torch.from_numpy((np.log(np.exp(U.np64(a)).sum(1)) + (0.5 if tail == O.REST else -0.7)).astype(np.float32))
+    ref = O.topk(U.np64(a), ids.numpy(), U.np64(h), U.np64(W), U.np64(lse), None, 1.0, tail)
+    out = K.kd_topk_fwd_bwd(a.cuda(), ids.cuda(), *U.device(h, W), lse=None if tail == O.RENORM else lse.cuda(), tail=tail)
+    torch.cuda.synchronize()
+    p = np.exp(O.log_softmax(U.np64(h) @ U.np64(W).T))
+    on = np.zeros((T, V), bool)
+    np.put_along_axis(on, ids.numpy(), True, 1)
+    # (DROP: the weights add up to 2; REST: beside the list, r / (1 - P))
+    big = 2 + 1.0 / np.where(on, 0, p).sum(1).min() if tail == O.REST else 2.1
+    U.check(out, ref, U.np64(h), U.np64(W), in_dtype="f32", grad_dtype="f32", coefficient=big)
+
+
+@pytest.mark.parametrize("T", [20, 300])
+def test_arrays_aligned_to_their_elements_only(T):
+    """Labels, lists, masks (bool), and the losses' places need no more; what lies beside them stays."""
+    H, V, k = 128, 1000, 9
+    h, W, y, rng = U.make(91, T, H, V, "bf16")
+    y = _labels(y, rng, T)
+    a, ids = U.top_lists(rng, T, V, k, y.abs() % V)
+    hd, Wd = U.device(h, W)
+    mask = torch.from_numpy(rng.random(T) < 0.7)
+
+    def odd(t, fill):
+        whole = torch.full((t.numel() + 2,), fill, dtype=t.dtype, device="cuda")
+        whole[1:-1] = t.flatten().cuda()
+        return whole[1:-1].view(t.shape)
+    for itype, ttype in ((torch.int32, torch.bfloat16), (torch.int64, torch.float32)):
+        want = K.kd_ce_fwd_bwd(hd, Wd, y.to(itype).cuda(), mask.cuda().to(torch.uint8))
+        ytop = (a.to(ttype), ids.to(itype))
+        want2 = K.kd_topk_fwd_bwd(*(t.cuda() for t in ytop), hd, Wd, mask=mask.cuda())
+        got = K.kd_ce_fwd_bwd(hd, Wd, odd(y.to(itype), 3), odd(mask, True))
+        got2 = K.kd_topk_fwd_bwd(odd(ytop[0], 99.0), odd(ytop[1], 3), hd, Wd, mask=odd(mask, True))
+        for w, g in ((want, got), (want2, got2)):
+            for n in w:
+                assert n == "workspace" or torch.equal(w[n], g[n]), n
+        p = K.make_ce_params(T, H, V, index_dtype=K.I32 if itype == torch.int32 else K.I64)
+        places = torch.full((T + 4,), 5.0, device="cuda")
+        K.kd_ce_fwd_raw(p, hd, Wd, y.to(itype).cuda(), mask.cuda(), places[1:2], places[3:3 + T], K.alloc_workspace(p))
+        assert torch.equal(places[1:2], want["loss"]) and torch.equal(places[3:3 + T], want["per_token_loss"])
+        assert (places[[0, 2, T + 3]] == 5).all()
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Captured one after the other on one workspace and replayed in turn, in both orders, with eager calls between."""
+    H, V = 128, 2056
+    h, W, y, rng = U.make(92, 300, H, V, "bf16")
+    a, ids = U.top_lists(rng, 300, V, 12, y)
+    hd, Wd = U.device(h, W)
+    ws = torch.empty(max(K.kd_loss_workspace_size(K.make_ce_params(300, H, V)), K.kd_loss_workspace_size(K.make_topk_params(50, H, V, 12))),
+                     dtype=torch.uint8, device="cuda")
+    calls = [lambda: K.kd_ce_fwd_bwd(hd, Wd, yd, workspace=ws),
+             lambda: K.kd_topk_fwd_bwd(ad, idd, xd, Wd, workspace=ws)]
+    yd, ad, idd, xd = y.cuda(), a[:50].cuda(), ids[:50].cuda(), hd[:50].contiguous()
+    want, graphs, outs = [], [], []
+    for call in calls:
+        want.append({k: v.clone() for k, v in call().items() if k != "workspace"})
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call())
+        graphs.append(g)
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1)):
+        for i in order:
+            graphs[i].replay()
+        calls[order[0]]()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            assert all(torch.equal(outs[i][k], want[i][k]) for k in want[i]), (order, i)
+            for k in want[i]:
+                outs[i][k].fill_(3)
