@@ -33,7 +33,8 @@ __global__ __launch_bounds__(256) void label_targets_kernel(const TargetArgs a) 
   if (t < a.T) (void)label_target(a, t);
 }
 
-// G threads per token.  The entries that are there (a row that is not negative, a logit above minus infinity) go to the place that the
+// G threads per token, 64 or, of lists longer than that, 256 (4096 tokens with 64 entries 11 us).
+// The entries that are there (a row that is not negative, a logit above minus infinity) go to the place that the
 // count of smaller rows gives them: K compares each, out of LDS, four at a time (K = 217, 4546 tokens: 37.5 us).  Entries of the same row,
 // which meet in one place, add up, in a second look that most calls do not need.  All sums in 64 bits: the mass beside the list is a
 // difference from 1.
@@ -311,7 +312,9 @@ __device__ __forceinline__ void sum_losses(const LossSumArgs& a, double* sums) {
   }
 }
 
-// Merges a token's partial sums and its listed logits.  Logarithms in base 2; what is a difference of large quantities in double.
+// Merges a token's partial sums and its listed logits: lse, and with it the loss and the coefficients of dL/dz (kd_head.hpp).  Bound by
+// latency (T = 4096 22 us with packing h beside it, T = 100 with 256 partial sums a token 11 us).  Logarithms in base 2; what is a
+// difference of large quantities in double.
 template <int TX, int NT>
 __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs a) {
   constexpr int BYTES = sizeof(float) * 64 * 65;
@@ -407,7 +410,8 @@ static LossSumArgs loss_sum_args(const HeadProblem& h) {
 
 hipError_t launch_head_combine(const HeadProblem& h, bool backward, bool pack_h, hipStream_t st) {
   const Problem& p = h.p;
-  // 8 tokens x 128 threads where a token has many parts, 32 x 8 else (see merge_parts); 32 x 32 where that is all the tokens
+  // 8 tokens x 128 threads where a token has many parts, 32 x 8 else (see merge_parts); 32 x 32 where that is all the
+  // tokens and the sum can follow (one token 10.4 us; 8.7 and 4.6 in two launches)
   const bool all = p.T <= 32, many = !all && (h.few ? h.parts : p.n_split) >= 128;
   HeadCombineArgs a{p.partials, p.meta, p.rowmap, p.inv, p.T, p.T_pad, h.t.smoothing > 0.f ? 3 : 2, h.t.K, h.few ? h.parts : 0,
                     1.4426950408889634f / p.tau, h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.kept, p.V_c, h.t.info,
@@ -458,7 +462,8 @@ hipError_t launch_head_stats(const HeadProblem& h, hipStream_t st) {
 #undef KD_HS
 }
 
-// dL/dz of a chunk on the lists: A_in p - q - U, where the tile kernel has written what it would be beside them.  One thread per entry.
+// dL/dz of a chunk on the lists: A_in p - q - U, where the tile kernel has written what it would be beside them.  One thread per entry;
+// bound by latency (4096 tokens' lists of 64 5 us a chunk).
 struct ListedArgs {
   const int *meta, *rowmap, *list;
   const float *q, *z;
@@ -492,7 +497,8 @@ __global__ __launch_bounds__(256) void head_listed_kernel(const ListedArgs a) {
 }
 
 // All of it from kept logits (the whole vocabulary is one chunk).  A workgroup makes 256 columns of a panel of 64 tokens, 4 KiB of
-// each 32; bound by memory, 6 bytes a logit.  Which of them are listed stands in LDS, a word per token and 32 columns.
+// each 32; bound by memory, 6 bytes a logit (T = 200, V = 151936: 35 us, 6.5 TB/s with what the last-level cache still holds).  Which of
+// them are listed stands in LDS, a word per token and 32 columns.
 struct KeptArgs {
   HeadArgs h;
   const int* inv;

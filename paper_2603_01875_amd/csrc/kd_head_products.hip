@@ -5,13 +5,17 @@
 
 namespace kd {
 
+// Bound by the matrix pipe (T = 4096, 3584 computed, H = 1024, V = 151936: 867 us in five chunks, 1.29 PFLOP/s), of one token tile
+// (head_gw_few_kernel) by the stores of grad_W (T = 100 65 us, 5.4 TB/s).  What the contraction adds in front of the rounding is one
+// multiplication a result.
 template <int NB, bool HV, bool F32, bool ADD>
 KD_STRIP_KERNEL void head_gw_kernel(const GradWArgs a) { grad_w<NB, HV, F32, ADD, true>(a); }
 template <bool HV, bool ADD>
 __global__ __launch_bounds__(256, 2) void head_gw_few_kernel(const GradWArgs a) { grad_w_few<HV, false, ADD, true>(a); }
 
 // grad_h with few tokens: bound by the head, which streams through once, so by how much of it is in flight.  The accumulator of 64 NB
-// tokens leaves room for two workgroups a CU, 32 KiB each on their way (and the stores of one under the products of the other).
+// tokens leaves room for two workgroups a CU, 32 KiB each on their way (and the stores of one under the products of the other).  T = 128,
+// H = 1024, V = 151936: 79 us, 4.4 TB/s (three workgroups a CU: slower).
 template <int NB, bool HV>
 __global__ __launch_bounds__(256, 2) void head_gh_few_kernel(const GradHArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];

@@ -26,7 +26,8 @@ inline int grad_W_tile(int64_t H_s, int64_t width, int n_cu) {
   return best;
 }
 
-// The one-head losses take kernels of their own with at most so many tokens; grad_h_s then has so many workgroups at a time.
+// The one-head losses take kernels of their own with at most so many tokens (kd_head_few.hip, head_gh_few_kernel); grad_h_s then has so
+// many workgroups at a time.
 constexpr int kFewHeadTokens = 128;
 constexpr int kFewGradHGroups = 2 * kNumCU;
 
