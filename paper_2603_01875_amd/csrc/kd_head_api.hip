@@ -139,8 +139,11 @@ void plan(const Call& c, HeadProblem& h, HeadLayout& L, bool backward) {
     }
   }
 
-  const bool keeps = backward && q.V_c == v_all && (int64_t)q.T_pad * v_all * 4 <= kKept;
-  h.few = q.T <= kd::kFewHeadTokens && !q.w_hv_inplace && q.K_s == (q.prep_Ws ? q.K_s : q.H_s) && (keeps || !backward);
+  // (the loop for few tokens keeps whole panels of 64 tokens, the strip loop whole tiles)
+  const bool few = q.T <= kd::kFewHeadTokens && !q.w_hv_inplace && (q.prep_Ws || q.K_s == q.H_s);
+  const int64_t kept_bytes = (few ? round_up(q.T, 64) : q.T_pad) * v_all * 4;
+  const bool keeps = backward && q.V_c == v_all && kept_bytes <= kKept;
+  h.few = few && (keeps || !backward);
   if (h.few) {
     const int units32 = (q.V + 31) / 32;
     h.parts = units32 < q.n_cu ? units32 : q.n_cu;
@@ -178,7 +181,7 @@ void plan(const Call& c, HeadProblem& h, HeadLayout& L, bool backward) {
   const size_t end = (size_t)round_up((int64_t)(L.partials + partial_bytes), 256);
   if (off < end) off = end;
   L.kept = off;
-  if (keeps) take((size_t)q.T_pad * q.V_c * 4);
+  if (keeps) take((size_t)kept_bytes);
   L.total = off;
   h.kept = keeps ? reinterpret_cast<float*>(1) : nullptr;      // (the address: carve)
 }

@@ -534,3 +534,35 @@ def test_two_graphs_that_share_a_workspace():
             assert all(torch.equal(outs[i][k], want[i][k]) for k in want[i]), (order, i)
             for k in want[i]:
                 outs[i][k].fill_(3)
+
+
+@pytest.mark.parametrize("T,H,V,k", [(1, 64, 264, 3), (64, 64, 1000, 5), (65, 72, 1000, 70), (128, 128, 2056, 9), (129, 128, 776, 9),
+                                     (300, 136, 1544, 33)])
+@pytest.mark.parametrize("dtype,layout", [("bf16", "vh"), ("f32", "vh"), ("bf16", "hv")])
+def test_nothing_beside_the_buffers_is_written(T, H, V, k, dtype, layout):
+    h, W, y, rng = U.make(93, T, H, V, dtype)
+    a, ids = U.top_lists(rng, T, V, k, y)
+    hd, Wd = U.device(h, W, layout)
+    ids, a, y = ids.cuda(), a.cuda(), y.cuda()
+    kw = dict(in_dtype=K.BF16 if dtype == "bf16" else K.F32, w_layout=U.LAYOUT[layout])
+    for chunk in (0, 256):
+        calls = [(K.make_ce_params(T, H, V, 0.1, vocab_chunk=chunk, **kw),
+                  lambda p, o: K.kd_ce_fwd_bwd_raw(p, hd, Wd, y, None, *o)),
+                 (K.make_topk_params(T, H, V, k, vocab_chunk=chunk, **kw),
+                  lambda p, o: K.kd_topk_fwd_bwd_raw(p, a, ids, None, hd, Wd, None, *o))]
+        for p, call in calls:
+            es = hd.element_size()
+            sizes = [4, 4 * T, es * T * H, es * V * H, K.kd_loss_workspace_size(p)]
+            at = [4096]
+            for n in sizes:
+                at.append((at[-1] + n + 4096 + 255) // 256 * 256)
+            whole = torch.full((at[-1],), 0x5a, dtype=torch.uint8, device="cuda")
+            part = [whole[b:b + n] for b, n in zip(at, sizes)]
+            types = [torch.float32, torch.float32, hd.dtype, hd.dtype, torch.uint8]
+            call(p, [x.view(t) for x, t in zip(part, types)])
+            torch.cuda.synchronize()
+            for x in part[:4]:
+                assert not (x == 0x5a).all()
+            for x in part:
+                x.fill_(0x5a)
+            assert (whole == 0x5a).all()
