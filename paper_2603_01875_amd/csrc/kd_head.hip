@@ -412,7 +412,7 @@ hipError_t launch_head_combine(const HeadProblem& h, bool backward, bool pack_h,
   const Problem& p = h.p;
   // 8 tokens x 128 threads where a token has many parts, 32 x 8 else (see merge_parts); 32 x 32 where that is all the
   // tokens and the sum can follow (one token 10.4 us; 8.7 and 4.6 in two launches)
-  const bool all = p.T <= 32, many = !all && (h.few ? h.parts : p.n_split) >= 128;
+  const bool all = p.T <= 32, many = !all && ((h.few ? h.parts : p.n_split) >= 128 || h.t.K >= 128);
   HeadCombineArgs a{p.partials, p.meta, p.rowmap, p.inv, p.T, p.T_pad, h.t.smoothing > 0.f ? 3 : 2, h.t.K, h.few ? h.parts : 0,
                     1.4426950408889634f / p.tau, h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.kept, p.V_c, h.t.info,
                     (f32x4*)p.rowinfo, p.row_loss, p.out_weight, p.per_token_loss, all ? 1 : many ? p.T_pad / 8 : p.T_pad / 32,
@@ -506,7 +506,7 @@ struct KeptArgs {
   LossSumArgs sum;         // (if the merge has not done it: loss not null)
 };
 template <int PARTS>
-__global__ __launch_bounds__(256) void head_dz_kernel(const KeptArgs k) {
+__global__ __launch_bounds__(256, PARTS == 1 ? 5 : 4) void head_dz_kernel(const KeptArgs k) {
   __shared__ uint32_t listed[64][8];
   __shared__ int first[64], whose[64];
   const HeadArgs& a = k.h;
@@ -527,27 +527,31 @@ __global__ __launch_bounds__(256) void head_dz_kernel(const KeptArgs k) {
     z[s][1] = *(const f32x4*)(from + 4);
   }
   const f32x4 ri = a.rowinfo[panel * 64 + i];
-  if (threadIdx.x < 64) {
-    const int i = threadIdx.x, j = panel * 64 + i;
+  {                                          // four threads a token, four entries each at a time
+    const int i = threadIdx.x >> 2, r = threadIdx.x & 3, j = panel * 64 + i;
     const int token = j < a.meta[META_N_VALID] ? a.rowmap[j] : -1;
     const bool counts = token >= 0 && k.inv[token] >= 0;
-    *(u32x4*)listed[i] = u32x4{0u, 0u, 0u, 0u};
-    *(u32x4*)(listed[i] + 4) = u32x4{0u, 0u, 0u, 0u};
-    whose[i] = counts ? token : -1;
+    listed[i][2 * r] = listed[i][2 * r + 1] = 0u;
+    if (r == 0) whose[i] = counts ? token : -1;
     if (counts) {
       const int* const list = a.list + (int64_t)token * a.n_list;
-      int at = first_entry(list, a.n_list, 32 * sub0);
-      first[i] = at;
-      for (; at < a.n_list; ++at) {
-        const int col = list[at] - 32 * sub0;
-        if (col >= 256) break;
-        listed[i][col >> 5] |= 1u << (col & 31);
+      const int from = first_entry(list, a.n_list, 32 * sub0);
+      if (r == 0) first[i] = from;
+      for (int at = from + r; at < a.n_list; at += 16) {
+        int col[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) col[e] = list[min(at + 4 * e, a.n_list - 1)] - 32 * sub0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at + 4 * e < a.n_list && col[e] < 256) atomicOr(&listed[i][col[e] >> 5], 1u << (col[e] & 31));
+        if (col[3] >= 256) break;
       }
     }
   }
   __syncthreads();
   const int token = whose[i];                                              // (of tokens that do not count there may be no logits)
   const int64_t stride = (int64_t)panels * 64 * a.ldz;
+  int rank = first[i];                                                     // entries of the list in front of the sub-step
 #pragma unroll
   for (int s = 0; s < 8; ++s) {
     if (s >= subs) break;
@@ -561,17 +565,19 @@ __global__ __launch_bounds__(256) void head_dz_kernel(const KeptArgs k) {
       x[e] = there ? d : 0.f;
     }
     if (mine) {
-      int rank = first[i];
-      for (int w = 0; w < s; ++w) rank += __popc(listed[i][w]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int bit = (e < 4 ? 0 : 16) + (e & 3);
-        if (mine >> bit & 1) {
-          const int n = rank + __popc(word & ((1u << (bit + 4 * g)) - 1));
-          x[e] = listed_dz(ri, z[s][e >> 2][e & 3], a.c, k.q[(int64_t)token * a.n_list + n]);
-        }
+      for (int half = 0; half < 2; ++half) {           // (four on their way together; with eight registers run out)
+        float q[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          q[e] = k.q[(int64_t)token * a.n_list + min(rank + (int)__popc(word & ((1u << (4 * g + 16 * half + e)) - 1)), a.n_list - 1)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[4 * half + e] = mine >> (16 * half + e) & 1 ? listed_dz(ri, z[s][half][e], a.c, q[e]) : x[4 * half + e];
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    rank += __popc(word);
     store_dz<PARTS>(x, a.dz + at, stride, a.sets);
   }
 }
