@@ -410,8 +410,9 @@ static LossSumArgs loss_sum_args(const HeadProblem& h) {
 
 hipError_t launch_head_combine(const HeadProblem& h, bool backward, bool pack_h, hipStream_t st) {
   const Problem& p = h.p;
-  // 8 tokens x 128 threads where a token has many parts, 32 x 8 else (see merge_parts); 32 x 32 where that is all the
-  // tokens and the sum can follow (one token 10.4 us; 8.7 and 4.6 in two launches)
+  // 8 tokens x 128 threads where a token has many parts (see merge_parts) or a long list (128 entries 12.6 us, by 32 x 8 18.2, 64 entries of
+  // 4096 tokens 37.8 and 23.5), 32 x 8 else; 32 x 32 where that is all the tokens and the sum can follow (one token 10.4 us; 8.7 and 4.6 in
+  // two launches)
   const bool all = p.T <= 32, many = !all && ((h.few ? h.parts : p.n_split) >= 128 || h.t.K >= 128);
   HeadCombineArgs a{p.partials, p.meta, p.rowmap, p.inv, p.T, p.T_pad, h.t.smoothing > 0.f ? 3 : 2, h.t.K, h.few ? h.parts : 0,
                     1.4426950408889634f / p.tau, h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.kept, p.V_c, h.t.info,
@@ -498,7 +499,8 @@ __global__ __launch_bounds__(256) void head_listed_kernel(const ListedArgs a) {
 
 // All of it from kept logits (the whole vocabulary is one chunk).  A workgroup makes 256 columns of a panel of 64 tokens, 4 KiB of
 // each 32; bound by memory, 6 bytes a logit (T = 200, V = 151936: 35 us, 6.5 TB/s with what the last-level cache still holds).  Which of
-// them are listed stands in LDS, a word per token and 32 columns.
+// them are listed stands in LDS, a word per token and 32 columns.  With long lists by the latency of their marking and of loading
+// their probabilities (T = 1909, V = 5424, K = 202: 29 us for 60 MB; one entry at a time 62 us).
 struct KeptArgs {
   HeadArgs h;
   const int* inv;
