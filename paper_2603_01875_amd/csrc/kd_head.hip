@@ -533,7 +533,8 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 5 : 4) void head_dz_kernel(const 
     const int i = threadIdx.x >> 2, r = threadIdx.x & 3, j = panel * 64 + i;
     const int token = j < a.meta[META_N_VALID] ? a.rowmap[j] : -1;
     const bool counts = token >= 0 && k.inv[token] >= 0;
-    listed[i][2 * r] = listed[i][2 * r + 1] = 0u;
+    listed[i][2 * r] = listed[i][2 * r + 1] = 0u;            // (a token's four threads are one wave's: its LDS operations are made in order)
+    __builtin_amdgcn_wave_barrier();
     if (r == 0) whose[i] = counts ? token : -1;
     if (counts) {
       const int* const list = a.list + (int64_t)token * a.n_list;
