@@ -329,10 +329,11 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
   const int n_valid = a.meta[META_N_VALID], n_parts = a.n_parts ? a.n_parts : a.meta[META_N_SPLIT];
   const int64_t token = a.rowmap[t];
   const bool counts = t < n_valid && a.inv[token] >= 0;
+  const f32x4 nothing = {1.0e30f, 0.f, a.nv == 3 ? 0.f : 1.0e30f, 0.f};
   if (a.groups == 1)                     // (rows behind the workgroup's)
-    for (int j = TX + threadIdx.x; j < a.T_pad; j += NT) a.rowinfo[j] = f32x4{1.0e30f, 0.f, 0.f, 0.f};
+    for (int j = TX + threadIdx.x; j < a.T_pad; j += NT) a.rowinfo[j] = nothing;
   if (!counts && g == 0) {             // everything evaluates to 0
-    a.rowinfo[t] = f32x4{1.0e30f, 0.f, 0.f, 0.f};
+    a.rowinfo[t] = nothing;
     a.row_loss[t] = 0.f;
   }
   if (g == 0 && t < a.T && a.per_token && a.inv[t] < 0) a.per_token[t] = 0.f;
@@ -377,15 +378,16 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
       const double on = v[4] != 0.f ? (double)v[3] + (double)m[1] * (double)v[4] : 0.0;   // sum q z in base 2
       double loss = ent + mass * nat - ln2 * on - (a.nv == 3 ? (double)a.uniform * (double)v[2] : 0.0) + (double)a.z_loss * nat * nat;
       const double in = mass + 2.0 * (double)a.z_loss * nat;
-      double out = in;
+      double out = in, base = lse;
       if (rest > 0.0) {
         loss -= rest * lo * ln2;
-        out -= rest * exp2(lse - lo);
+        out = in * exp2(lo - lse) - rest;
+        base = lo;
       }
-      // (the log-sum-exp as a float is up to 1e-6 off, the same way for all of a token's entries: that goes into the coefficients)
-      const float high = (float)lse;
-      const double corr = exp2((double)high - lse);
-      a.rowinfo[t] = f32x4{high, (float)(out * corr), a.uniform, (float)(in * corr)};
+      // (a logarithm as a float is up to 1e-6 off, the same way for all of a token's entries: that goes into the factors)
+      const float high = (float)lse, high_out = (float)base;
+      a.rowinfo[t] = f32x4{high, (float)(out * exp2((double)high_out - base)), a.nv == 3 ? a.uniform : high_out,
+                           (float)(in * exp2((double)high - lse))};
       a.row_loss[t] = (float)loss;
       if (a.per_token) a.per_token[token] = a.weight * (float)loss;
     }
@@ -469,7 +471,7 @@ struct ListedArgs {
   const int *meta, *rowmap, *list;
   const float *q, *z;
   const f32x4* rowinfo;
-  int K, v0, v_end, ldz, sets;
+  int K, v0, v_end, ldz, sets, smooth;
   float c;
   bf16_t* dz;
 };
@@ -481,7 +483,7 @@ __global__ __launch_bounds__(256) void head_listed_kernel(const ListedArgs a) {
   const int v = a.list[at];
   if (v < a.v0 || v >= a.v_end) return;
   const f32x4 ri = a.rowinfo[j];
-  float x = listed_dz(ri, a.z[(int64_t)j * a.K + k], a.c, a.q[at]);
+  float x = listed_dz(ri, a.z[(int64_t)j * a.K + k], a.c, a.q[at], a.smooth ? ri[2] : 0.f);
   const int col = v - a.v0, c = col & 31, half = c >> 4, g = (c & 15) >> 2;
   const int64_t to = dz_chunk(a.ldz, j >> 6, col >> 5, (j >> 4) & 3, 16 * g + (j & 15)) + 4 * half + (c & 3);
   if (a.sets == 1) {
@@ -505,6 +507,7 @@ struct KeptArgs {
   HeadArgs h;
   const int* inv;
   const float* q;
+  int smooth;
   LossSumArgs sum;         // (if the merge has not done it: loss not null)
 };
 template <int PARTS>
@@ -529,6 +532,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 5 : 4) void head_dz_kernel(const 
     z[s][1] = *(const f32x4*)(from + 4);
   }
   const f32x4 ri = a.rowinfo[panel * 64 + i];
+  const float base = k.smooth ? ri[0] : ri[2], u = k.smooth ? ri[2] : 0.f;
   {                                          // four threads a token, four entries each at a time
     const int i = threadIdx.x >> 2, r = threadIdx.x & 3, j = panel * 64 + i;
     const int token = j < a.meta[META_N_VALID] ? a.rowmap[j] : -1;
@@ -564,7 +568,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 5 : 4) void head_dz_kernel(const 
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const bool there = token >= 0 && (sub0 + s) * 32 + 4 * g + (e < 4 ? 0 : 16) < a.V;       // (V is a multiple of 8)
-      const float d = unlisted_dz(ri, z[s][e >> 2][e & 3], a.c, -ri[2]);
+      const float d = unlisted_dz(ri[1], base, z[s][e >> 2][e & 3], a.c, u);
       x[e] = there ? d : 0.f;
     }
     if (mine) {
@@ -576,7 +580,7 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 5 : 4) void head_dz_kernel(const 
           q[e] = k.q[(int64_t)token * a.n_list + min(rank + (int)__popc(word & ((1u << (4 * g + 16 * half + e)) - 1)), a.n_list - 1)];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          x[4 * half + e] = mine >> (16 * half + e) & 1 ? listed_dz(ri, z[s][half][e], a.c, q[e]) : x[4 * half + e];
+          x[4 * half + e] = mine >> (16 * half + e) & 1 ? listed_dz(ri, z[s][half][e], a.c, q[e], u) : x[4 * half + e];
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -597,7 +601,7 @@ hipError_t launch_head_grad(const HeadProblem& h, int v0, int width, hipStream_t
   hipError_t e = hipSuccess;
   if (h.kept) {
     const dim3 blocks((p.V + 255) / 256, p.T_pad / 64 + 1);
-    KeptArgs k{a, p.inv, h.t.q, loss_sum_args(h)};
+    KeptArgs k{a, p.inv, h.t.q, smooth, loss_sum_args(h)};
     if (p.T <= 32) k.sum.loss = nullptr;
     if (parts) hipLaunchKernelGGL(head_dz_kernel<3>, blocks, dim3(256), 0, st, k);
     else hipLaunchKernelGGL(head_dz_kernel<1>, blocks, dim3(256), 0, st, k);
@@ -608,7 +612,7 @@ hipError_t launch_head_grad(const HeadProblem& h, int v0, int width, hipStream_t
 #undef KD_HG
   if (e != hipSuccess) return e;
   const ListedArgs l{p.meta, p.rowmap, h.t.list, h.t.q, h.t.z, (const f32x4*)p.rowinfo, h.t.K, v0, v0 + width, p.V_c, p.dz_sets,
-                     1.4426950408889634f / p.tau, (bf16_t*)p.dz};
+                     smooth, 1.4426950408889634f / p.tau, (bf16_t*)p.dz};
   const FlatGrid g = flat_grid(((int64_t)p.T * h.t.K + 255) / 256);
   hipLaunchKernelGGL(head_listed_kernel, dim3(g.x, g.y), dim3(256), 0, st, l);
   return hipGetLastError();

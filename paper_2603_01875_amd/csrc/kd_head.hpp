@@ -3,10 +3,11 @@
 // Both losses are a divergence of p = softmax(h W / tau) from a distribution q that lives on a short list of vocabulary entries per
 // token (a label: one entry), beside a constant U elsewhere (label smoothing) or one more category for all the rest:
 //   l = sum_list q (log q - log p) + r (log r - log p_rest) - U sum_v z + z_loss lse^2
-//   dl/dz_v = A_in p_v - q_v - U on the list,  A_out p_v - U beside it
+//   dl/dz_v = A_in p_v - q_v - U on the list,  A_in p_v - r p_v / p_rest - U beside it
 // The list is left out of the running sums of a tile and its logits are stored instead, so that p_rest is a sum of what lies beside
 // the list and never a difference from 1 (which a student that is sure of the list would lose), and so that dl/dz on the list is
-// written from fp32 values with one rounding.
+// written from fp32 values with one rounding.  Beside the list, where there is a rest, dl/dz is (A_in p_rest - r) 2^(z c - lse_rest): with the
+// rest's own log-sum-exp both factors stay in a float's range, also where p_v and p_rest (by themselves) are far below it.
 #pragma once
 #include "kd_common.hpp"
 #include "kd_logit_math.hpp"
@@ -41,7 +42,8 @@ struct HeadArgs {
   float* z;
   float* kept;             // all logits, in the order of dz_chunk, where there are few enough (null otherwise)
   // gradient
-  const f32x4* rowinfo;    // [T_pad]: {log-sum-exp (base 2), A_out, U, A_in}
+  const f32x4* rowinfo;    // [T_pad]: {log-sum-exp (base 2), factor beside the list, U if there is label smoothing, else the logarithm (base 2) that
+                           // goes with that factor: the log-sum-exp beside the list, if the teacher has a rest, or of all logits; A_in}
   bf16_t* dz;
   int ldz, sets;
 };
@@ -341,16 +343,16 @@ __device__ __forceinline__ void store_dz(float (&x)[8], bf16_t* to, int64_t stri
   }
 }
 // (a token of zeros beside infinite weights: 0 x infinity is NaN, and the larger of that and a number the number.  A token that counts
-// keeps its NaN through A_out.)
-__device__ __forceinline__ float unlisted_dz(const f32x4& ri, float z, float c, float u) {
-  return fmaf(ri[1], fexp2(fmaxf(fmaf(z, c, -ri[0]), -1.0e38f)), u);
+// keeps its NaN through the factor.)
+__device__ __forceinline__ float unlisted_dz(float factor, float base, float z, float c, float u) {
+  return fmaf(factor, fexp2(fmaxf(fmaf(z, c, -base), -1.0e38f)), -u);
 }
 
-__device__ __forceinline__ float listed_dz(const f32x4& ri, float z, float c, float q) {
-  return fmaf(ri[3], fexp2(fmaxf(fmaf(z, c, -ri[0]), -1.0e38f)), -q) - ri[2];
+__device__ __forceinline__ float listed_dz(const f32x4& ri, float z, float c, float q, float u) {
+  return fmaf(ri[3], fexp2(fmaxf(fmaf(z, c, -ri[0]), -1.0e38f)), -q) - u;
 }
 
-// dL/dz of a tile, without its common factor (Targets::scale): A_out p - U, in bf16 (PARTS 1), or as three bf16 parts that hold 24 bits,
+// dL/dz of a tile beside the lists, without its common factor (Targets::scale), in bf16 (PARTS 1), or as three bf16 parts that hold 24 bits,
 // each in the copies of the token axis that multiply it (`sets`: 3, parts 0 1 2; 6, parts 0 0 0 1 1 2).  What is listed is written over
 // by head_listed_kernel.  Rows that do not exist give 0; panels of 64 tokens without a valid one are left out.
 template <bool SMOOTH, int PARTS>
@@ -382,7 +384,7 @@ struct HeadGradEpi {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float z = T[16 * p + 8 * u + e];
-          x[e] = unlisted_dz(ri, z, a.c, SMOOTH ? (counts_in(z) ? -ri[2] : 0.f) : 0.f);
+          x[e] = SMOOTH ? unlisted_dz(ri[1], ri[0], z, a.c, counts_in(z) ? ri[2] : 0.f) : unlisted_dz(ri[1], ri[2], z, a.c, 0.f);
         }
         store_dz<PARTS>(x, a.dz + dz_chunk(a.ldz, panel, (m0 >> 5) + 2 * p + u, j, geo.lane), (int64_t)panels * 64 * a.ldz, a.sets);
       }
