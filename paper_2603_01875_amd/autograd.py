@@ -40,6 +40,13 @@ def kd_loss(h_s, W_s, h_t, W_t, mask=None, tau=1.0, kind=K.FKL, beta=0.5, w_layo
                            int(flags), float(teacher_scale), workspace, float(loss_scale))
 
 
+def _scaled(x, g):
+    """x times the scalar tensor g, in fp32 with one rounding to x's type.  (g rounded to bf16 first would shift all of a gradient the
+    same way, and torch rounds a scalar tensor on the device to the other operand's type.  One pass, of [151936, 1024] in bf16
+    141 us; 120 with g rounded.)"""
+    return None if x is None else torch.mul(x, g.reshape(1), out=torch.empty_like(x))
+
+
 class _HeadLossFn(torch.autograd.Function):
     """A one-head loss: `call(want_grad_h, want_grad_W)` gives the dict of a *_fwd_bwd call.  Only the gradients that are asked
     for are computed."""
@@ -53,7 +60,7 @@ class _HeadLossFn(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g):
-        return tuple(None if x is None else x * g.to(x.dtype) for x in ctx.saved_tensors) + (None, None)
+        return tuple(_scaled(x, g) for x in ctx.saved_tensors) + (None, None)
 
 
 def cross_entropy(h, W, labels, mask=None, label_smoothing=0.0, z_loss=0.0, w_layout=K.W_VH, workspace=None,

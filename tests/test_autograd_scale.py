@@ -1,0 +1,61 @@
+"""What the autograd front ends do with the factor that comes in from behind the loss: it is an fp32 number, and a gradient in bf16
+is rounded once, after the product."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_01875_amd import autograd as A
+from paper_2603_01875_amd import kdloss as K
+
+FACTORS = [0.3, -1.7, 1 / 3, 1e-4, 1.0]
+
+
+def _tensors(device="cpu", T=70, H=128, V=1000, dtype=torch.bfloat16):
+    g = torch.Generator().manual_seed(5)
+    return [(torch.randn(n, H, generator=g) * s).to(dtype).to(device).requires_grad_(True) for n, s in ((T, 1.0), (V, 0.05))]
+
+
+def _check(got, stored, factor):
+    want = stored.double() * float(np.float32(factor))
+    once = want.float().to(stored.dtype)                   # (the product of a bf16 and an fp32 number has 32 bits: fp32, then bf16)
+    assert got.dtype == stored.dtype
+    step = torch.finfo(stored.dtype).eps / 2
+    assert ((got.double() - want).abs() <= step * want.abs() * 1.0001 + 1e-38).all()
+    assert (got == once).double().mean() > 0.999
+    # no common shift: what the roundings leave is of both signs
+    if want.abs().sum() > 0:
+        assert abs(float((got.double() - want).sum() / want.abs().sum())) < 0.05 * step or factor == 1.0
+
+
+@pytest.mark.parametrize("factor", FACTORS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_one_head_losses_multiply_once_rounded(factor, dtype):
+    h, W = _tensors(dtype=dtype)
+    grads = dict(grad_h=h.detach() * 0.7, grad_W=W.detach() * 0.9, loss=torch.ones(1))
+    loss = A._HeadLossFn.apply(h, W, lambda gh, gW: grads, ("grad_h", "grad_W"))
+    (factor * loss).backward()
+    _check(h.grad, grads["grad_h"], factor)
+    _check(W.grad, grads["grad_W"], factor)
+    only = A._HeadLossFn.apply(h.detach(), W, lambda gh, gW: dict(grads, grad_h=None), ("grad_h", "grad_W"))
+    assert torch.equal(torch.autograd.grad(factor * only, W)[0], W.grad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("factor", [0.3, 1 / 3])
+@pytest.mark.parametrize("T", [70, 300])
+def test_one_head_losses_on_the_gpu(factor, T):
+    """A factor behind the loss against the stored gradients, and against the same factor in front of it (loss_scale, which the
+    library multiplies in fp32 in front of its only rounding): each is one rounding away from the same numbers, to fp32."""
+    h, W = _tensors("cuda", T=T)
+    y = torch.arange(T, device="cuda") * 3
+    ids, a = torch.arange(5, device="cuda").repeat(T, 1), torch.randn(T, 5, device="cuda")
+    calls = [lambda s=1.0: A.cross_entropy(h, W, y, loss_scale=s), lambda s=1.0: A.topk_loss(h, W, a, ids, loss_scale=s)]
+    raw = [K.kd_ce_fwd_bwd(h.detach(), W.detach(), y), K.kd_topk_fwd_bwd(a, ids, h.detach(), W.detach())]
+    for call, out in zip(calls, raw):
+        got = torch.autograd.grad(factor * call(), (h, W))
+        front = torch.autograd.grad(call(factor), (h, W))
+        for g, f, stored in zip(got, front, (out.get("grad_h", out.get("grad_h_s")), out.get("grad_W", out.get("grad_W_s")))):
+            _check(g.cpu(), stored.cpu(), factor)
+            g, f = g.double(), f.double()
+            assert ((g - f).abs() <= 3 * 2.0 ** -8 * f.abs() * 1.01 + 1e-38).all()     # three roundings lie between them
+            assert abs(float((g.abs().sum() - f.abs().sum()) / f.abs().sum())) < 2.0 ** -12
