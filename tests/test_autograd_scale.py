@@ -59,3 +59,37 @@ def test_one_head_losses_on_the_gpu(factor, T):
             g, f = g.double(), f.double()
             assert ((g - f).abs() <= 3 * 2.0 ** -8 * f.abs() * 1.01 + 1e-38).all()     # three roundings lie between them
             assert abs(float((g.abs().sum() - f.abs().sum()) / f.abs().sum())) < 2.0 ** -12
+
+
+@pytest.mark.parametrize("factor", FACTORS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_two_model_loss_multiplies_once_rounded(factor, dtype, monkeypatch):
+    h, W = _tensors(dtype=dtype)
+    grads = dict(grad_h_s=h.detach() * 0.7, grad_W_s=W.detach() * 0.9, loss=torch.ones(1))
+    monkeypatch.setattr(K, "kd_loss_fwd_bwd", lambda *a, **k: grads)
+    (factor * A.kd_loss(h, W, h.detach(), W.detach())).backward()
+    _check(h.grad, grads["grad_h_s"], factor)
+    _check(W.grad, grads["grad_W_s"], factor)
+
+
+@pytest.mark.gpu
+def test_two_model_loss_on_the_gpu():
+    h, W = _tensors("cuda")
+    h_t, W_t = (x.detach() for x in _tensors("cuda", H=192))
+    out = K.kd_loss_fwd_bwd(h_t, W_t, h.detach(), W.detach())
+    for factor in (0.3, 1 / 3, 1.0):
+        got = torch.autograd.grad(factor * A.kd_loss(h, W, h_t, W_t), (h, W))
+        _check(got[0].cpu(), out["grad_h_s"].cpu(), factor)
+        _check(got[1].cpu(), out["grad_W_s"].cpu(), factor)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_two_model_loss_gradients_know_the_factor_in_a_graph_of_the_backward_pass(dtype, monkeypatch):
+    h, W = _tensors(dtype=dtype)
+    grads = dict(grad_h_s=h.detach() * 0.7, grad_W_s=W.detach() * 0.9, loss=torch.ones(1))
+    monkeypatch.setattr(K, "kd_loss_fwd_bwd", lambda *a, **k: grads)
+    w = torch.tensor(0.3, requires_grad=True)
+    got = torch.autograd.grad(w * A.kd_loss(h, W, h.detach(), W.detach()), (h, W), create_graph=True)
+    _check(got[0].detach(), grads["grad_h_s"], 0.3)
+    slope, = torch.autograd.grad(got[0].sum(), w)
+    assert float(slope) == pytest.approx(float(grads["grad_h_s"].double().sum()), rel=1e-2, abs=1e-2)
