@@ -153,6 +153,7 @@ __global__ __launch_bounds__(256) void top_targets_kernel(const TargetArgs a) {
   info[0] = any_bad || held != held ? __builtin_nan("") : held + rest;
   info[1] = rest;
   info[2] = ent + (rest > 0.0 ? rest * log(rest) : 0.0);
+  info[3] = held;
   const bool counts_ = (n > 0 || any_bad) && (!a.t.mask || a.t.mask[t]);
   a.t.valid[t] = counts_;
   keep_places(a, t, counts_);
@@ -232,7 +233,8 @@ struct HeadCombineArgs {
   const int* meta;
   const int *rowmap, *inv;
   int T, T_pad, nv, K, n_parts;        // n_parts: 0 = the device's plan
-  float c, uniform, z_loss;            // uniform: U
+  float c, z_loss;
+  double uniform;                      // U
   const int* list;
   const float* q;
   const float* z;
@@ -314,7 +316,7 @@ __device__ __forceinline__ void sum_losses(const LossSumArgs& a, double* sums) {
 
 // Merges a token's partial sums and its listed logits: lse, and with it the loss and the coefficients of dL/dz (kd_head.hpp).  Bound by
 // latency (T = 4096 22 us with packing h beside it, T = 100 with 256 partial sums a token 11 us).  Logarithms in base 2; what is a
-// difference of large quantities in double.
+// difference of large quantities in double (but for label smoothing's sum of all logits, which is an fp32 sum of V of them).
 template <int TX, int NT>
 __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs a) {
   constexpr int BYTES = sizeof(float) * 64 * 65;
@@ -324,7 +326,7 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
     return;
   }
   float* const lds = (float*)shared;
-  static_assert(NT / 64 * 5 * TX * 4 <= BYTES && NT * 8 <= BYTES, "the merges' and the sum's share");
+  static_assert(NT / 64 * 4 * TX * 4 <= BYTES && NT * 8 <= BYTES, "the merges' and the sum's share");
   const int t = blockIdx.x * TX + threadIdx.x % TX, g = threadIdx.x / TX, G = NT / TX;
   const int n_valid = a.meta[META_N_VALID], n_parts = a.n_parts ? a.n_parts : a.meta[META_N_SPLIT];
   const int64_t token = a.rowmap[t];
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
     for (int p = g; p < n_parts; p += G) m[0] = fmaxf(m[0], q0[p * stride]);
     for (int k = g; k < a.K && list[k] != kNoEntry; k += G) m[1] = fmaxf(m[1], z(k) * a.c);
     merge_parts<TX, NT, 2, MergeMax>(m, lds);
-    float v[5] = {0.f, 0.f, 0.f, 0.f, 0.f};            // sum beside the list, on it, sum of logits, sum q (z - max), sum q
+    float v[4] = {0.f, 0.f, 0.f, 0.f};                 // sum beside the list, on it, sum of logits, sum q (z - max)
 #pragma unroll 4
     for (int p = g; p < n_parts; p += G) {
       const float* const q = q0 + p * stride;
@@ -364,19 +366,20 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
       v[1] += fexp2(d);
       if (a.nv == 3) v[2] += zk;
       if (prob[k] != 0.f) v[3] = fmaf(prob[k], d, v[3]);        // (0 log 0 = 0: a logit of minus infinity)
-      v[4] += prob[k];
     }
-    merge_parts<TX, NT, 5, MergeSum>(v, lds);
+    merge_parts<TX, NT, 4, MergeSum>(v, lds);
     if (g == 0 && counts) {
       const double ln2 = 0.6931471805599453;
       const double* const info = a.info + token * kTargetInfo;
-      const double mass = info[0], rest = info[1], ent = info[2];
+      const double mass = info[0], rest = info[1], ent = info[2], held = info[3];
       const double lo = v[0] == 0.f ? -INFINITY : (double)m[0] + log2((double)v[0]);     // beside the list
       const double ll = v[1] == 0.f ? -INFINITY : (double)m[1] + log2((double)v[1]);
       const double big = fmax(lo, ll), lse = v[0] != v[0] || v[1] != v[1] ? __builtin_nan("") : big + log2(exp2(lo - big) + exp2(ll - big));
       const double nat = lse * ln2;
-      const double on = v[4] != 0.f ? (double)v[3] + (double)m[1] * (double)v[4] : 0.0;   // sum q z in base 2
-      double loss = ent + mass * nat - ln2 * on - (a.nv == 3 ? (double)a.uniform * (double)v[2] : 0.0) + (double)a.z_loss * nat * nat;
+      // sum q z in base 2.  (The list's mass in double, as in `mass`: what the logits have in common is to cancel.  As an fp32 sum it left 1e-7 of
+      // the largest logit over tau.)
+      const double on = held != 0.0 ? (double)v[3] + (double)m[1] * held : 0.0;
+      double loss = ent + mass * nat - ln2 * on - (a.nv == 3 ? a.uniform * (double)v[2] : 0.0) + (double)a.z_loss * nat * nat;
       const double in = mass + 2.0 * (double)a.z_loss * nat;
       double out = in, base = lse;
       if (rest > 0.0) {
@@ -386,7 +389,7 @@ __global__ __launch_bounds__(NT) void head_combine_kernel(const HeadCombineArgs 
       }
       // (a logarithm as a float is up to 1e-6 off, the same way for all of a token's entries: that goes into the factors)
       const float high = (float)lse, high_out = (float)base;
-      a.rowinfo[t] = f32x4{high, (float)(out * exp2((double)high_out - base)), a.nv == 3 ? a.uniform : high_out,
+      a.rowinfo[t] = f32x4{high, (float)(out * exp2((double)high_out - base)), a.nv == 3 ? (float)a.uniform : high_out,
                            (float)(in * exp2((double)high - lse))};
       a.row_loss[t] = (float)loss;
       if (a.per_token) a.per_token[token] = a.weight * (float)loss;
@@ -417,7 +420,7 @@ hipError_t launch_head_combine(const HeadProblem& h, bool backward, bool pack_h,
   // two launches)
   const bool all = p.T <= 32, many = !all && ((h.few ? h.parts : p.n_split) >= 128 || h.t.K >= 128);
   HeadCombineArgs a{p.partials, p.meta, p.rowmap, p.inv, p.T, p.T_pad, h.t.smoothing > 0.f ? 3 : 2, h.t.K, h.few ? h.parts : 0,
-                    1.4426950408889634f / p.tau, h.t.smoothing / (float)p.V, h.t.z_loss, h.t.list, h.t.q, h.t.z, h.kept, p.V_c, h.t.info,
+                    1.4426950408889634f / p.tau, h.t.z_loss, (double)h.t.smoothing / p.V, h.t.list, h.t.q, h.t.z, h.kept, p.V_c, h.t.info,
                     (f32x4*)p.rowinfo, p.row_loss, p.out_weight, p.per_token_loss, all ? 1 : many ? p.T_pad / 8 : p.T_pad / 32,
                     loss_sum_args(h), {}};
   int64_t groups = a.groups;

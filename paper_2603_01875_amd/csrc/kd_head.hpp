@@ -90,6 +90,7 @@ __device__ __forceinline__ int label_target(const TargetArgs& a, int t) {
   double* const info = a.t.info + (int64_t)t * kTargetInfo;
   info[0] = out ? __builtin_nan("") : 1.0;
   info[1] = info[2] = 0.0;
+  info[3] = out ? 0.0 : 1.0 - (double)a.t.smoothing;
   return row;
 }
 TargetArgs target_args(const HeadProblem& h);  // kd_head.hip

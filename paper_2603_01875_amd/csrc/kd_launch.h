@@ -109,7 +109,7 @@ struct Targets {
   float* scale;            // loss_scale tau^2 / (n tau), what both gradients are multiplied by
 };
 constexpr int kNoEntry = 0x7fffffff;
-constexpr int kTargetInfo = 3;         // mass (of the list and of what stands for the rest), mass of the rest, sum q log q over both
+constexpr int kTargetInfo = 4;         // mass (of the list and of what stands for the rest), mass of the rest, sum q log q over both, mass of the list alone
 constexpr int kHeadRows = 256;         // vocabulary rows per tile
 // few: at most kFewHeadTokens tokens and [V][K] rows of whole k-steps, the head streams past tokens in LDS (kd_head_few.hip); kept: the logits are
 // kept in fp32, in dz's order, and turned into dz without multiplying again
