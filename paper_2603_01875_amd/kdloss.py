@@ -165,8 +165,12 @@ def quantize_e4m3(x, scale, out=None):
 def kd_loss_workspace_size(params) -> int:
     """Workspace bytes of a call with this parameter block (KdLossParams, KdCeParams or KdTopkParams)."""
     n = ctypes.c_size_t(0)
-    query = {KdLossParams: lib().kd_loss_workspace_size, KdCeParams: lib().kd_ce_workspace_size,
-             KdTopkParams: lib().kd_topk_workspace_size}[type(params)]
+    for block, query in ((KdLossParams, lib().kd_loss_workspace_size), (KdCeParams, lib().kd_ce_workspace_size),
+                         (KdTopkParams, lib().kd_topk_workspace_size)):
+        if isinstance(params, block):
+            break
+    else:
+        raise TypeError(f"params must be a KdLossParams, KdCeParams or KdTopkParams, got {type(params).__name__}")
     st = query(ctypes.byref(params), ctypes.byref(n))
     if st != KD_OK:
         raise KdLossError(st)
