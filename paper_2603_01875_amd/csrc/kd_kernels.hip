@@ -516,7 +516,7 @@ __device__ __forceinline__ void prepare(int block, int tid, const void* src, int
   const int k0 = (by * 64 + (tid & 63)) * 8;
   if (k0 >= K) return;
   const int place = src_f32 ? k0 / H : 0, col = k0 - place * H;      // H is a multiple of 8: eight values of one part
-  const int part = src_f32 == 2 ? part_of_six(place < 6 ? place : 0, split_mode == 1) : (split_mode == 1 && place == 2) || (split_mode == 2 && place == 1);
+  const int part = src_f32 == 2 ? part_of_six(place < 6 ? place : 0, false) : (split_mode == 1 && place == 2) || (split_mode == 2 && place == 1);
   const bool pad = src_f32 ? place > (src_f32 == 2 ? 5 : 2) : k0 >= H;
   const int n = rowmap ? meta[META_N_VALID] : R;
 #pragma unroll
@@ -838,7 +838,7 @@ hipError_t launch_operands(const Problem& p, bool rowmap, bool student, bool tea
   };
   auto head = [&](const void* src, int H, void* dst, int K) {
     OperandJob j{};
-    j.src = src; j.dst = (bf16_t*)dst; j.src_f32 = p.in_f32 ? (p.f32_parts ? 2 : 1) : 0;
+    j.src = src; j.dst = (bf16_t*)dst; j.src_f32 = p.in_f32;      // (fp32 heads of the one-head losses: launch_head_split)
     j.R = p.V; j.H = H; j.K = K; j.mode = 1;
     add(false, j, (int64_t)((j.R + 15) / 16) * ((j.K + 511) / 512));
   };
