@@ -241,8 +241,8 @@ kd_status kd_loss_fwd_bwd_multi(const kd_loss_params* params, int n_teachers,
  * (kd_ce_*), and the divergence from a teacher of which only the largest logits were kept (kd_topk_*).  Same
  * conventions as above: plain C ABI, every buffer the caller's, no allocation, no synchronisation, only kernels
  * enqueued, nothing kept from call to call, results bitwise reproducible, all checks on the host before anything is
- * enqueued.  z = h W, logits produced tile by tile (twice with gradients), never stored; tokens that do not count are
- * compacted away.
+ * enqueued.  z = h W, logits produced tile by tile, and again for the gradients; where they are few (at most 160 MiB in
+ * fp32), a call with gradients keeps them in its workspace instead.  Tokens that do not count are compacted away.
  *
  *  h       [T, H] device, in_dtype;  W: head in the order w_layout, in_dtype
  *  mask    [T] uint8 device, non-zero = token may count; NULL = every token may
@@ -250,7 +250,9 @@ kd_status kd_loss_fwd_bwd_multi(const kd_loss_params* params, int n_teachers,
  *  per_token_loss  device, [T] floats (0 for tokens that do not count) or NULL
  *  grad_h [T, H], grad_W (order of W) device, grad_dtype; either may be NULL and is then not computed.  Rows of grad_h
  *          of tokens that do not count are exactly 0; grad_W is overwritten, or added to with accumulate_grad_W
- *  workspace  device, 256-byte aligned, workspace_bytes >= the size query
+ *  workspace  device, 256-byte aligned, workspace_bytes >= the size query for these parameters (one token more may need
+ *          less: T = 256, H = 1024, V = 151936 keeps its logits and takes 268 MB, T = 257 takes 192; a program whose T
+ *          varies asks for each size and takes the largest)
  * h, W, grad_h, grad_W must be 16-byte aligned, the other arrays to their elements.  Inputs must not alias outputs or
  * the workspace.
  *
@@ -258,7 +260,7 @@ kd_status kd_loss_fwd_bwd_multi(const kd_loss_params* params, int n_teachers,
  * products in which dL/dz is held in three parts: fp32 results are as exact as fp32 arithmetic gives them.  (Infinite
  * weights need bf16 operands, where a logit of minus infinity is a row of probability 0; the parts of fp32 ones give NaN.)  For bf16
  * gradients dL/dz is rounded to bf16 once, without the factor loss_scale / n that all its entries share, and the sums
- * once more. */
+ * once more; of fp32 operands the products for bf16 gradients take h and W rounded to bf16 as well (losses do not). */
 
 /* Type of labels and of vocabulary rows. */
 typedef enum { KD_I32 = 0, KD_I64 = 1 } kd_index_dtype;

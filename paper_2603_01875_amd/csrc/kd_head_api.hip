@@ -17,9 +17,13 @@ using kd::aligned16;
 using kd::round_up;
 
 // Most bytes of logits that a call with gradients keeps in its workspace, in fp32, instead of making them twice.  What they cost is a store
-// and a load of 4 bytes, what they save is 2 H flop and the head's second reading.  All kept against none, us a call: T = 128, H = 1024,
-// V = 151936 (78 MB) 292 / 400; T = 200, H = 2048, V = 151936 (155 MB) 614 / 778; T = 500, H = 1024, V = 50264 (103 MB) 281 / 302.  Of
-// more the workspace would be several times what dL/dz takes.
+// and a load of 4 bytes, what they save is 2 H flop and the head's second reading.  All kept against none, us a call, bf16:
+//   within the limit     T = 128, H = 1024, V = 151936 (78 MB) 285 / 380; T = 200, H = 2048, V = 151936 (156 MB) 570 / 734; T = 500,
+//                        H = 1024, V = 50264 (103 MB) 266 / 276, H = 4096 677 / 825
+//   beyond it            T = 256, V = 200000 (205 MB) H = 1024 509 / 540, H = 4096 1334 / 1719; T = 800, V = 100000 (410 MB, the most that one
+//                        chunk has) H = 1024 686 / 724, H = 4096 1999 / 2481; T = 500, H = 1024, V = 151936, fp32 gradients (311 MB) 1151 / 1195
+// so keeping them pays wherever the vocabulary is one chunk (3 to 8 % with H = 1024, 17 to 30 % with 4096, more with few tokens): the limit is
+// there for the workspace alone, which would be 2 to 3 times as large (T = 256, H = 4096, V = 400000 686 MB for 276).
 constexpr int64_t kKept = 160ll << 20;
 
 // Most bytes of grad_h's partial sums for which the products of its parts get sums of their own, in one launch (one launch a product, each
@@ -94,7 +98,8 @@ void plan(const Call& c, HeadProblem& h, HeadLayout& L, bool backward) {
   q.f32_parts = 1;
   q.w_hv = c.w_layout == KD_W_HV;
   q.head_rows = kd::kHeadRows;
-  // fp32 gradients are exact to fp32: dL/dz is held as three bf16 parts, h and W, if they are fp32, as well
+  // fp32 gradients are exact to fp32: dL/dz is held as three bf16 parts, h and W, if they are fp32, as well.  bf16 gradients of fp32 operands:
+  // one product of first parts, each factor rounded to bf16 as the result is
   q.dz_sets = !q.grad_f32 ? 1 : q.in_f32 ? 6 : 3;
   q.K_s = (int)round_up(q.in_f32 ? 6 * c.H : c.H, 64);
   q.prep_hs = 1;                                       // (the strip loop reads packed tokens)
