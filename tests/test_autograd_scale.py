@@ -93,3 +93,27 @@ def test_two_model_loss_gradients_know_the_factor_in_a_graph_of_the_backward_pas
     _check(got[0].detach(), grads["grad_h_s"], 0.3)
     slope, = torch.autograd.grad(got[0].sum(), w)
     assert float(slope) == pytest.approx(float(grads["grad_h_s"].double().sum()), rel=1e-2, abs=1e-2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [70, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_type_that_gradients_are_computed_in(T, dtype):
+    """grad_dtype=F32: a bf16 leaf gets the fp32 gradient (head_util's bounds for it), rounded once."""
+    from oracle import head_oracle as O
+    from tests import head_util as U
+    h, W, y, rng = U.make(T, T, 64, 1000, dtype)
+    a, ids = U.top_lists(rng, T, 1000, 6, y)
+    n64, factor = (U.np64(h), U.np64(W)), float(np.float32(0.3))
+    hd, Wd = (x.requires_grad_(True) for x in U.device(h, W))
+    for loss, ref in ((A.cross_entropy(hd, Wd, y.cuda(), grad_dtype=K.F32), O.cross_entropy(*n64, y.numpy())),
+                      (A.topk_loss(hd, Wd, a.cuda(), ids.cuda(), grad_dtype=K.F32), O.topk(U.np64(a), ids.numpy(), *n64))):
+        b = U.bounds(*n64, ref, 1.0, dtype, "f32")
+        for g, k in zip(torch.autograd.grad(factor * loss, (hd, Wd)), ("grad_h", "grad_W")):
+            assert g.dtype == hd.dtype
+            last = U.BF16 * 1.001 if dtype == "bf16" else U.F32
+            want, bound = factor * ref[k], factor * b[k] * 1.01
+            assert (np.abs(U.np64(g) - want) <= bound + last * (np.abs(want) + bound)).all()
+    bf = torch.autograd.grad(A.cross_entropy(hd, Wd, y.cuda(), grad_dtype=K.BF16), Wd)[0]      # (of fp32 operands, too)
+    raw = K.kd_ce_fwd_bwd(hd.detach(), Wd.detach(), y.cuda(), grad_dtype=K.BF16)["grad_W"]
+    assert bf.dtype == Wd.dtype and torch.equal(bf, raw.to(Wd.dtype))
