@@ -72,8 +72,8 @@ def cross_entropy(h, W, labels, mask=None, label_smoothing=0.0, z_loss=0.0, w_la
     """Cross entropy of `labels` (negative: ignored) under softmax(h W) as a scalar tensor, the mean over the tokens that
     count; gradients flow to h and W.  Arguments as in kdloss.kd_ce_fwd_bwd; loss_scale as in kd_loss.  Where no gradient is
     asked for, none is computed.  grad_dtype=kdloss.F32 with bf16 h and W: what the library computes and keeps for backward() is
-    fp32, and the gradients are rounded to bf16 once, by backward(); by default dL/dz is rounded to bf16 as well, in a third to
-    two thirds of the time.  (A workspace that is given has to be one for the same grad_dtype.)"""
+    fp32, and the gradients are rounded to bf16 once, by backward(); by default dL/dz is rounded to bf16 as well, in half the
+    time (T = 4096, H = 1024, V = 151936 4.2 ms, 9.0 in fp32).  (A workspace that is given has to be one for the same grad_dtype.)"""
     kw = dict(label_smoothing=float(label_smoothing), z_loss=float(z_loss), w_layout=int(w_layout), workspace=workspace,
               loss_scale=float(loss_scale))
     if not (torch.is_grad_enabled() and (h.requires_grad or W.requires_grad)):

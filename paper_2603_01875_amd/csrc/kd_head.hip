@@ -503,7 +503,7 @@ __global__ __launch_bounds__(256) void head_listed_kernel(const ListedArgs a) {
 }
 
 // All of it from kept logits (the whole vocabulary is one chunk).  A workgroup makes 256 columns of a panel of 64 tokens, 4 KiB of
-// each 32; bound by memory, 6 bytes a logit (T = 200, V = 151936: 35 us, 6.5 TB/s with what the last-level cache still holds).  Which of
+// each 32; bound by memory, 6 bytes a logit (T = 200, three panels that count, V = 151936: 34 us, 5.1 TB/s).  Which of
 // them are listed stands in LDS, a word per token and 32 columns.  With long lists by the latency of their marking and of loading
 // their probabilities (T = 1909, V = 5424, K = 202: 29 us for 60 MB; one entry at a time 62 us).
 struct KeptArgs {

@@ -414,10 +414,10 @@ struct HeadDrive {
 HeadArgs head_args(const HeadProblem& h);      // kd_head.hip
 
 // Statistics: per token max and sum of e^(z/tau) beside the list, and sum z.  A workgroup has one token tile and a range of the vocabulary,
-// so that a token's running sums stay in its LDS and partial sums leave once a range.  Bound by the matrix pipe (T = 4096, 3584 computed,
-// H = 1024, V = 151936: 876 us, 1.27 PFLOP/s; with lists of 64 1019 us, of which the difference is taking their logits out, one listed row
-// of a lane at a time), with one token tile by memory as much (T = 200, H = 2048, V = 151936: 169 us, 3.7 TB/s and 0.94 PFLOP/s on the whole
-// tile; 225 us where it stores the logits).
+// so that a token's running sums stay in its LDS and partial sums leave once a range.  Bound by the matrix pipe (T = 4096, 15 tiles computed,
+// H = 1024, V = 151936: 866 us, 1.38 PFLOP/s beside 2.3 TB/s; with lists of 64 1004 us, of which the difference is taking their logits out,
+// one listed row of a lane at a time), with one token tile by memory as much (T = 200, H = 2048, V = 151936, storing the logits: 206 us, 649 MB
+// read and 156 written, 3.9 TB/s, and 0.77 PFLOP/s on the whole tile).
 template <bool HV, bool SMOOTH, bool KEPT>
 KD_STRIP_KERNEL void head_stats_kernel(const HeadArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -429,7 +429,7 @@ KD_STRIP_KERNEL void head_stats_kernel(const HeadArgs a) {
 }
 
 // dL/dz of a chunk: the logits again, four token tiles by all of the chunk's rows at a time, so that the head's come from L2.  Bound by the
-// matrix pipe, and by a tile's stores, for which its one wave per SIMD waits (the same size: 1058 us in five chunks, 1.05 PFLOP/s).
+// matrix pipe, and by a tile's stores, for which its one wave per SIMD waits (the same size: 1048 us in five chunks, 1.15 PFLOP/s).
 template <bool HV, bool SMOOTH, int PARTS>
 KD_STRIP_KERNEL void head_grad_kernel(const HeadArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
