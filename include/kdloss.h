@@ -330,6 +330,131 @@ kd_status kd_topk_fwd(const kd_topk_params* params, const void* top_logits, cons
                       const void* h_s, const void* W_s, const uint8_t* mask, float* loss, float* per_token_loss,
                       void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Beside the losses: what a distillation program calls in front of them and behind them.
+ *
+ * A linear layer in e4m3 with a scale per block of 128 (teacher layers as they are stored for FP8 inference, or a student trained
+ * in FP8), the top logits of a teacher as kd_topk_* reads them, tokens sampled from a student's logits, and the norm of all
+ * gradients with clipping.  Same conventions as above: plain C ABI, every buffer the caller's, no allocation, no synchronisation,
+ * only kernels enqueued, nothing kept from call to call, results bitwise reproducible, all checks on the host before anything is
+ * enqueued.  Inputs must not alias outputs or the workspace, unless it is said. */
+
+/* Blocks of a matrix [rows, cols] that share a scale: 1 x 128 (of a row) or 128 x 128; the last ones of a row or column may be
+ * narrower.  Codes are OCP e4m3 bytes in rows of cols rounded up to a multiple of 16, zero behind the row's end; scales are
+ * [rows, ceil(cols / 128)] or [ceil(rows / 128), ceil(cols / 128)] floats.  A block stands for codes times scale. */
+typedef enum { KD_BLOCK_ROW = 0, KD_BLOCK_TILE = 1 } kd_block;
+
+typedef struct {
+  int64_t rows, cols;         /* 1 .. 2^24, 1 .. 2^22 (2^22 both with a transposed result)       */
+  int64_t ld;                 /* elements from row to row of src, >= cols                        */
+  int32_t src_dtype;          /* kd_dtype of src                                                 */
+  int32_t block;              /* kd_block                                                        */
+  int32_t reserved[2];        /* must be 0                                                       */
+} kd_blocks_params;
+
+/* Quantises a matrix in blocks:  scale = m / 448 with m = max(largest |src| of the block, 448 2^-126), code = e4m3(448 src / m), the
+ * quotient rounded once in fp32, then to nearest even.  A block that holds an infinity or a NaN has the scale NaN.
+ * codes, scales: of src.  codes_t, scales_t: of its transpose [cols, rows] (KD_BLOCK_ROW: blocks along src's columns, with scales of
+ * their own; KD_BLOCK_TILE: the same codes and scales).  Either pair may be NULL; src is read once for both.
+ * src: aligned to its elements, codes to 16 bytes, scales to 4. */
+kd_status kd_quantize_e4m3_blocks(const kd_blocks_params* params, const void* src, uint8_t* codes, float* scales, uint8_t* codes_t,
+                                  float* scales_t, void* hip_stream);
+
+/* Product of two matrices in blocks:
+ *   out[m, n] = sum over blocks j of 128 columns  a_scale[m, j] b_scale[n or n / 128, j] sum_{k in j} a[m, k] b[n, k]
+ * (the scaled blocks are summed in fp32, in an order that depends on the sizes alone.  A block's own products: for an fp32 result in
+ * fp32, on the bf16 matrix pipe; for a bf16 result on the e4m3 pipe at twice the rate, which cuts products off at 2^-13 of the largest of their
+ * group of eight: 1.5e-5 of a result of normal numbers, whose rounding to bf16 is 1.7e-3).
+ * A linear layer y = x W^T is a = x, b = W; its gradients are grad_x: a = grad_y, b = W's transpose, grad_W: a = grad_y's transpose,
+ * b = x's transpose. */
+typedef struct {
+  int64_t M, N, K;            /* a [M, K], b [N, K], out [M, N]; M, N 1 .. 2^24, K 1 .. 2^22     */
+  int32_t in_dtype;           /* kd_linear_e4m3: kd_dtype of x                                   */
+  int32_t out_dtype;          /* kd_dtype of out                                                 */
+  int32_t b_block;            /* kd_block of b (a: KD_BLOCK_ROW); kd_linear_e4m3: KD_BLOCK_TILE   */
+  int32_t accumulate;         /* 0: out is overwritten.  1: added to, in front of the rounding   */
+  int32_t reserved[2];        /* must be 0                                                       */
+} kd_linear_params;
+
+/* Bytes of device workspace (256-byte aligned) that either call below needs for these parameters (in_dtype is read here as well). */
+kd_status kd_linear_workspace_size(const kd_linear_params* params, size_t* bytes);
+/* a, b: codes, 16-byte aligned; scales, out: aligned to their elements. */
+kd_status kd_matmul_e4m3(const kd_linear_params* params, const uint8_t* a, const float* a_scales, const uint8_t* b, const float* b_scales,
+                         void* out, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* out = x W^T with x [M, K] in in_dtype (row-major, aligned to its elements), quantised in the call (KD_BLOCK_ROW). */
+kd_status kd_linear_e4m3(const kd_linear_params* params, const void* x, const uint8_t* w, const float* w_scales, void* out,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The K largest logits of each row, as kd_topk_* takes them, in descending order, of equal ones the lower index first:
+ *   top_logits [T, K] in the logits' type, top_index [T, K], lse [T] = log sum_v exp(logits[t, v] / tau) (may be NULL)
+ * A logit of minus infinity is no entry: where a row has fewer than K others, the list ends with entries of index -1 and logit minus
+ * infinity.  A NaN counts as larger than every number; the row's lse is then NaN (infinite where the row's largest logit is).  An empty row's lse is minus
+ * infinity. */
+typedef struct {
+  int64_t T, V;               /* rows, entries of a row: 1 .. 2^22, 1 .. 2^24                    */
+  int64_t ld;                 /* elements from row to row of logits, >= V                        */
+  int32_t K;                  /* 1 .. KD_TOPK_MAX, at most V                                     */
+  int32_t in_dtype;           /* kd_dtype of logits and top_logits                               */
+  int32_t index_dtype;        /* kd_index_dtype of top_index                                     */
+  float tau;                  /* 1e-6 <= tau <= 1e6                                              */
+  int32_t reserved[2];        /* must be 0                                                       */
+} kd_top_logits_params;
+
+kd_status kd_top_logits_workspace_size(const kd_top_logits_params* params, size_t* bytes);
+/* Arrays aligned to their elements. */
+kd_status kd_top_logits(const kd_top_logits_params* params, const void* logits, void* top_logits, void* top_index, float* lse,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One token per row of logits, from one given number u[t] in [0, 1):
+ *   w_v = exp((logits[t, v] - largest) / temperature).  Entries in descending order of their logits, of equal ones the lower index
+ *   first: kept are the first top_k (0: all); of those the fewest whose sum of w is at least top_p times the sum over all of them
+ *   (1: all, at least one); of those the ones with w >= min_p (0: all).
+ *   token[t] = the first kept v, in order of v, where the sum of the kept w up to and with v exceeds u[t] times the sum of all kept
+ *   logp[t]  = log of w_token over that sum (may be NULL)
+ * w and its sums are held in 64 bits (exp to 2^-39, sums exact in fixed point of 2^-62 V), so that which token is drawn does not depend
+ * on the order of a sum.  temperature 0: the first of the largest logits, logp 0.  A setting may be the
+ * same for all rows (in params) or an array of one per row (temperature_rows, ... device pointers; NULL: params').  A logit of minus
+ * infinity is never drawn.  token is -1 and logp NaN in a row without a finite logit, with a NaN or a logit of plus infinity,
+ * and where u or a row's own setting is outside its range. */
+typedef struct {
+  int64_t T, V;               /* rows, entries of a row: 1 .. 2^22, 1 .. 2^24                    */
+  int64_t ld;                 /* elements from row to row of logits, >= V                        */
+  int32_t in_dtype;           /* kd_dtype of logits                                              */
+  int32_t index_dtype;        /* kd_index_dtype of token                                         */
+  float temperature;          /* 0, or 1e-6 .. 1e6                                               */
+  int32_t top_k;              /* >= 0                                                            */
+  float top_p;                /* 0 < top_p <= 1                                                  */
+  float min_p;                /* 0 <= min_p <= 1                                                 */
+  int32_t reserved[2];        /* must be 0                                                       */
+} kd_sample_params;
+
+kd_status kd_sample_workspace_size(const kd_sample_params* params, size_t* bytes);
+/* Arrays aligned to their elements. */
+kd_status kd_sample(const kd_sample_params* params, const void* logits, const float* u, const float* temperature_rows,
+                    const int32_t* top_k_rows, const float* top_p_rows, const float* min_p_rows, void* token, float* logp,
+                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Norm of n arrays taken together, and clipping:
+ *   KD_NORM_L2   total = sum of squares, norm = sqrt(total)          KD_NORM_MAX   total = norm = largest magnitude
+ *   kd_grad_clip: out = in min(1, max_norm / norm), in fp32, rounded once.
+ * Sums are held in 64 bits.  Where the norm is not finite nothing is scaled (a program sees it in norm and skips the step); a norm of
+ * NaN is one with a NaN among the elements.  grads, counts, dtypes, out: HOST arrays of n entries (device pointers, elements, kd_dtype);
+ * an array may have 0 elements (its pointer is not read).  The calls read the host arrays before they return.
+ * The arrays of one call must not overlap each other.
+ *  total  device, one double.  A program whose gradients are spread over ranks adds up (KD_NORM_MAX: takes the largest of) the ranks'
+ *         totals between the two calls.
+ *  out, out_dtypes  where the clipped values go; out NULL, or out[i] == grads[i] with the same type: in place, where nothing is written
+ *         if nothing has to be scaled
+ *  norm   device, one float, or NULL */
+typedef enum { KD_NORM_L2 = 0, KD_NORM_MAX = 1 } kd_norm;
+#define KD_GRADS_MAX 65536
+
+kd_status kd_grad_norm_workspace_size(int32_t n, const int64_t* counts, size_t* bytes);
+kd_status kd_grad_norm(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t norm_kind,
+                       double* total, void* workspace, size_t workspace_bytes, void* hip_stream);
+kd_status kd_grad_clip(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t norm_kind,
+                       const double* total, double max_norm, void* const* out, const int32_t* out_dtypes, float* norm, void* hip_stream);
+
 /* Static, NUL-terminated description of a status code (error reporting of this boundary; nothing of
  * the paper's). */
 const char* kd_status_string(kd_status status);

@@ -94,3 +94,42 @@ def topk_loss(h_s, W_s, top_logits, top_index, lse=None, mask=None, tau=1.0, tai
     return _HeadLossFn.apply(h_s, W_s, lambda gh, gW: K.kd_topk_fwd_bwd(top_logits, top_index, h_s.detach(), W_s.detach(),
                                                                         grad_dtype=grad_dtype, want_grad_h=gh, want_grad_W=gW,
                                                                         **kw), ("grad_h_s", "grad_W_s"))
+
+
+class _LinearE4m3Fn(torch.autograd.Function):
+    """x W^T with all three products in e4m3.  What backward needs of x and W is kept as codes, transposed, one byte an element."""
+
+    @staticmethod
+    def forward(ctx, x, W):
+        need_x, need_W = ctx.needs_input_grad
+        q, qt = K.quantize_e4m3_blocks(x, both=True) if need_W else (K.quantize_e4m3_blocks(x), None)
+        w, wt = K.quantize_e4m3_blocks(W, K.BLOCK_TILE, both=True) if need_x else (K.quantize_e4m3_blocks(W, K.BLOCK_TILE), None)
+        ctx.save_for_backward(*(t for y in (qt, wt) if y is not None for t in (y.codes, y.scales)))
+        ctx.types = (x.dtype, W.dtype)
+        return K.kd_matmul_e4m3(q, w, out_dtype=K.BF16 if x.dtype == torch.bfloat16 else K.F32)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gy):
+        need_x, need_W = ctx.needs_input_grad
+        kept = list(ctx.saved_tensors)
+        gy = gy.contiguous()
+        grad_x = grad_W = None
+        if need_x and need_W:
+            g, gt = K.quantize_e4m3_blocks(gy, both=True)
+        else:
+            g, gt = (K.quantize_e4m3_blocks(gy), None) if need_x else (None, K.quantize_e4m3_blocks(gy, transpose=True))
+        if need_W:
+            xt = K.E4m3Blocks(kept.pop(0), kept.pop(0), K.BLOCK_ROW)
+            grad_W = K.kd_matmul_e4m3(gt, xt, out_dtype=K.BF16 if ctx.types[1] == torch.bfloat16 else K.F32)
+        if need_x:
+            wt = K.E4m3Blocks(kept.pop(0), kept.pop(0), K.BLOCK_TILE)
+            grad_x = K.kd_matmul_e4m3(g, wt, out_dtype=K.BF16 if ctx.types[0] == torch.bfloat16 else K.F32)
+        return grad_x, grad_W
+
+
+def linear_e4m3(x, W):
+    """y = x W^T for x [T, H] and W [V, H], bf16 or fp32, computed in e4m3: x in blocks of 1 x 128, W in blocks of 128 x 128; backward,
+    gradients of y in blocks of 128 outputs for grad_x, and both factors of grad_W in blocks of 128 tokens.  y has x's type,
+    each gradient its leaf's."""
+    return _LinearE4m3Fn.apply(x, W)

@@ -1,0 +1,80 @@
+// Host-side interface of what stands beside the losses: kd_blocks.hip (e4m3 in blocks), kd_rows.hip (rows of logits), kd_norm.hip
+// (gradient norm), called by kd_beside_api.hip.
+#pragma once
+#include <hip/hip_runtime_api.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace kd {
+
+// ---- e4m3 in blocks ----
+struct BlocksArgs {
+  const void* src;
+  int64_t rows, cols, ld;
+  int src_f32, tile;
+  uint8_t *codes, *codes_t;
+  float *scales, *scales_t;
+};
+hipError_t launch_quantize_blocks(const BlocksArgs& a, hipStream_t st);
+
+struct ProductArgs {
+  const uint8_t *a, *b;
+  const float *a_scales, *b_scales;
+  void* out;
+  int64_t M, N, K;
+  int out_f32, b_tile, accumulate;
+};
+hipError_t launch_product(const ProductArgs& p, hipStream_t st);
+
+// ---- rows of logits ----
+// A workgroup of the first kernel reads kRowThreads * per_thread entries of a row, a chunk.  Each thread leaves the largest key of its
+// entries (a group), the workgroup the chunk's.
+constexpr int kRowThreads = 256;
+struct RowChunk {
+  uint64_t sum;      // sampling: of w relative to the chunk's largest entry, in fixed point
+  float part;        // top logits: the same in fp32
+  uint32_t key;      // the largest entry's
+};
+struct RowsArgs {
+  const void* logits;
+  int64_t T, V, ld;
+  int f32, index64;
+  int per_thread, chunks;     // entries per thread; chunks per row
+  float tau;                  // top logits; sampling: the temperature of all rows
+  // top logits
+  int K;
+  void *top, *index;
+  float* lse;
+  // sampling
+  const float *u, *temperature_rows, *top_p_rows, *min_p_rows;
+  const int32_t* top_k_rows;
+  int top_k;
+  float top_p, min_p;
+  void* token;
+  float* logp;
+  // workspace
+  RowChunk* chunk;            // [T][chunks]
+  uint32_t* group;            // [T][chunks * kRowThreads]
+};
+hipError_t launch_top_logits(const RowsArgs& r, hipStream_t st);
+hipError_t launch_sample(const RowsArgs& r, hipStream_t st);
+
+// ---- gradient norm ----
+constexpr int kGradsPerLaunch = 160;
+constexpr int kNormGroups = 2048;      // workgroups of a launch
+struct GradTable {
+  int n;                               // arrays of this launch
+  uint32_t chunks, chunk_elements;     // pieces of all arrays of this launch; elements of a piece
+  uint64_t in[kGradsPerLaunch];        // address, bit 0: fp32
+  uint64_t count[kGradsPerLaunch];
+  uint32_t first[kGradsPerLaunch];     // first piece of the array
+};
+struct ClipTable {
+  GradTable t;
+  uint64_t out[kGradsPerLaunch];       // address, bit 0: fp32
+};
+hipError_t launch_grad_norm(const GradTable& t, int max_norm_kind, double* partials, int groups, hipStream_t st);
+hipError_t launch_grad_total(const double* partials, int64_t n, int max_norm_kind, double* total, hipStream_t st);
+hipError_t launch_grad_clip(const ClipTable& t, int max_norm_kind, const double* total, double max_norm, float* norm, hipStream_t st);
+
+}  // namespace kd

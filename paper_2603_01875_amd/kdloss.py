@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import Any, NamedTuple
 
 FKL, RKL, JSD, TVD, SKEW_FKL, SKEW_RKL, AKL = 0, 1, 2, 3, 4, 5, 6
 BF16, F32 = 0, 1
@@ -16,6 +17,9 @@ W_HV, W_VH = 0, 1
 I32, I64 = 0, 1
 TAIL_RENORM, TAIL_REST, TAIL_DROP = 0, 1, 2
 TOPK_MAX = 1024
+BLOCK_ROW, BLOCK_TILE = 0, 1
+NORM_L2, NORM_MAX = 0, 1
+GRADS_MAX = 65536
 
 KD_OK = 0
 STATUS_NAMES = {0: "KD_OK", 1: "KD_ERR_NULL", 2: "KD_ERR_SHAPE", 3: "KD_ERR_ALIGN", 4: "KD_ERR_PARAM",
@@ -54,6 +58,33 @@ class KdTopkParams(ctypes.Structure):
                 ("index_dtype", ctypes.c_int32), ("top_dtype", ctypes.c_int32), ("tail", ctypes.c_int32),
                 ("tau", ctypes.c_float), ("loss_scale", ctypes.c_float), ("accumulate_grad_W", ctypes.c_int32),
                 ("flags", ctypes.c_int32), ("vocab_chunk", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2)]
+
+
+class KdBlocksParams(ctypes.Structure):
+    """kd_blocks_params of the C header."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("src_dtype", ctypes.c_int32),
+                ("block", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2)]
+
+
+class KdLinearParams(ctypes.Structure):
+    """kd_linear_params of the C header."""
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("in_dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("b_block", ctypes.c_int32), ("accumulate", ctypes.c_int32),
+                ("reserved", ctypes.c_int32 * 2)]
+
+
+class KdTopLogitsParams(ctypes.Structure):
+    """kd_top_logits_params of the C header."""
+    _fields_ = [("T", ctypes.c_int64), ("V", ctypes.c_int64), ("ld", ctypes.c_int64), ("K", ctypes.c_int32),
+                ("in_dtype", ctypes.c_int32), ("index_dtype", ctypes.c_int32), ("tau", ctypes.c_float),
+                ("reserved", ctypes.c_int32 * 2)]
+
+
+class KdSampleParams(ctypes.Structure):
+    """kd_sample_params of the C header."""
+    _fields_ = [("T", ctypes.c_int64), ("V", ctypes.c_int64), ("ld", ctypes.c_int64), ("in_dtype", ctypes.c_int32),
+                ("index_dtype", ctypes.c_int32), ("temperature", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("reserved", ctypes.c_int32 * 2)]
 
 
 class KdLossError(RuntimeError):
@@ -111,6 +142,20 @@ def lib():
         L.kd_topk_fwd_bwd.argtypes = [Q] + [vp] * 11 + [ctypes.c_size_t, vp]
         for call in (L.kd_ce_fwd, L.kd_ce_fwd_bwd, L.kd_topk_fwd, L.kd_topk_fwd_bwd):
             call.restype = ctypes.c_int
+        size_t = ctypes.c_size_t
+        B, M, U, S = (ctypes.POINTER(p) for p in (KdBlocksParams, KdLinearParams, KdTopLogitsParams, KdSampleParams))
+        i32 = ctypes.c_int32
+        for name, args in (("kd_quantize_e4m3_blocks", [B] + [vp] * 6), ("kd_linear_workspace_size", [M, ctypes.POINTER(size_t)]),
+                           ("kd_matmul_e4m3", [M] + [vp] * 6 + [size_t, vp]), ("kd_linear_e4m3", [M] + [vp] * 5 + [size_t, vp]),
+                           ("kd_top_logits_workspace_size", [U, ctypes.POINTER(size_t)]),
+                           ("kd_top_logits", [U] + [vp] * 5 + [size_t, vp]),
+                           ("kd_sample_workspace_size", [S, ctypes.POINTER(size_t)]),
+                           ("kd_sample", [S] + [vp] * 9 + [size_t, vp]),
+                           ("kd_grad_norm_workspace_size", [i32, vp, ctypes.POINTER(size_t)]),
+                           ("kd_grad_norm", [i32, vp, vp, vp, i32, vp, vp, size_t, vp]),
+                           ("kd_grad_clip", [i32, vp, vp, vp, i32, vp, ctypes.c_double, vp, vp, vp, vp])):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = ctypes.c_int
         L.kd_quantize_e4m3.argtypes = [vp, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, vp, vp]
         L.kd_quantize_e4m3.restype = ctypes.c_int
         L.kd_loss_profile_clock.argtypes = [vp]
@@ -163,14 +208,18 @@ def quantize_e4m3(x, scale, out=None):
 
 
 def kd_loss_workspace_size(params) -> int:
-    """Workspace bytes of a call with this parameter block (KdLossParams, KdCeParams or KdTopkParams)."""
+    """Workspace bytes of a call with this parameter block (KdLossParams, KdCeParams, KdTopkParams, KdLinearParams,
+    KdTopLogitsParams or KdSampleParams)."""
     n = ctypes.c_size_t(0)
     for block, query in ((KdLossParams, lib().kd_loss_workspace_size), (KdCeParams, lib().kd_ce_workspace_size),
-                         (KdTopkParams, lib().kd_topk_workspace_size)):
+                         (KdTopkParams, lib().kd_topk_workspace_size), (KdLinearParams, lib().kd_linear_workspace_size),
+                         (KdTopLogitsParams, lib().kd_top_logits_workspace_size),
+                         (KdSampleParams, lib().kd_sample_workspace_size)):
         if isinstance(params, block):
             break
     else:
-        raise TypeError(f"params must be a KdLossParams, KdCeParams or KdTopkParams, got {type(params).__name__}")
+        raise TypeError("params must be a KdLossParams, KdCeParams, KdTopkParams, KdLinearParams, KdTopLogitsParams or "
+                        f"KdSampleParams, got {type(params).__name__}")
     st = query(ctypes.byref(params), ctypes.byref(n))
     if st != KD_OK:
         raise KdLossError(st)
@@ -711,3 +760,324 @@ def kd_topk_fwd(top_logits, top_index, h_s, W_s, lse=None, mask=None, tau=1.0, t
     loss, ptl, _, _, ws = _head_outputs(p, h_s, W_s, workspace, False, None, None)
     kd_topk_fwd_raw(p, top_logits, top_index, lse, h_s, W_s, mask, loss, ptl, ws)
     return dict(loss=loss, per_token_loss=ptl)
+
+
+# ------------------------------------------------------------------------------------------------
+# beside the losses: e4m3 in blocks of 128, top logits, sampling, the norm of the gradients
+# ------------------------------------------------------------------------------------------------
+def _call(name, dev, args, stream):
+    """Makes a call on the device of its tensors, whatever the current one is, on `stream` or that device's current one."""
+    import torch
+    call = getattr(lib(), name)
+    if dev.index == torch.cuda.current_device():
+        st = call(*args, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream if stream is None else stream))
+    else:
+        with torch.cuda.device(dev):
+            st = call(*args, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream if stream is None else stream))
+    if st != KD_OK:
+        raise KdLossError(st)
+
+
+def _check_workspace(workspace, dev):
+    if workspace is None or workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA (HIP) tensor on the operands' device")
+
+
+def _check_matrix(t, name):
+    """(rows, columns, elements from row to row) of a CUDA matrix whose rows are contiguous."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-dimensional torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    ld = t.stride(0) if rows > 1 else max(cols, 1)
+    if ld < cols:
+        raise ValueError(f"{name} has rows that overlap")
+    return rows, cols, ld
+
+
+class E4m3Blocks(NamedTuple):
+    """A matrix [rows, cols] as e4m3 codes (uint8 [rows, cols rounded up to 16], zero behind a row's end) with a scale per block:
+    BLOCK_ROW, [rows, ceil(cols / 128)], or BLOCK_TILE, [ceil(rows / 128), ceil(cols / 128)]."""
+    codes: Any
+    scales: Any
+    block: int
+
+
+def _check_blocks(q, name, rows, ld, dev):
+    import torch
+    if not isinstance(q, E4m3Blocks):
+        raise ValueError(f"{name} must be E4m3Blocks")
+    if q.block not in (BLOCK_ROW, BLOCK_TILE):
+        raise ValueError(f"{name} has an unknown block")
+    n = (ld + 127) // 128
+    _check_tensors([(name + ".codes", q.codes, (torch.uint8,), rows * ld, False),
+                    (name + ".scales", q.scales, (torch.float32,), (rows if q.block == BLOCK_ROW else (rows + 127) // 128) * n, False)],
+                   dev)
+
+
+def make_blocks_params(rows, cols, ld=None, src_dtype=BF16, block=BLOCK_ROW):
+    return KdBlocksParams(int(rows), int(cols), int(cols if ld is None else ld), int(src_dtype), int(block))
+
+
+def quantize_e4m3_blocks(x, block=BLOCK_ROW, transpose=False, both=False, stream=None):
+    """E4m3Blocks of a bf16 or fp32 matrix with contiguous rows: a scale per row and 128 columns (BLOCK_ROW) or per 128 x 128
+    (BLOCK_TILE).  transpose: of x's transpose instead; both: (x's, its transpose's) from one reading.  Other than quantize_e4m3, which
+    multiplies by a reciprocal, it divides: code = e4m3(448 x / largest of the block), rounded once before."""
+    import torch
+    rows, cols, ld = _check_matrix(x, "x")
+    p = make_blocks_params(rows, cols, ld, _float_dtype(x, "x"), block)
+    if block not in (BLOCK_ROW, BLOCK_TILE):
+        raise ValueError("unknown block")
+
+    def made(r, c):
+        n = (c + 127) // 128
+        return E4m3Blocks(torch.empty(r, (c + 15) // 16 * 16, dtype=torch.uint8, device=x.device),
+                          torch.empty(r if block == BLOCK_ROW else (r + 127) // 128, n, dtype=torch.float32, device=x.device), block)
+    q = None if transpose and not both else made(rows, cols)
+    qt = made(cols, rows) if transpose or both else None
+    args = [_ptr(t) for y in (q, qt) for t in ((None, None) if y is None else (y.codes, y.scales))]
+    _call("kd_quantize_e4m3_blocks", x.device, [ctypes.byref(p), _ptr(x)] + args, stream)
+    return (q, qt) if both else qt if transpose else q
+
+
+def make_linear_params(M, N, K, in_dtype=BF16, out_dtype=BF16, b_block=BLOCK_TILE, accumulate=False):
+    return KdLinearParams(int(M), int(N), int(K), int(in_dtype), int(out_dtype), int(b_block), int(bool(accumulate)))
+
+
+def _linear_call(name, p, first, b, out, workspace, stream):
+    import torch
+    dev = out.device
+    ld = (p.K + 15) // 16 * 16
+    _check_blocks(b, "b", p.N, ld, dev)
+    if b.block != p.b_block:
+        raise ValueError("the blocks of b are not those of the parameter block")
+    _check_tensors([("out", out, (torch.bfloat16 if p.out_dtype == BF16 else torch.float32,), p.M * p.N, False)], dev)
+    _check_workspace(workspace, dev)
+    _call(name, dev, [ctypes.byref(p)] + first + [_ptr(b.codes), _ptr(b.scales), _ptr(out), _ptr(workspace),
+                                                  ctypes.c_size_t(_nbytes(workspace))], stream)
+
+
+def kd_matmul_e4m3_raw(params, a, b, out, workspace, stream=None):
+    """Thin call: a and b are E4m3Blocks (a by rows), out and workspace the caller's."""
+    _check_blocks(a, "a", params.M, (params.K + 15) // 16 * 16, out.device)
+    if a.block != BLOCK_ROW:
+        raise ValueError("a must be in blocks of rows (BLOCK_ROW)")
+    _linear_call("kd_matmul_e4m3", params, [_ptr(a.codes), _ptr(a.scales)], b, out, workspace, stream)
+
+
+def kd_linear_e4m3_raw(params, x, w, out, workspace, stream=None):
+    """Thin call: x [M, K] is quantised in the call, w is E4m3Blocks by tiles, out and workspace the caller's."""
+    import torch
+    _check_tensors([("x", x, (torch.bfloat16 if params.in_dtype == BF16 else torch.float32,), params.M * params.K, False)], out.device)
+    _linear_call("kd_linear_e4m3", params, [_ptr(x)], w, out, workspace, stream)
+
+
+def _linear_out(M, N, out, out_dtype, accumulate, dev):
+    import torch
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the out to add to")
+        return torch.empty(M, N, dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=dev), out_dtype
+    if tuple(out.shape) != (M, N):
+        raise ValueError(f"out has shape {tuple(out.shape)}, expected {(M, N)}")
+    return out, _float_dtype(out, "out")
+
+
+def kd_matmul_e4m3(a, b, out=None, out_dtype=BF16, accumulate=False, workspace=None):
+    """a b^T of two matrices in blocks: a [M, K] by rows, b [N, K] by rows or tiles.  Returns out [M, N]."""
+    if not isinstance(a, E4m3Blocks) or not isinstance(b, E4m3Blocks) or a.codes.dim() != 2 or b.codes.dim() != 2:
+        raise ValueError("a and b must be E4m3Blocks with codes [rows, columns]")
+    (M, K), (N, K_b) = a.codes.shape, b.codes.shape
+    if K != K_b or K % 16:
+        raise ValueError(f"a and b have rows of {K} and {K_b} codes, expected the same multiple of 16")
+    out, out_dtype = _linear_out(M, N, out, out_dtype, accumulate, a.codes.device)
+    p = make_linear_params(M, N, K, BF16, out_dtype, b.block, accumulate)
+    kd_matmul_e4m3_raw(p, a, b, out, alloc_workspace(p, out.device) if workspace is None else workspace)
+    return out
+
+
+def kd_linear_e4m3(x, w, out=None, out_dtype=None, accumulate=False, workspace=None):
+    """x W^T with x [M, K] in bf16 or fp32, quantised in the call by rows, and W [N, K] in E4m3Blocks by tiles.  Returns out [M, N], in
+    x's type unless it is given or out_dtype says otherwise."""
+    M, K, ld = _check_matrix(x, "x")
+    in_dtype = _float_dtype(x, "x")
+    if not isinstance(w, E4m3Blocks) or w.codes.dim() != 2:
+        raise ValueError("w must be E4m3Blocks with codes [rows, columns]")
+    N = w.codes.shape[0]
+    out, out_dtype = _linear_out(M, N, out, in_dtype if out_dtype is None else out_dtype, accumulate, x.device)
+    p = make_linear_params(M, N, K, in_dtype, out_dtype, w.block, accumulate)
+    kd_linear_e4m3_raw(p, x, w, out, alloc_workspace(p, x.device) if workspace is None else workspace)
+    return out
+
+
+def make_top_logits_params(T, V, K, ld=None, tau=1.0, in_dtype=BF16, index_dtype=I64):
+    return KdTopLogitsParams(int(T), int(V), int(V if ld is None else ld), int(K), int(in_dtype), int(index_dtype), float(tau))
+
+
+def make_sample_params(T, V, ld=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, in_dtype=BF16, index_dtype=I64):
+    return KdSampleParams(int(T), int(V), int(V if ld is None else ld), int(in_dtype), int(index_dtype), float(temperature),
+                          int(top_k), float(top_p), float(min_p))
+
+
+def _check_logits(p, logits):
+    import torch
+    rows, cols, ld = _check_matrix(logits, "logits")
+    if (rows, cols) != (p.T, p.V) or (rows > 1 and ld != p.ld):
+        raise ValueError(f"logits are {rows} x {cols}, {ld} from row to row; the parameter block says {p.T} x {p.V}, {p.ld}")
+    if logits.dtype != (torch.bfloat16 if p.in_dtype == BF16 else torch.float32):
+        raise ValueError(f"logits are {logits.dtype}, not what the parameter block says")
+    return logits.device
+
+
+def kd_top_logits_raw(params, logits, top_logits, top_index, lse, workspace, stream=None):
+    """Thin call: all tensors are the caller's (lse may be None)."""
+    import torch
+    dev = _check_logits(params, logits)
+    n = params.T * params.K
+    _check_tensors([("top_logits", top_logits, (logits.dtype,), n, False),
+                    ("top_index", top_index, (torch.int32 if params.index_dtype == I32 else torch.int64,), n, False),
+                    ("lse", lse, (torch.float32,), params.T, True)], dev)
+    _check_workspace(workspace, dev)
+    _call("kd_top_logits", dev, [ctypes.byref(params), _ptr(logits), _ptr(top_logits), _ptr(top_index), _ptr(lse), _ptr(workspace),
+                                 ctypes.c_size_t(_nbytes(workspace))], stream)
+
+
+def kd_top_logits(logits, K, tau=1.0, index_dtype=I64, workspace=None):
+    """The K largest logits of each row of [T, V] with their places, in descending order, and the row's log-sum-exp of logits / tau:
+    what kd_topk_fwd_bwd takes as top_logits, top_index and lse.  Returns a dict of tensors."""
+    import torch
+    T, V, ld = _check_matrix(logits, "logits")
+    dev = logits.device
+    p = make_top_logits_params(T, V, K, ld, tau, _float_dtype(logits, "logits"), index_dtype)
+    ws = alloc_workspace(p, dev) if workspace is None else workspace
+    top = torch.empty(T, int(K), dtype=logits.dtype, device=dev)
+    index = torch.empty(T, int(K), dtype=torch.int32 if index_dtype == I32 else torch.int64, device=dev)
+    lse = torch.empty(T, dtype=torch.float32, device=dev)
+    kd_top_logits_raw(p, logits, top, index, lse, ws)
+    return dict(top_logits=top, top_index=index, lse=lse)
+
+
+def kd_sample_raw(params, logits, u, token, logp, workspace, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """Thin call: all tensors are the caller's (logp may be None).  temperature, top_k, top_p, min_p: tensors of one setting per row,
+    or None for the parameter block's."""
+    import torch
+    dev = _check_logits(params, logits)
+    f, T = (torch.float32,), params.T
+    _check_tensors([("u", u, f, T, False), ("token", token, (torch.int32 if params.index_dtype == I32 else torch.int64,), T, False),
+                    ("logp", logp, f, T, True), ("temperature", temperature, f, T, True), ("top_k", top_k, (torch.int32,), T, True),
+                    ("top_p", top_p, f, T, True), ("min_p", min_p, f, T, True)], dev)
+    _check_workspace(workspace, dev)
+    _call("kd_sample", dev, [ctypes.byref(params), _ptr(logits), _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                             _ptr(token), _ptr(logp), _ptr(workspace), ctypes.c_size_t(_nbytes(workspace))], stream)
+
+
+def kd_sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, index_dtype=I64, workspace=None):
+    """One token per row of logits [T, V], drawn with the given uniform numbers u [T] (fp32, in [0, 1)); each setting is a number or a
+    tensor of one per row.  Returns a dict: token [T] (-1 in a row that cannot be drawn from), logp [T], its log-probability among the
+    kept entries."""
+    import torch
+    T, V, ld = _check_matrix(logits, "logits")
+    dev = logits.device
+    settings = dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+    rows = {k: v for k, v in settings.items() if isinstance(v, torch.Tensor)}
+    p = make_sample_params(T, V, ld, in_dtype=_float_dtype(logits, "logits"), index_dtype=index_dtype,
+                           **{k: v for k, v in settings.items() if k not in rows})
+    ws = alloc_workspace(p, dev) if workspace is None else workspace
+    token = torch.empty(T, dtype=torch.int32 if index_dtype == I32 else torch.int64, device=dev)
+    logp = torch.empty(T, dtype=torch.float32, device=dev)
+    kd_sample_raw(p, logits, u, token, logp, ws, **rows)
+    return dict(token=token, logp=logp)
+
+
+class GradList:
+    """The gradients of a model as the library's calls take them: contiguous bf16 or fp32 tensors on one device, checked once (a None
+    is left out, as a parameter without a gradient has one).  out: where clipped gradients go, a tensor of each one's size; None:
+    in place.  The tensors are kept; a program whose gradients are allocated anew in every step makes a new list."""
+
+    def __init__(self, grads, out=None):
+        import torch
+        grads = list(grads)
+        outs = [None] * len(grads) if out is None else list(out)
+        if len(outs) != len(grads):
+            raise ValueError("out must have one tensor per gradient")
+        pairs = [(g, o) for g, o in zip(grads, outs) if g is not None]
+        if not pairs:
+            raise ValueError("there is no gradient")
+        self.grads = [g for g, _ in pairs]
+        self.out = None if out is None else [o for _, o in pairs]
+        if not all(isinstance(t, torch.Tensor) and t.is_cuda for t in self.grads):
+            raise ValueError("gradients must be CUDA (HIP) tensors")
+        self.device = self.grads[0].device
+        for name, tensors in (("gradient", self.grads), ("out", self.out or [])):
+            for i, t in enumerate(tensors):
+                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != self.device:
+                    raise ValueError(f"{name} {i} must be a CUDA (HIP) tensor on {self.device}")
+                if not t.is_contiguous():
+                    raise ValueError(f"{name} {i} must be contiguous")
+                _float_dtype(t, f"{name} {i}")
+                if t.numel() != self.grads[i].numel():
+                    raise ValueError(f"{name} {i} has {t.numel()} elements, expected {self.grads[i].numel()}")
+        for g, o in zip(self.grads, self.out or []):
+            if g.data_ptr() == o.data_ptr() and g.dtype != o.dtype:
+                raise ValueError("out is a gradient in another type")
+        written = self.out or self.grads
+        spans = {(t.data_ptr(), t.data_ptr() + _nbytes(t), i) for x in (self.grads, written) for i, t in enumerate(x) if t.numel()}
+        spans = sorted(spans)
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])) or len(spans) != len({s[:2] for s in spans}):
+            raise ValueError("gradients (or out) overlap each other")
+        n = self.n = len(self.grads)
+        if n > GRADS_MAX:
+            raise ValueError(f"at most {GRADS_MAX} gradients")
+
+        def pointers(ts):
+            return (ctypes.c_void_p * n)(*[t.data_ptr() for t in ts])
+
+        def dtypes(ts):
+            return (ctypes.c_int32 * n)(*[BF16 if t.dtype == torch.bfloat16 else F32 for t in ts])
+        self.counts = (ctypes.c_int64 * n)(*[t.numel() for t in self.grads])
+        self._in = pointers(self.grads), dtypes(self.grads)
+        self._out = (None, None) if self.out is None else (pointers(self.out), dtypes(self.out))
+        size = ctypes.c_size_t(0)
+        st = lib().kd_grad_norm_workspace_size(n, self.counts, ctypes.byref(size))
+        if st != KD_OK:
+            raise KdLossError(st)
+        self.workspace_bytes = size.value
+
+
+def _grad_list(grads):
+    return grads if isinstance(grads, GradList) else GradList(grads)
+
+
+def kd_grad_norm(grads, norm_kind=NORM_L2, workspace=None, stream=None):
+    """The sum of all squares (NORM_L2) or the largest magnitude (NORM_MAX) over a GradList or a list of tensors, as one float64 on the
+    device.  A program with gradients spread over ranks all-reduces it and goes on with kd_grad_clip."""
+    import torch
+    g = _grad_list(grads)
+    total = torch.empty((), dtype=torch.float64, device=g.device)
+    ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=g.device) if workspace is None else workspace
+    _check_workspace(ws, g.device)
+    _call("kd_grad_norm", g.device, [g.n, g._in[0], g.counts, g._in[1], int(norm_kind), _ptr(total), _ptr(ws),
+                                     ctypes.c_size_t(_nbytes(ws))], stream)
+    return total
+
+
+def kd_grad_clip(grads, total, max_norm, norm_kind=NORM_L2, stream=None):
+    """Scales all gradients (into the list's out, or in place) by min(1, max_norm / norm), the norm being that of `total` (kd_grad_norm);
+    where it is not finite they stay as they are.  Returns the norm, one float32 on the device."""
+    import torch
+    g = _grad_list(grads)
+    _check_tensors([("total", total, (torch.float64,), 1, False)], g.device)
+    norm = torch.empty((), dtype=torch.float32, device=g.device)
+    _call("kd_grad_clip", g.device, [g.n, g._in[0], g.counts, g._in[1], int(norm_kind), _ptr(total), float(max_norm), g._out[0],
+                                     g._out[1], _ptr(norm)], stream)
+    return norm
+
+
+def kd_clip_grad_norm(grads, max_norm, norm_kind=NORM_L2, workspace=None, stream=None):
+    """kd_grad_norm and kd_grad_clip in one: clips all gradients together to the norm max_norm.  Returns the norm they had."""
+    g = _grad_list(grads)
+    return kd_grad_clip(g, kd_grad_norm(g, norm_kind, workspace, stream), max_norm, norm_kind, stream)
