@@ -6,7 +6,7 @@ FLAGS="--offload-arch=gfx950 -O3 -std=c++17 -fPIC -Xclang -target-feature -Xclan
 OBJ=$(mktemp -d)
 trap 'rm -rf "$OBJ"' EXIT
 pids=()
-for f in kd_kernels kd_strip_hv kd_products kd_few kd_api kd_head kd_head_few kd_head_products kd_head_api kd_blocks kd_rows kd_norm kd_beside_api; do
+for f in kd_kernels kd_strip_hv kd_products kd_few kd_api kd_head kd_head_few kd_head_products kd_head_api kd_blocks kd_product kd_rows kd_norm kd_beside_api; do
   hipcc $FLAGS "$@" -c $f.hip -o "$OBJ/$f.o" & pids+=($!)
 done
 for p in "${pids[@]}"; do wait $p; done

@@ -1,0 +1,224 @@
+// Product of two matrices of e4m3 in blocks (kd_matmul_e4m3, kd_linear_e4m3):
+//   out[m][n] = sum_j a_scale[m][j] b_scale[n or n / 128][j] sum_{k in block j} a[m][k] b[n][k]
+//
+// Rows of b are the register axis of the matrix instructions, rows of a the lane axis, so that a lane has one a's scale.
+// A bf16 result takes the e4m3 pipe (16x16x128: one instruction is one block's sum).  That pipe aligns the products of a group of eight to the
+// largest of them and cuts off what is 2^-14 below: 1.5e-5 of a result of normal numbers, nothing beside its rounding to bf16
+// (1.7e-3), but not what fp32 stands for.  An fp32 result takes the codes to bf16, which holds them exactly, and the bf16 pipe at
+// half the rate (CUT false).
+#include <hip/hip_runtime.h>
+
+#include "kd_beside.h"
+#include "kd_common.hpp"
+#include "kd_launch.h"
+#include "kd_unaligned.hpp"
+
+namespace kd {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+// eight codes as bf16
+__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.f, true);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// A lane's 32 codes of a row as the matrix instructions take them.
+template <bool CUT> struct Codes { i32x8 v; };
+template <> struct Codes<false> { bf16x8 v[4]; };
+template <bool CUT>
+__device__ __forceinline__ Codes<CUT> codes_from(const u32x4& lo, const u32x4& hi) {
+  Codes<CUT> c;
+  if constexpr (CUT) {
+    c.v = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    c.v[0] = widen(lo[0], lo[1]);
+    c.v[1] = widen(lo[2], lo[3]);
+    c.v[2] = widen(hi[0], hi[1]);
+    c.v[3] = widen(hi[2], hi[3]);
+  }
+  return c;
+}
+// sum over a block of 16 rows by 16 rows
+template <bool CUT>
+__device__ __forceinline__ f32x4 block_product(const Codes<CUT>& x, const Codes<CUT>& y) {
+  f32x4 c = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (CUT) {
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x.v, y.v, c, 0, 0, 0, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.v[i], y.v[i], c, 0, 0, 0);
+  }
+  return c;
+}
+
+// four results of one row m, columns n .. n + 3 (at most N)
+__device__ __forceinline__ void store4(const ProductArgs& p, int64_t m, int64_t n, f32x4 v) {
+  const int64_t at = m * p.N + n;
+  if (n + 4 <= p.N) {
+    if (p.out_f32) {
+      const global_t o = (global_t)((float*)p.out + at);
+      if (p.accumulate) {
+        const u32x4_t w = load16((const float*)p.out + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(w[i]);
+      }
+      store16(o, u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+    } else {
+      const global_t o = (global_t)((uint16_t*)p.out + at);
+      if (p.accumulate) {
+        const u32x2_t w = ((const Bytes8*)((uint16_t*)p.out + at))->v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += bf16_float((uint16_t)(w[i >> 1] >> (16 * (i & 1))));
+      }
+      store8(o, u32x2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])});
+    }
+    return;
+  }
+  for (int i = 0; i < 4 && n + i < p.N; ++i) {
+    if (p.out_f32) {
+      float* const o = (float*)p.out + at + i;
+      *o = v[i] + (p.accumulate ? *o : 0.f);
+    } else {
+      uint16_t* const o = (uint16_t*)p.out + at + i;
+      *o = bf16_bits(v[i] + (p.accumulate ? bf16_float(*o) : 0.f));
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// tiles
+//
+// WN x WM waves, each with NB x MB blocks of 16 x 16 results.  A k-step is one block of 128: the tile's rows of b and a, 128 bytes each, and
+// their scales, loaded straight into LDS while the step before is multiplied (two stages).  16-byte chunks of a row are permuted by
+// XOR with bits of its number, so that 16 rows' reads of one chunk fall into different banks.
+// ------------------------------------------------------------------------------------------------
+template <int NB_, int MB_, int WN_, int WM_>
+struct ProductTile {
+  static constexpr int NB = NB_, MB = MB_, WN = WN_, WM = WM_, NT = 64 * WN * WM, BN = 16 * NB * WN, BM = 16 * MB * WM;
+  static constexpr int LOAD_ROWS = NT / 8;                                  // rows of one 16-byte load a thread
+  static constexpr int N_LOADS = BN / LOAD_ROWS, M_LOADS = BM / LOAD_ROWS;
+  static constexpr int SCALES = BN + BM, SCALE_LOADS = (SCALES + NT - 1) / NT;
+  static constexpr int STAGE = (BN + BM) * 128 + SCALE_LOADS * NT * 4, SMEM = 2 * STAGE;
+  static_assert(BN % LOAD_ROWS == 0 && BM % LOAD_ROWS == 0 && LOAD_ROWS % 16 == 0, "whole loads, one permutation a thread");
+  static_assert(SMEM <= 160 * 1024, "LDS");
+};
+
+template <class Tile, bool CUT, bool B_TILE>
+__global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArgs p) {
+  constexpr int NB = Tile::NB, MB = Tile::MB, NT = Tile::NT, BN = Tile::BN, BM = Tile::BM;
+  extern __shared__ __attribute__((aligned(128))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wn = wave % Tile::WN, wm = wave / Tile::WN;
+  const int l = lane & 15, g = lane >> 4;
+  const int n_mt = (int)((p.M + BM - 1) / BM), n_nt = (int)((p.N + BN - 1) / BN);
+  int tm, tn;
+  group_decode(xcd_logical_id(blockIdx.x, gridDim.x), n_mt, n_nt, tm, tn);
+  const int64_t n0 = (int64_t)tn * BN, m0 = (int64_t)tm * BM;
+  const int ld = (int)((p.K + 15) / 16 * 16), nk = (int)((p.K + 127) / 128);
+
+  // loads: thread tid has chunk tid % 8 (as stored) of rows tid / 8 + j LOAD_ROWS; rows behind the matrix give 0
+  const int row = tid >> 3, chunk = (tid & 7) ^ ((row >> 1) & 7);
+  const int64_t n_rows = p.N - n0 < BN ? p.N - n0 : BN, m_rows = p.M - m0 < BM ? p.M - m0 : BM;
+  const rsrc_t rb = make_rsrc(p.b + n0 * ld, (uint32_t)(n_rows * ld)), ra = make_rsrc(p.a + m0 * ld, (uint32_t)(m_rows * ld));
+  const uint32_t at = (uint32_t)row * ld + chunk * 16, step = (uint32_t)Tile::LOAD_ROWS * ld;
+  const float* scale[Tile::SCALE_LOADS];
+#pragma unroll
+  for (int j = 0; j < Tile::SCALE_LOADS; ++j) {
+    int i = j * NT + tid;
+    if (i < BN) {
+      const int64_t n = n0 + i < p.N ? n0 + i : p.N - 1;
+      scale[j] = p.b_scales + (B_TILE ? n / 128 : n) * nk;
+    } else {
+      const int64_t m = m0 + i - BN < p.M ? m0 + i - BN : p.M - 1;
+      scale[j] = p.a_scales + m * nk;
+    }
+  }
+  auto load = [&](int stage, int k) {
+    char* const to = smem + stage * Tile::STAGE + wave * 1024;
+    const uint32_t from = at | (k * 128 + chunk * 16 < ld ? 0u : 0x80000000u);           // (a row's chunks behind its end: 0)
+#pragma unroll
+    for (int j = 0; j < Tile::N_LOADS; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void_t*)(to + j * (NT * 16)), 16, from + j * step, k * 128, 0, 0);
+#pragma unroll
+    for (int j = 0; j < Tile::M_LOADS; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_t*)(to + BN * 128 + j * (NT * 16)), 16, from + j * step, k * 128, 0, 0);
+#pragma unroll
+    for (int j = 0; j < Tile::SCALE_LOADS; ++j)
+      __builtin_amdgcn_global_load_lds((const void*)(scale[j] + k), (lds_void_t*)(smem + stage * Tile::STAGE + (BN + BM) * 128 + j * (NT * 4) + wave * 256),
+                                       4, 0, 0);
+  };
+
+  f32x4 acc[NB][MB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < MB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int sw = (l >> 1) & 7, c0 = ((2 * g) ^ sw) * 16, c1 = ((2 * g + 1) ^ sw) * 16;
+  auto read = [&](const char* rows, int block) {
+    const char* const r = rows + (block * 16 + l) * 128;
+    return codes_from<CUT>(*(const u32x4*)(r + c0), *(const u32x4*)(r + c1));
+  };
+  auto multiply = [&](int stage) {
+    const char* const base = smem + stage * Tile::STAGE;
+    const float* const sb = (const float*)(base + (BN + BM) * 128);
+    const char *const b = base + wn * (NB * 16 * 128), *const a = base + BN * 128 + wm * (MB * 16 * 128);
+    Codes<CUT> y[MB];
+    float s[MB];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+      y[j] = read(a, j);
+      s[j] = sb[BN + wm * (MB * 16) + j * 16 + l];
+      if (B_TILE) s[j] *= sb[wn * (NB * 16)];
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const Codes<CUT> x = read(b, i);
+      f32x4 t;
+      if (!B_TILE) t = *(const f32x4*)(sb + wn * (NB * 16) + i * 16 + 4 * g);
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        const f32x4 c = block_product<CUT>(x, y[j]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(c[r], B_TILE ? s[j] : s[j] * t[r], acc[i][j][r]);
+      }
+    }
+  };
+
+  load(0, 0);
+  for (int k = 0; k < nk; ++k) {
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");      // step k has landed; nobody reads the other stage any more
+    if (k + 1 < nk) load((k + 1) & 1, k + 1);
+    multiply(k & 1);
+  }
+#pragma unroll
+  for (int j = 0; j < MB; ++j) {
+    const int64_t m = m0 + wm * (MB * 16) + j * 16 + l;
+    if (m >= p.M) continue;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int64_t n = n0 + wn * (NB * 16) + i * 16 + 4 * g;
+      if (n < p.N) store4(p, m, n, acc[i][j]);
+    }
+  }
+}
+
+template <class Tile, bool CUT>
+static hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
+  const int64_t tiles = (p.M + Tile::BM - 1) / Tile::BM * ((p.N + Tile::BN - 1) / Tile::BN);
+  if (tiles > INT32_MAX / Tile::NT) return hipErrorInvalidValue;
+  void* args = const_cast<ProductArgs*>(&p);
+  void* params[] = {args};
+  return p.b_tile ? launch_big<product_tile_kernel<Tile, CUT, true>>((int)tiles, Tile::NT, Tile::SMEM, st, params[0])
+                  : launch_big<product_tile_kernel<Tile, CUT, false>>((int)tiles, Tile::NT, Tile::SMEM, st, params[0]);
+}
+
+hipError_t launch_product(const ProductArgs& p, hipStream_t st) {
+  if (p.out_f32) return launch_tiles<ProductTile<4, 4, 2, 2>, false>(p, st);
+  const int64_t big = (p.M + 255) / 256 * ((p.N + 255) / 256);
+  if (big >= kNumCU) return launch_tiles<ProductTile<8, 4, 2, 4>, true>(p, st);
+  return launch_tiles<ProductTile<4, 4, 2, 2>, true>(p, st);
+}
+
+}  // namespace kd
