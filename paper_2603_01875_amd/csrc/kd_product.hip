@@ -160,38 +160,75 @@ __global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArg
     const char* const r = rows + (block * 16 + l) * 128;
     return codes_from<CUT>(*(const u32x4*)(r + c0), *(const u32x4*)(r + c1));
   };
-  auto multiply = [&](int stage) {
-    const char* const base = smem + stage * Tile::STAGE;
-    const float* const sb = (const float*)(base + (BN + BM) * 128);
-    const char *const b = base + wn * (NB * 16 * 128), *const a = base + BN * 128 + wm * (MB * 16 * 128);
-    Codes<CUT> y[MB];
-    float s[MB];
+  // What a step multiplies by: codes and scales of the wave's rows of a, and 16 rows of b after the other.
+  Codes<CUT> y[MB], x[2];
+  float s[MB], s_next[MB];
+  f32x4 t[2];
+  auto read_a = [&](const char* base, int j) {
+    const float* const scales = (const float*)(base + (BN + BM) * 128);
+    y[j] = read(base + BN * 128 + wm * (MB * 16 * 128), j);
+    s_next[j] = scales[BN + wm * (MB * 16) + j * 16 + l];
+    if (B_TILE) s_next[j] *= scales[wn * (NB * 16)];
+  };
+  auto read_b = [&](const char* base, int i) { x[i & 1] = read(base + wn * (NB * 16 * 128), i); };
+  auto read_t = [&](const char* base, int i) {
+    if (!B_TILE) t[i & 1] = *(const f32x4*)((const float*)(base + (BN + BM) * 128) + wn * (NB * 16) + i * 16 + 4 * g);
+  };
+  // A product's result is scaled and added three products later, so that nothing waits for the matrix pipe.
+  constexpr int PRODUCTS = NB * MB, LATE = 3;
+  static_assert(NB % 2 == 0 && PRODUCTS % 4 == 0 && MB > LATE / NB && PRODUCTS > 4, "places of x, t and c");
+  f32x4 c[4];
 #pragma unroll
-    for (int j = 0; j < MB; ++j) {
-      y[j] = read(a, j);
-      s[j] = sb[BN + wm * (MB * 16) + j * 16 + l];
-      if (B_TILE) s[j] *= sb[wn * (NB * 16)];
-    }
+  for (int i = 0; i < 4; ++i) c[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  t[0] = t[1] = c[0];
+  auto add = [&](int q) {
+    const int i = q / MB, j = q % MB;
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const Codes<CUT> x = read(b, i);
-      f32x4 t;
-      if (!B_TILE) t = *(const f32x4*)(sb + wn * (NB * 16) + i * 16 + 4 * g);
-#pragma unroll
-      for (int j = 0; j < MB; ++j) {
-        const f32x4 c = block_product<CUT>(x, y[j]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(c[r], B_TILE ? s[j] : s[j] * t[r], acc[i][j][r]);
-      }
-    }
+    for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(c[q & 3][r], B_TILE ? s[j] : s[j] * t[i & 1][r], acc[i][j][r]);
   };
 
   load(0, 0);
-  for (int k = 0; k < nk; ++k) {
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");      // step k has landed; nobody reads the other stage any more
-    if (k + 1 < nk) load((k + 1) & 1, k + 1);
-    multiply(k & 1);
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  load(1, nk > 1 ? 1 : 0);
+#pragma unroll
+  for (int j = 0; j < MB; ++j) {
+    read_a(smem, j);
+    s[j] = 0.f;
   }
+  read_b(smem, 0);
+  for (int k = 0; k < nk; ++k) {
+    const char* const base = smem + (k & 1) * Tile::STAGE;
+    const char* const next = smem + ((k + 1) & 1) * Tile::STAGE;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      if (i < NB - 1) {
+        read_b(base, i + 1);
+        if (i) read_t(base, i);
+      } else {
+        // the step's last rows: all of it has been read, the next one has landed, and its loads' successors may go where it was
+        read_t(base, i);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        load(k & 1, k + 2 < nk ? k + 2 : nk - 1);      // (behind the end the last step again, so that the loop is one block of code)
+        read_b(next, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        const int q = i * MB + j;
+        c[q & 3] = block_product<CUT>(x[i & 1], y[j]);
+        add((q + PRODUCTS - LATE) % PRODUCTS);
+        if (q == LATE - 1) {
+#pragma unroll
+          for (int n = 0; n < MB; ++n) s[n] = s_next[n];
+          read_t(base, 0);
+        }
+        if (i == NB - 1) read_a(next, j);
+        __builtin_amdgcn_sched_barrier(0);             // (in this order: a place is free once it is used)
+      }
+    }
+  }
+#pragma unroll
+  for (int q = PRODUCTS - LATE; q < PRODUCTS; ++q) add(q);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (loads behind the end still write to this workgroup's LDS)
 #pragma unroll
   for (int j = 0; j < MB; ++j) {
     const int64_t m = m0 + wm * (MB * 16) + j * 16 + l;
