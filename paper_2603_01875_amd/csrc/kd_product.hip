@@ -92,7 +92,9 @@ __device__ __forceinline__ void store4(const ProductArgs& p, int64_t m, int64_t 
 //
 // WN x WM waves, each with NB x MB blocks of 16 x 16 results.  A k-step is one block of 128: the tile's rows of b and a, 128 bytes each, and
 // their scales, loaded straight into LDS while the step before is multiplied (two stages).  16-byte chunks of a row are permuted by
-// XOR with bits of its number, so that 16 rows' reads of one chunk fall into different banks.
+// XOR with bits of its number, and a lane takes chunks g and g + 4 (which of a block's codes an instruction contracts together does not
+// matter), so that the lanes that LDS serves at once read from different banks, in whichever order it takes them.  (Chunks 2 g and 2 g + 1: 25 k of 137 k
+// cycles in conflicts.)
 // ------------------------------------------------------------------------------------------------
 template <int NB_, int MB_, int WN_, int WM_>
 struct ProductTile {
@@ -105,48 +107,68 @@ struct ProductTile {
   static_assert(SMEM <= 160 * 1024, "LDS");
 };
 
+// Tile number q: rows of a in panels of 16 tiles, a panel's rows of b in strips of eight tiles, a strip four by eight after four by eight
+// (group_decode).  32 numbers, the workgroups of an XCD, so share what they load through its L2, and 256 of them, all workgroups,
+// 16 + 16 tiles' rows through the last-level cache: a b of any size comes from memory once for 4096 rows of a.
+__device__ __forceinline__ void tile_of(int q, int n_mt, int n_nt, int& tm, int& tn) {
+  const int panel = q / (16 * n_nt), m_first = panel * 16, m = n_mt - m_first < 16 ? n_mt - m_first : 16;
+  q -= panel * 16 * n_nt;
+  const int strip = q / (8 * m), n_first = strip * 8, n = n_nt - n_first < 8 ? n_nt - n_first : 8;
+  group_decode(q - strip * 8 * m, m, n, tm, tn);
+  tm += m_first;
+  tn += n_first;
+}
+
+// The tile that comes `round` rounds of the grid after a workgroup's first: its rows and what loads them.
+template <class Tile>
+struct TileRows {
+  int64_t n0, m0;
+  rsrc_t b, a, scales;      // scales: of b's or of a's rows, by the wave
+};
+
 template <class Tile, bool CUT, bool B_TILE>
-__global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArgs p) {
+__device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) {
   constexpr int NB = Tile::NB, MB = Tile::MB, NT = Tile::NT, BN = Tile::BN, BM = Tile::BM;
-  extern __shared__ __attribute__((aligned(128))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wn = wave % Tile::WN, wm = wave / Tile::WN;
   const int l = lane & 15, g = lane >> 4;
-  const int n_mt = (int)((p.M + BM - 1) / BM), n_nt = (int)((p.N + BN - 1) / BN);
-  int tm, tn;
-  group_decode(xcd_logical_id(blockIdx.x, gridDim.x), n_mt, n_nt, tm, tn);
-  const int64_t n0 = (int64_t)tn * BN, m0 = (int64_t)tm * BM;
-  const int ld = (int)((p.K + 15) / 16 * 16), nk = (int)((p.K + 127) / 128);
+  const int n_mt = (int)((p.M + BM - 1) / BM), n_nt = (int)((p.N + BN - 1) / BN), tiles = n_mt * n_nt;
+  const int ld = (int)((p.K + 15) / 16 * 16), nk = (int)((p.K + 127) / 128), steps = nk < 2 ? 2 : nk;
+  const int my = xcd_logical_id(blockIdx.x, gridDim.x), mine = (tiles - my + (int)gridDim.x - 1) / (int)gridDim.x;      // (the grid is not larger)
+  const bool b_scales = wave * 64 < BN;
+  static_assert(BN % 64 == 0 && Tile::SCALE_LOADS == 1, "a wave loads scales of one matrix");
 
-  // loads: thread tid has chunk tid % 8 (as stored) of rows tid / 8 + j LOAD_ROWS; rows behind the matrix give 0
+  auto rows_of = [&](int round) {
+    TileRows<Tile> r;
+    int tm, tn;
+    tile_of(my + round * (int)gridDim.x, n_mt, n_nt, tm, tn);
+    r.n0 = (int64_t)tn * BN;
+    r.m0 = (int64_t)tm * BM;
+    const int64_t n = p.N - r.n0 < BN ? p.N - r.n0 : BN, m = p.M - r.m0 < BM ? p.M - r.m0 : BM;
+    r.b = make_rsrc(p.b + r.n0 * ld, (uint32_t)(n * ld));
+    r.a = make_rsrc(p.a + r.m0 * ld, (uint32_t)(m * ld));
+    if (b_scales) r.scales = make_rsrc(p.b_scales + (B_TILE ? r.n0 / 128 : r.n0) * nk, (uint32_t)((B_TILE ? (n + 127) / 128 : n) * nk * 4));
+    else r.scales = make_rsrc(p.a_scales + r.m0 * nk, (uint32_t)(m * nk * 4));
+    return r;
+  };
+
+  // Loads of a step: thread tid has chunk tid % 8 (as stored) of rows tid / 8 + j LOAD_ROWS.  Rows behind the matrix and chunks behind a row's
+  // end are 0, and so are scales behind either.
+  constexpr uint32_t BEHIND = 0x80000000u;
   const int row = tid >> 3, chunk = (tid & 7) ^ ((row >> 1) & 7);
-  const int64_t n_rows = p.N - n0 < BN ? p.N - n0 : BN, m_rows = p.M - m0 < BM ? p.M - m0 : BM;
-  const rsrc_t rb = make_rsrc(p.b + n0 * ld, (uint32_t)(n_rows * ld)), ra = make_rsrc(p.a + m0 * ld, (uint32_t)(m_rows * ld));
   const uint32_t at = (uint32_t)row * ld + chunk * 16, step = (uint32_t)Tile::LOAD_ROWS * ld;
-  const float* scale[Tile::SCALE_LOADS];
-#pragma unroll
-  for (int j = 0; j < Tile::SCALE_LOADS; ++j) {
-    int i = j * NT + tid;
-    if (i < BN) {
-      const int64_t n = n0 + i < p.N ? n0 + i : p.N - 1;
-      scale[j] = p.b_scales + (B_TILE ? n / 128 : n) * nk;
-    } else {
-      const int64_t m = m0 + i - BN < p.M ? m0 + i - BN : p.M - 1;
-      scale[j] = p.a_scales + m * nk;
-    }
-  }
-  auto load = [&](int stage, int k) {
+  const int scale_row = b_scales ? (B_TILE ? tid / 128 : tid) : tid - BN;
+  const uint32_t scale_at = scale_row < (b_scales ? BN : BM) ? (uint32_t)scale_row * (nk * 4) : BEHIND;
+  auto load = [&](int stage, const TileRows<Tile>& r, int k) {
     char* const to = smem + stage * Tile::STAGE + wave * 1024;
-    const uint32_t from = at | (k * 128 + chunk * 16 < ld ? 0u : 0x80000000u);           // (a row's chunks behind its end: 0)
+    const uint32_t from = at | (k * 128 + chunk * 16 < ld ? 0u : BEHIND);
 #pragma unroll
     for (int j = 0; j < Tile::N_LOADS; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void_t*)(to + j * (NT * 16)), 16, from + j * step, k * 128, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r.b, (lds_void_t*)(to + j * (NT * 16)), 16, from + j * step, k * 128, 0, 0);
 #pragma unroll
     for (int j = 0; j < Tile::M_LOADS; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_t*)(to + BN * 128 + j * (NT * 16)), 16, from + j * step, k * 128, 0, 0);
-#pragma unroll
-    for (int j = 0; j < Tile::SCALE_LOADS; ++j)
-      __builtin_amdgcn_global_load_lds((const void*)(scale[j] + k), (lds_void_t*)(smem + stage * Tile::STAGE + (BN + BM) * 128 + j * (NT * 4) + wave * 256),
-                                       4, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r.a, (lds_void_t*)(to + BN * 128 + j * (NT * 16)), 16, from + j * step, k * 128, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r.scales, (lds_void_t*)(smem + stage * Tile::STAGE + (BN + BM) * 128 + wave * 256), 4,
+                                             scale_at | (k < nk ? 0u : BEHIND), k * 4, 0, 0);
   };
 
   f32x4 acc[NB][MB];
@@ -155,7 +177,7 @@ __global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArg
 #pragma unroll
     for (int j = 0; j < MB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int sw = (l >> 1) & 7, c0 = ((2 * g) ^ sw) * 16, c1 = ((2 * g + 1) ^ sw) * 16;
+  const int sw = (l >> 1) & 7, c0 = (g ^ sw) * 16, c1 = ((g + 4) ^ sw) * 16;
   auto read = [&](const char* rows, int block) {
     const char* const r = rows + (block * 16 + l) * 128;
     return codes_from<CUT>(*(const u32x4*)(r + c0), *(const u32x4*)(r + c1));
@@ -176,7 +198,7 @@ __global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArg
   };
   // A product's result is scaled and added three products later, so that nothing waits for the matrix pipe.
   constexpr int PRODUCTS = NB * MB, LATE = 3;
-  static_assert(NB % 2 == 0 && PRODUCTS % 4 == 0 && MB > LATE / NB && PRODUCTS > 4, "places of x, t and c");
+  static_assert(NB % 2 == 0 && PRODUCTS % 4 == 0 && PRODUCTS > 4, "places of x, t and c");
   f32x4 c[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) c[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -187,28 +209,20 @@ __global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArg
     for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(c[q & 3][r], B_TILE ? s[j] : s[j] * t[i & 1][r], acc[i][j][r]);
   };
 
-  load(0, 0);
-  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-  load(1, nk > 1 ? 1 : 0);
-#pragma unroll
-  for (int j = 0; j < MB; ++j) {
-    read_a(smem, j);
-    s[j] = 0.f;
-  }
-  read_b(smem, 0);
-  for (int k = 0; k < nk; ++k) {
-    const char* const base = smem + (k & 1) * Tile::STAGE;
-    const char* const next = smem + ((k + 1) & 1) * Tile::STAGE;
+  int stage = 0;
+  // One step; the loads of the one after the next go where it was.
+  auto multiply = [&](const TileRows<Tile>& r, int k_load) {
+    const char* const base = smem + stage * Tile::STAGE;
+    const char* const next = smem + (stage ^ 1) * Tile::STAGE;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       if (i < NB - 1) {
-        read_b(base, i + 1);
         if (i) read_t(base, i);
       } else {
-        // the step's last rows: all of it has been read, the next one has landed, and its loads' successors may go where it was
+        // the step's last rows: all of it has been read, and the next one has landed
         read_t(base, i);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        load(k & 1, k + 2 < nk ? k + 2 : nk - 1);      // (behind the end the last step again, so that the loop is one block of code)
+        load(stage, r, k_load);
         read_b(next, 0);
       }
 #pragma unroll
@@ -222,33 +236,78 @@ __global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArg
           read_t(base, 0);
         }
         if (i == NB - 1) read_a(next, j);
+        else if (j == 0) read_b(base, i + 1);
         __builtin_amdgcn_sched_barrier(0);             // (in this order: a place is free once it is used)
       }
     }
-  }
-#pragma unroll
-  for (int q = PRODUCTS - LATE; q < PRODUCTS; ++q) add(q);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (loads behind the end still write to this workgroup's LDS)
+    stage ^= 1;
+  };
+
+  TileRows<Tile> rows = rows_of(0);
+  load(0, rows, 0);
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  load(1, rows, 1);
 #pragma unroll
   for (int j = 0; j < MB; ++j) {
-    const int64_t m = m0 + wm * (MB * 16) + j * 16 + l;
-    if (m >= p.M) continue;
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int64_t n = n0 + wn * (NB * 16) + i * 16 + 4 * g;
-      if (n < p.N) store4(p, m, n, acc[i][j]);
-    }
+    read_a(smem, j);
+    s[j] = 0.f;
   }
+  read_b(smem, 0);
+  for (int round = 0; round < mine; ++round) {
+    for (int k = 2; k < steps; ++k) multiply(rows, k);
+    const int64_t n0 = rows.n0, m0 = rows.m0;
+    if (round + 1 < mine) rows = rows_of(round + 1);   // (behind the last tile its own first steps again)
+    multiply(rows, 0);
+    multiply(rows, 1);
+#pragma unroll
+    for (int q = PRODUCTS - LATE; q < PRODUCTS; ++q) {
+      add(q);
+      c[q & 3] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // (what the next tile's first sums add is 0 times these, which may be NaN)
+#pragma unroll
+    for (int j = 0; j < MB; ++j) s[j] = 0.f;
+    t[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (!p.out_f32 && !p.accumulate && n0 + BN <= p.N && m0 + BM <= p.M) {
+      global_t o = (global_t)((uint16_t*)p.out + (m0 + wm * (MB * 16) + l) * p.N + n0 + wn * (NB * 16) + 4 * g);
+#pragma unroll
+      for (int j = 0; j < MB; ++j, o += 32 * p.N)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) store8(o + i * 32, u32x2_t{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])});
+    } else {
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        const int64_t m = m0 + wm * (MB * 16) + j * 16 + l;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const int64_t n = n0 + wn * (NB * 16) + i * 16 + 4 * g;
+          if (m < p.M && n < p.N) store4(p, m, n, acc[i][j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < MB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (loads behind the end still write to this workgroup's LDS)
+}
+
+template <class Tile, bool CUT, bool B_TILE>
+__global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArgs p) {
+  extern __shared__ __attribute__((aligned(128))) char smem[];
+  product_tiles<Tile, CUT, B_TILE>(p, smem);
 }
 
 template <class Tile, bool CUT>
 static hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
   const int64_t tiles = (p.M + Tile::BM - 1) / Tile::BM * ((p.N + Tile::BN - 1) / Tile::BN);
-  if (tiles > INT32_MAX / Tile::NT) return hipErrorInvalidValue;
+  if (tiles > INT32_MAX / 2) return hipErrorInvalidValue;
+  constexpr int resident = 160 * 1024 / Tile::SMEM * kNumCU;
+  const int grid = tiles < resident ? (int)tiles : resident;
   void* args = const_cast<ProductArgs*>(&p);
-  void* params[] = {args};
-  return p.b_tile ? launch_big<product_tile_kernel<Tile, CUT, true>>((int)tiles, Tile::NT, Tile::SMEM, st, params[0])
-                  : launch_big<product_tile_kernel<Tile, CUT, false>>((int)tiles, Tile::NT, Tile::SMEM, st, params[0]);
+  return p.b_tile ? launch_big<product_tile_kernel<Tile, CUT, true>>(grid, Tile::NT, Tile::SMEM, st, args)
+                  : launch_big<product_tile_kernel<Tile, CUT, false>>(grid, Tile::NT, Tile::SMEM, st, args);
 }
 
 hipError_t launch_product(const ProductArgs& p, hipStream_t st) {

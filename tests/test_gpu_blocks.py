@@ -128,6 +128,33 @@ def test_product(M, N, K_, tile, out):
     check_product(into, ref, size, K_, out, before)
 
 
+@pytest.mark.parametrize("tile", [True, False])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K_", [(4096, 5000, 128), (4000, 4800, 100), (2300, 9000, 272), (20_000, 300, 130)])
+def test_more_tiles_than_workgroups(M, N, K_, tile, out):
+    """Workgroups that take several tiles, each with the loads of the next under way: a row of tiles with scales of NaN touches nothing
+    but itself."""
+    a = K.quantize_e4m3_blocks(matrix(M, M, K_, "f32", 1.0).cuda())
+    b = K.quantize_e4m3_blocks(matrix(N, N, K_, "f32", 1.0).cuda(), K.BLOCK_TILE if tile else K.BLOCK_ROW)
+    a.scales[300:301] = float("nan")
+    b.scales[1, -1] = float("nan")
+    y = K.kd_matmul_e4m3(a, b, out_dtype=K.F32 if out == "f32" else K.BF16)
+    bad = torch.zeros(M, N, dtype=torch.bool)
+    bad[300] = True
+    bad[:, 128:256 if tile else 129][:, :] = True
+    if not tile:
+        bad[:, 128:] = False
+        bad[:, 1] = True
+        bad[300] = True
+    assert torch.equal(torch.isnan(y).cpu(), bad)
+    rows = [0, 1, 255, 256, 299, M // 2, M - 1]
+    some = K.E4m3Blocks(a.codes[rows], a.scales[rows], K.BLOCK_ROW)
+    b.scales[1, -1] = 0.0
+    ref, size = reference(some, b, K_, tile)
+    good = ~bad[rows].numpy()
+    check_product(torch.where(torch.from_numpy(good), y[rows].cpu(), 0.0), np.where(good, ref, 0), np.where(good, size, 0), K_, out)
+
+
 @pytest.mark.parametrize("M,N,K_,dtype,out", [(1, 1000, 512, "bf16", "f32"), (2, 48, 1000, "f32", "f32"), (9, 515, 200, "bf16", "bf16"),
                                               (16, 1024, 1024, "bf16", "f32"), (31, 130, 77, "f32", "bf16"), (65, 300, 640, "bf16", "f32"),
                                               (300, 200, 250, "f32", "f32"), (1, 256, 8192, "f32", "f32"), (8, 151936, 64, "bf16", "bf16")])
