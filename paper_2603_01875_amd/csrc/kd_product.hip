@@ -102,7 +102,8 @@ struct ProductTile {
   static constexpr int LOAD_ROWS = NT / 8;                                  // rows of one 16-byte load a thread
   static constexpr int N_LOADS = BN / LOAD_ROWS, M_LOADS = BM / LOAD_ROWS;
   static constexpr int SCALES = BN + BM, SCALE_LOADS = (SCALES + NT - 1) / NT;
-  static constexpr int STAGE = (BN + BM) * 128 + SCALE_LOADS * NT * 4, SMEM = 2 * STAGE;
+  static constexpr int STAGE = (BN + BM) * 128 + SCALE_LOADS * NT * 4;
+  static constexpr int OUT_ROW = 144, OUT = 16 * OUT_ROW, SMEM = 2 * STAGE + WN * WM * OUT;      // OUT: where a wave turns results into rows
   static_assert(BN % LOAD_ROWS == 0 && BM % LOAD_ROWS == 0 && LOAD_ROWS % 16 == 0, "whole loads, one permutation a thread");
   static_assert(SMEM <= 160 * 1024, "LDS");
 };
@@ -198,7 +199,7 @@ __device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) 
   };
   // A product's result is scaled and added three products later, so that nothing waits for the matrix pipe.
   constexpr int PRODUCTS = NB * MB, LATE = 3;
-  static_assert(NB % 2 == 0 && PRODUCTS % 4 == 0 && PRODUCTS > 4, "places of x, t and c");
+  static_assert(NB % 4 == 0 && PRODUCTS % 4 == 0 && PRODUCTS > 4, "places of x, t and c");
   f32x4 c[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) c[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -269,11 +270,21 @@ __device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) 
     for (int j = 0; j < MB; ++j) s[j] = 0.f;
     t[1] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (!p.out_f32 && !p.accumulate && n0 + BN <= p.N && m0 + BM <= p.M) {
-      global_t o = (global_t)((uint16_t*)p.out + (m0 + wm * (MB * 16) + l) * p.N + n0 + wn * (NB * 16) + 4 * g);
+      // 16 rows x 64 results at a time through LDS, so that a row's 128 bytes go out together (32 at a time, as a lane has them, cost
+      // 340 of 2520 us at T = 4096, H = 4096, V = 151936)
+      char* const turn = smem + 2 * Tile::STAGE + wave * Tile::OUT;
+      global_t o = (global_t)((uint16_t*)p.out + (m0 + wm * (MB * 16) + (lane >> 3)) * p.N + n0 + wn * (NB * 16) + (lane & 7) * 8);
 #pragma unroll
       for (int j = 0; j < MB; ++j, o += 32 * p.N)
 #pragma unroll
-        for (int i = 0; i < NB; ++i) store8(o + i * 32, u32x2_t{bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3])});
+        for (int h = 0; h < NB; h += 4) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *(u32x2_t*)(turn + l * Tile::OUT_ROW + i * 32 + g * 8) = u32x2_t{bf16_pair(acc[h + i][j][0], acc[h + i][j][1]), bf16_pair(acc[h + i][j][2], acc[h + i][j][3])};
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            store16(o + r * 16 * p.N + h * 32, *(const u32x4_t*)(turn + ((lane >> 3) + 8 * r) * Tile::OUT_ROW + (lane & 7) * 16));
+        }
     } else {
 #pragma unroll
       for (int j = 0; j < MB; ++j) {
