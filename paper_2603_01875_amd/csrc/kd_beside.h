@@ -25,6 +25,9 @@ struct ProductArgs {
   int out_f32, b_tile, accumulate;
 };
 hipError_t launch_product(const ProductArgs& p, hipStream_t st);
+// whether a is so small that the product's workgroups quantise it themselves; p.a and p.a_scales are then not read
+bool product_quantises(int64_t M, int64_t K);
+hipError_t launch_linear_few(const ProductArgs& p, const void* x, int x_f32, hipStream_t st);
 
 // ---- rows of logits ----
 // A workgroup of the first kernel reads kRowThreads * per_thread entries of a row, a chunk.  Each thread leaves the largest key of its

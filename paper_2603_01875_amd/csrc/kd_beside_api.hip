@@ -233,6 +233,10 @@ kd_status kd_linear_e4m3(const kd_linear_params* params, const void* x, const ui
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   uint8_t* const codes = static_cast<uint8_t*>(workspace) + L.codes;
   float* const scales = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.scales);
+  if (kd::product_quantises(params->M, params->K)) {
+    KD_TRY(kd::launch_linear_few(product_args(*params, nullptr, nullptr, w, w_scales, out), x, params->in_dtype == KD_F32, st));
+    return KD_OK;
+  }
   const kd::BlocksArgs q{x, params->M, params->K, params->K, params->in_dtype == KD_F32, 0, codes, nullptr, scales, nullptr};
   KD_TRY(kd::launch_quantize_blocks(q, st));
   KD_TRY(kd::launch_product(product_args(*params, codes, scales, w, w_scales, out), st));

@@ -106,16 +106,16 @@ __device__ __forceinline__ bf16_t part_of(float f, int part) {
 
 // Launch of a kernel that needs more dynamic LDS than the default limit.  The limit is a property of
 // the kernel on a device: it is raised once per kernel and device (one flag word per instantiation,
-// one bit per device), not on every launch.
+// one bit per device), not on every launch: to `most_bytes` for a kernel whose launches take different amounts.
 template <auto Kern>
-static hipError_t launch_big(int grid, int threads, int smem_bytes, hipStream_t st, const void* args_ptr) {
+static hipError_t launch_big(int grid, int threads, int smem_bytes, hipStream_t st, const void* args_ptr, int most_bytes = 0) {
   static std::atomic<uint64_t> attr_done{0};
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(attr_done.load(std::memory_order_acquire) & bit)) {
-    e = hipFuncSetAttribute((const void*)Kern, hipFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
+    e = hipFuncSetAttribute((const void*)Kern, hipFuncAttributeMaxDynamicSharedMemorySize, most_bytes ? most_bytes : smem_bytes);
     if (e != hipSuccess) return e;
     attr_done.fetch_or(bit, std::memory_order_release);
   }

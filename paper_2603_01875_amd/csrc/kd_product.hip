@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include "kd_beside.h"
+#include "kd_blocks.hpp"
 #include "kd_common.hpp"
 #include "kd_launch.h"
 #include "kd_unaligned.hpp"
@@ -53,7 +54,7 @@ __device__ __forceinline__ f32x4 block_product(const Codes<CUT>& x, const Codes<
   return c;
 }
 
-// four results of one row m, columns n .. n + 3 (at most N)
+// four results of one row m, columns n .. n + 3 (at most N), as a lane has them
 __device__ __forceinline__ void store4(const ProductArgs& p, int64_t m, int64_t n, f32x4 v) {
   const int64_t at = m * p.N + n;
   if (n + 4 <= p.N) {
@@ -84,6 +85,24 @@ __device__ __forceinline__ void store4(const ProductArgs& p, int64_t m, int64_t 
       uint16_t* const o = (uint16_t*)p.out + at + i;
       *o = bf16_bits(v[i] + (p.accumulate ? bf16_float(*o) : 0.f));
     }
+  }
+}
+
+// 16 bytes of results of row m from column n on, as far as they are in the matrix
+template <bool F32>
+__device__ __forceinline__ void store_row(const ProductArgs& p, int64_t m, int64_t n, u32x4_t v) {
+  constexpr int VE = F32 ? 4 : 8;
+  if (m >= p.M || n >= p.N) return;
+  const global_t o = (global_t)p.out + (m * p.N + n) * (F32 ? 4 : 2);
+  if (n + VE <= p.N) {
+    store16(o, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < VE; ++i) {
+    if (n + i >= p.N) break;
+    if (F32) ((KD_GLOBAL uint32_t*)o)[i] = v[i % 4];
+    else ((KD_GLOBAL uint16_t*)o)[i] = (uint16_t)(v[i / 2 % 4] >> (16 * (i & 1)));
   }
 }
 
@@ -269,32 +288,34 @@ __device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) 
 #pragma unroll
     for (int j = 0; j < MB; ++j) s[j] = 0.f;
     t[1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (!p.out_f32 && !p.accumulate && n0 + BN <= p.N && m0 + BM <= p.M) {
-      // 16 rows x 64 results at a time through LDS, so that a row's 128 bytes go out together (32 at a time, as a lane has them, cost
-      // 340 of 2520 us at T = 4096, H = 4096, V = 151936)
-      char* const turn = smem + 2 * Tile::STAGE + wave * Tile::OUT;
-      global_t o = (global_t)((uint16_t*)p.out + (m0 + wm * (MB * 16) + (lane >> 3)) * p.N + n0 + wn * (NB * 16) + (lane & 7) * 8);
+    if (p.accumulate) {
 #pragma unroll
-      for (int j = 0; j < MB; ++j, o += 32 * p.N)
-#pragma unroll
-        for (int h = 0; h < NB; h += 4) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *(u32x2_t*)(turn + l * Tile::OUT_ROW + i * 32 + g * 8) = u32x2_t{bf16_pair(acc[h + i][j][0], acc[h + i][j][1]), bf16_pair(acc[h + i][j][2], acc[h + i][j][3])};
-#pragma unroll
-          for (int r = 0; r < 2; ++r)
-            store16(o + r * 16 * p.N + h * 32, *(const u32x4_t*)(turn + ((lane >> 3) + 8 * r) * Tile::OUT_ROW + (lane & 7) * 16));
-        }
-    } else {
-#pragma unroll
-      for (int j = 0; j < MB; ++j) {
-        const int64_t m = m0 + wm * (MB * 16) + j * 16 + l;
+      for (int j = 0; j < MB; ++j)
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-          const int64_t n = n0 + wn * (NB * 16) + i * 16 + 4 * g;
+          const int64_t m = m0 + wm * (MB * 16) + j * 16 + l, n = n0 + wn * (NB * 16) + i * 16 + 4 * g;
           if (m < p.M && n < p.N) store4(p, m, n, acc[i][j]);
         }
-      }
+    } else {
+      // 16 rows at a time through LDS, so that 128 bytes of a row go out together (32 at a time, as a lane has them, cost 340 of 2520 us
+      // at T = 4096, H = 4096, V = 151936)
+      constexpr int BLOCKS = CUT ? 4 : 2, VE = CUT ? 8 : 4;
+      char* const turn = smem + 2 * Tile::STAGE + wave * Tile::OUT;
+      const int64_t m = m0 + wm * (MB * 16) + (lane >> 3), n = n0 + wn * (NB * 16) + (lane & 7) * VE;
+#pragma unroll
+      for (int j = 0; j < MB; ++j)
+#pragma unroll
+        for (int h = 0; h < NB; h += BLOCKS) {
+#pragma unroll
+          for (int i = 0; i < BLOCKS; ++i) {
+            const f32x4& v = acc[h + i][j];
+            if (CUT) *(u32x2_t*)(turn + l * Tile::OUT_ROW + i * 32 + g * 8) = u32x2_t{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+            else *(f32x4*)(turn + l * Tile::OUT_ROW + i * 64 + g * 16) = v;
+          }
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            store_row<!CUT>(p, m + j * 16 + r * 8, n + h * 16, *(const u32x4_t*)(turn + ((lane >> 3) + 8 * r) * Tile::OUT_ROW + (lane & 7) * 16));
+        }
     }
 #pragma unroll
     for (int i = 0; i < NB; ++i)
@@ -321,7 +342,157 @@ static hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
                   : launch_big<product_tile_kernel<Tile, CUT, false>>(grid, Tile::NT, Tile::SMEM, st, args);
 }
 
+// ------------------------------------------------------------------------------------------------
+// few rows of a (at most 16 MB)
+//
+// b is read once, straight into registers, each wave 16 rows of it and a lane 32 codes of a block at a time; a's codes lie in LDS,
+// quantised by the workgroup itself where they are few (QUANT).  WK of the workgroup's eight waves share the blocks of 16 rows of b
+// and join their sums through LDS in a fixed order.
+// ------------------------------------------------------------------------------------------------
+constexpr int kFewWaves = 8, kFewBlocks = 4;      // waves; blocks of b that a wave has in flight
+constexpr int kFewSmem = 128 * 1024;              // most LDS
+struct FewArgs {
+  ProductArgs p;
+  const void* x;                                  // QUANT: a in bf16 or fp32
+  int x_f32, wk;
+};
+inline int64_t few_row(int64_t K) { return (K + 127) / 128 * 128 + 16; }      // (16 rows' reads of a chunk fall into different banks)
+inline int64_t few_smem(int64_t M, int64_t K, int mb) {
+  const int64_t blocks = (K + 127) / 128, codes = M * few_row(K), scales = (M * blocks * 4 + 15) / 16 * 16;
+  return codes + scales + kFewWaves * mb * 1024;
+}
+
+template <int MB, bool CUT, bool B_TILE, bool QUANT>
+__global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(const FewArgs f) {
+  extern __shared__ __attribute__((aligned(128))) char smem[];
+  const ProductArgs& p = f.p;
+  constexpr int NT = 64 * kFewWaves, U = kFewBlocks;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l = lane & 15, g = lane >> 4;
+  const int M = (int)p.M, ld = (int)((p.K + 15) / 16 * 16), nk = (int)((p.K + 127) / 128), row = nk * 128 + 16;
+  char* const codes = smem;
+  float* const scales = (float*)(smem + M * row);
+  char* const joined = smem + M * row + (M * nk * 4 + 15) / 16 * 16;
+  if (QUANT) {
+    // 16 lanes a block of 128, eight values each
+    for (int i = tid / 16; i < M * nk; i += NT / 16) {
+      const int m = i / nk, j = i - m * nk, c = j * 128 + (tid & 15) * 8;
+      float x[8];
+      if (f.x_f32) load_row8<true>(x, (const float*)f.x + (int64_t)m * p.K, c, p.K);
+      else load_row8<false>(x, (const uint16_t*)f.x + (int64_t)m * p.K, c, p.K);
+      float top = kLeastBlock;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = block_max(top, fabsf(x[e]));
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) top = block_max(top, __shfl_xor(top, o, 64));
+      float tops[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tops[e] = top;
+      *(uint2*)(codes + m * row + c) = codes_of(x, tops);
+      if ((tid & 15) == 0) scales[i] = scale_of(top);
+    }
+  } else {
+    for (int i = tid; i < M * nk * 8; i += NT) {
+      const int m = i / (nk * 8), c = (i - m * nk * 8) * 16;
+      *(u32x4_t*)(codes + m * row + c) = c < ld ? *(const u32x4_t*)(p.a + (int64_t)m * ld + c) : u32x4_t{0, 0, 0, 0};
+    }
+    for (int i = tid; i < M * nk; i += NT) scales[i] = p.a_scales[i];
+  }
+  __syncthreads();
+
+  const int wk = f.wk, wn = kFewWaves / wk, my_k = wave % wk, my_n = wave / wk;
+  const int64_t groups = (p.N + 15) / 16;
+  const int64_t group = (int64_t)blockIdx.x * wn + my_n;
+  const int64_t n0 = (group < groups ? group : groups - 1) * 16;
+  const uint8_t* const b = p.b + (n0 + l < p.N ? n0 + l : p.N - 1) * ld + g * 16;
+  const float* const sb = p.b_scales + (B_TILE ? n0 / 128 : n0) * nk;
+  const int parts = (nk + U - 1) / U;
+  f32x4 acc[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 next[2 * U];
+  auto fetch = [&](int part) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = (part * U + u) * 128 + h * 64;
+        next[2 * u + h] = k + g * 16 < ld ? *(const u32x4*)(b + k) : u32x4{0, 0, 0, 0};
+      }
+  };
+  int a_row[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) a_row[i] = i * 16 + l < M ? i * 16 + l : M - 1;
+  fetch(my_k < parts ? my_k : parts - 1);
+  for (int part = my_k; part < parts; part += wk) {
+    u32x4 now[2 * U];
+#pragma unroll
+    for (int u = 0; u < 2 * U; ++u) now[u] = next[u];
+    if (part + wk < parts) fetch(part + wk);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = part * U + u;
+      if (k >= nk) break;
+      const Codes<CUT> x = codes_from<CUT>(now[2 * u], now[2 * u + 1]);
+      f32x4 t;
+      if (!B_TILE)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) t[r] = sb[(n0 + 4 * g + r < p.N ? 4 * g + r : 0) * nk + k];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const char* const a = codes + a_row[i] * row + k * 128 + g * 16;
+        const f32x4 c = block_product<CUT>(x, codes_from<CUT>(*(const u32x4*)a, *(const u32x4*)(a + 64)));
+        float s = scales[a_row[i] * nk + k];
+        if (B_TILE) s *= sb[k];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[i][r] = fmaf(c[r], B_TILE ? s : s * t[r], acc[i][r]);
+      }
+    }
+  }
+  if (wk > 1) {
+    f32x4* const to = (f32x4*)joined;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) to[(wave * MB + i) * 64 + lane] = acc[i];
+    __syncthreads();
+    if (my_k) return;
+    for (int w = 1; w < wk; ++w)
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const f32x4 v = to[((wave + w) * MB + i) * 64 + lane];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[i][r] += v[r];
+      }
+  }
+  if (group >= groups) return;
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+    if (i * 16 + l < M && n0 + 4 * g < p.N) store4(p, i * 16 + l, n0 + 4 * g, acc[i]);
+}
+
+template <int MB, bool CUT>
+static hipError_t launch_few_of(const FewArgs& f, int grid, int smem, hipStream_t st) {
+  void* args = const_cast<FewArgs*>(&f);
+  if (f.x) return launch_big<product_few_kernel<MB, CUT, true, true>>(grid, 64 * kFewWaves, smem, st, args, kFewSmem);
+  return f.p.b_tile ? launch_big<product_few_kernel<MB, CUT, true, false>>(grid, 64 * kFewWaves, smem, st, args, kFewSmem)
+                    : launch_big<product_few_kernel<MB, CUT, false, false>>(grid, 64 * kFewWaves, smem, st, args, kFewSmem);
+}
+
+static hipError_t launch_few(const ProductArgs& p, const void* x, int x_f32, hipStream_t st) {
+  const int mb = p.M <= 16 ? 1 : 2;
+  const int64_t groups = (p.N + 15) / 16;
+  int wk = kFewWaves;
+  while (wk > 1 && (groups * wk > 4 * kNumCU * kFewWaves || (wk / 2) * kFewBlocks * 128 >= p.K)) wk >>= 1;
+  const FewArgs f{p, x, x_f32, wk};
+  const int wn = kFewWaves / wk, grid = (int)((groups + wn - 1) / wn), smem = (int)few_smem(p.M, p.K, mb);
+  if (mb == 1) return p.out_f32 ? launch_few_of<1, false>(f, grid, smem, st) : launch_few_of<1, true>(f, grid, smem, st);
+  return p.out_f32 ? launch_few_of<2, false>(f, grid, smem, st) : launch_few_of<2, true>(f, grid, smem, st);
+}
+
+bool product_is_few(int64_t M, int64_t K) { return M <= 32 && few_smem(M, K, M <= 16 ? 1 : 2) <= kFewSmem; }
+bool product_quantises(int64_t M, int64_t K) { return product_is_few(M, K) && M * K <= 8192; }
+hipError_t launch_linear_few(const ProductArgs& p, const void* x, int x_f32, hipStream_t st) { return launch_few(p, x, x_f32, st); }
+
 hipError_t launch_product(const ProductArgs& p, hipStream_t st) {
+  if (product_is_few(p.M, p.K)) return launch_few(p, nullptr, 0, st);
   if (p.out_f32) return launch_tiles<ProductTile<4, 4, 2, 2>, false>(p, st);
   const int64_t big = (p.M + 255) / 256 * ((p.N + 255) / 256);
   if (big >= kNumCU) return launch_tiles<ProductTile<8, 4, 2, 4>, true>(p, st);

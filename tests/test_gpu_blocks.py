@@ -108,7 +108,8 @@ def check_product(y, ref, size, K_, dtype, before=None):
 
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 300, 256), (3, 17, 100), (8, 128, 1024), (16, 130, 272), (17, 64, 640), (33, 257, 384), (64, 100, 2000),
          (100, 1000, 128), (128, 256, 512), (129, 255, 144), (200, 520, 1040), (257, 515, 333), (300, 31, 4096), (500, 777, 1000),
-         (513, 1024, 896), (1, 4096, 4096), (5, 2048, 8192)]
+         (513, 1024, 896), (1, 4096, 4096), (5, 2048, 8192),
+         (13, 5000, 8192), (16, 16, 16), (17, 40, 30_000), (32, 1000, 3000), (2, 33_000, 256), (1, 15, 100_000), (31, 300, 4080)]
 
 
 @pytest.mark.parametrize("M,N,K_", SIZES)
