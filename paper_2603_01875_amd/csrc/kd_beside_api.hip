@@ -279,6 +279,9 @@ kd_status kd_sample(const kd_sample_params* params, const void* logits, const fl
   r.logits = logits; r.u = u; r.token = token; r.logp = logp;
   r.temperature_rows = temperature_rows; r.top_k_rows = top_k_rows; r.top_p_rows = top_p_rows; r.min_p_rows = min_p_rows;
   carve(r, L, workspace);
+  // (who draws from all entries needs no groups)
+  const bool same = !temperature_rows && !top_k_rows && !top_p_rows && !min_p_rows;
+  if (same && r.tau > 0.f && (r.top_k == 0 || r.top_k >= r.V) && r.top_p == 1.f && r.min_p == 0.f) r.group = nullptr;
   KD_TRY(kd::launch_sample(r, static_cast<hipStream_t>(hip_stream)));
   return KD_OK;
 }

@@ -35,32 +35,32 @@ __device__ __forceinline__ const void* row_of(const RowsArgs& a, int64_t t) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// w = 2^(t / 32) in 64 bits, as a whole number of 2^-bits
+// w = 2^t in 64 bits, t <= 0, times 2^bits
 //
-// t / 32 = n / 32 + r with a whole number n and |r| <= 1/64: 2^(n / 32) is one of 32 table entries (256 bytes of LDS: every bank once, any 64 lanes read
-// them without a conflict) and a shift, 2^r four terms of its series, off by (ln 2 / 64)^5 / 120 = 2^-39.6 at most.  Adding 2^52 leaves the rounded whole
-// number in the low bits.  (An exp in 32 bits would be off by 2^-24 in every sum that a uniform number is compared with: one token in some
-// thousand would be another one.)
+// t = n + x with a whole number n and |x| <= 1/2; 2^x is the polynomial of degree 8 that meets it at the Chebyshev nodes of [-1/2, 1/2] (1 at 0; off by
+// 2^-39.7 at most), 2^n is added to its exponent.  n comes out of the low bits of t + 1.5 2^52: no conversion, no table.  13 instructions in 64 bits; an exp
+// in 32 bits would be off by 2^-24 in every sum that a uniform number is compared with: one token in some thousand would be another one.
 // ------------------------------------------------------------------------------------------------
-constexpr double kLn2 = 0.693147180559945309417, kLog2e = 1.44269504088896340736;
-constexpr double kC1 = kLn2 / 32, kC2 = kC1 * kC1 / 2, kC3 = kC2 * kC1 / 3, kC4 = kC3 * kC1 / 4;
+constexpr double kLog2e = 1.44269504088896340736;
 constexpr int kChunkBits = 48;         // a chunk's sums: 2^14 entries of at most 2^48
 
-__device__ __forceinline__ void fill_table(double* tab) {
-  if (threadIdx.x < 32) tab[threadIdx.x] = exp2((double)threadIdx.x / 32);
-  __syncthreads();
+__device__ __forceinline__ double weight(double t, int bits) {
+  t = fmax(t, -80.);                                   // (2^-80 and less count as nothing; also for a NaN, where a chunk is empty)
+  const double m = t + 0x1.8p52, x = t - (m - 0x1.8p52);
+  double p = 0x1.63d1363930791p-20;
+  p = fma(p, x, 0x1.00dc4a53395d3p-16);
+  p = fma(p, x, 0x1.4308ac85a7718p-13);
+  p = fma(p, x, 0x1.5d8745a72831bp-10);
+  p = fma(p, x, 0x1.3b2ab7181b778p-7);
+  p = fma(p, x, 0x1.c6b08dd6fd236p-5);
+  p = fma(p, x, 0x1.ebfbdff823cedp-3);
+  p = fma(p, x, 0x1.62e42fef84cf0p-1);
+  p = fma(p, x, 1.);
+  const uint64_t v = __double_as_longlong(p);
+  const uint32_t high = (uint32_t)(v >> 32) + (((uint32_t)__double_as_longlong(m) + (uint32_t)bits) << 20);
+  return __longlong_as_double((long long)((uint64_t)high << 32 | (uint32_t)v));
 }
-__device__ __forceinline__ uint64_t weight(double t, const double* tab, int bits) {
-  t = fmax(t, -2560.);                                 // 2^-80 and less: 0 (also for a NaN, where a chunk is empty)
-  const double n = rint(t), r = t - n;
-  const int k = (int)n;
-  double p = fma(r, kC4, kC3);
-  p = fma(r, p, kC2);
-  p = fma(r, p, kC1);
-  p = fma(r, p, 1.);
-  const double v = ldexp(p * tab[k & 31], (k >> 5) + bits);
-  return __double_as_longlong(v + 0x1p52) - 0x4330000000000000ll;
-}
+__device__ __forceinline__ uint64_t whole(double v) { return (uint64_t)rint(v); }
 
 // ------------------------------------------------------------------------------------------------
 // first kernel
@@ -71,7 +71,6 @@ template <bool F32, int E, bool SAMPLE>
 __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a) {
   constexpr int VE = F32 ? 4 : 8, J = E / VE, NT = kRowThreads, NW = NT / 64;
   static_assert(E % VE == 0, "whole loads");
-  __shared__ double tab[32];
   __shared__ uint32_t keys[NW];
   __shared__ uint64_t sums[NW];
   const int64_t piece = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, t = piece / a.chunks;
@@ -111,12 +110,11 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
     m = fmaxf(m, z[i]);
   }
   uint32_t key = nan ? kKeyNaN : key_of(m);
-  a.group[t * ((int64_t)a.chunks * NT) + c * NT + tid] = key;
+  if (!SAMPLE || a.group) a.group[t * ((int64_t)a.chunks * NT) + c * NT + tid] = key;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) key = max(key, (uint32_t)__shfl_xor((int)key, o, 64));
   if ((tid & 63) == 0) keys[tid >> 6] = key;
-  if (SAMPLE) fill_table(tab);         // (and the barrier)
-  else __syncthreads();
+  __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) key = max(key, keys[w]);
   const float top = value_of(key);
@@ -125,9 +123,11 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
     const float tau = row_temperature(a, t);
     uint64_t s = 0;
     if (tau > 0.f) {
-      const double scale = 32 * kLog2e / (double)tau, zero = (double)top;
+      const double scale = kLog2e / (double)tau, zero = (double)top;
+      double w = 0;
 #pragma unroll
-      for (int i = 0; i < E; ++i) s += weight(((double)z[i] - zero) * scale, tab, kChunkBits);
+      for (int i = 0; i < E; ++i) w += weight(((double)z[i] - zero) * scale, kChunkBits);
+      s = whole(w);
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) s += __shfl_xor((unsigned long long)s, o, 64);
@@ -156,23 +156,30 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
 // second kernel: pieces
 // ------------------------------------------------------------------------------------------------
 constexpr int kSelect = 512;           // threads
-constexpr int kList = 8192;            // entries of the list at most
-constexpr int kTile = kSelect * 8;     // entries that a pass of the slow way takes at a time
-constexpr int kSlots = 4096;           // tiles of a row at most
+constexpr int kList = 4096;            // entries of the list at most
+constexpr int kGroups = 1536;          // groups that are read again at most
+constexpr int kNear = 1792;            // bins by the distance from the largest key
+constexpr int kFlat = 2048;            // bins by the distance from the largest value
+constexpr int kTile = 4096, kEach = kTile / kSelect, kTilesAtOnce = 4;      // entries whose sum the slow way keeps
 // Sampling: groups that the list takes, for a top-k of at most kReach as many, else (top-p and min-p, mostly) kReachAll.
 constexpr int kReach = 1024, kReachAll = 512;
 
 struct SelectLds {
   union {
     uint64_t list[kList];              // key, complement of the index: descending order is the order of the entries
-    uint64_t mass[kSlots];             // chunks' or tiles' sums
+    uint64_t mass[kList];              // chunks' or tiles' sums
+    uint64_t flat[kFlat];
+    uint32_t near_[kNear];
+  };
+  union {
+    uint32_t groups[kGroups];
+    uint64_t bin_mass[256];
   };
   uint64_t scan[kSelect / 64 + 1];
-  uint64_t bin_mass[256];
-  uint32_t bin[256];
+  uint32_t word[kSelect / 64];
+  double part[kSelect / 64];
   uint32_t count;
   uint64_t value[2];
-  double tab[32];
 };
 
 // Exclusive prefix sum over the workgroup; total to all.
@@ -197,35 +204,113 @@ __device__ __forceinline__ uint64_t prefix(uint64_t v, uint64_t& total, SelectLd
   return before + x - v;
 }
 
-// The 16 high bits of the G-th largest of n keys (at least G keys reach them).
-__device__ __forceinline__ uint32_t bound_of(const uint32_t* group, int64_t n, uint32_t G, SelectLds& s) {
-  uint32_t high = 0;
-#pragma unroll 1
-  for (int level = 0; level < 2; ++level) {
-    const int shift = 24 - 8 * level;
-    for (int i = threadIdx.x; i < 256; i += kSelect) s.bin[i] = 0;
-    __syncthreads();
-    for (int64_t i = threadIdx.x; i < n; i += kSelect) {
-      const uint32_t k = group[i];
-      if (level == 0 || k >> 24 == high >> 24) atomicAdd(&s.bin[k >> shift & 255], 1u);
-    }
-    __syncthreads();
-    // bins from the largest down: thread i < 256 has bin 255 - i
-    const uint32_t mine = threadIdx.x < 256 ? s.bin[255 - threadIdx.x] : 0;
-    uint64_t all;
-    const uint64_t before = prefix(mine, all, s);
-    if (threadIdx.x < 256 && before < G && before + mine >= G) {
-      s.value[0] = 255 - threadIdx.x;
-      s.value[1] = before;
-    }
-    __syncthreads();
-    high |= (uint32_t)s.value[0] << shift;
-    G -= (uint32_t)s.value[1];
-  }
-  return high;
+// The row's largest key.
+__device__ __forceinline__ uint32_t largest_key(const RowsArgs& a, int64_t t, SelectLds& s) {
+  uint32_t key = 0;
+  for (int c = threadIdx.x; c < a.chunks; c += kSelect) key = max(key, a.chunk[t * a.chunks + c].key);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) key = max(key, (uint32_t)__shfl_xor((int)key, o, 64));
+  if ((threadIdx.x & 63) == 0) s.word[threadIdx.x >> 6] = key;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSelect / 64; ++w) key = max(key, s.word[w]);
+  __syncthreads();
+  return key;
 }
 
-// Entries of the row that reach `bound` into the list; their number, which may be more than fit.
+// Entries of a row, 16 bytes a thread and several of them in flight: put(value, index).
+template <bool F32, class Put>
+__device__ __forceinline__ void for_row(const void* row, int64_t V, Put&& put) {
+  constexpr int VE = F32 ? 4 : 8, U = 4, STEP = kSelect * VE;
+  int64_t base = (int64_t)threadIdx.x * VE;
+  auto each = [&](const u32x4_t& v, int64_t at) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (F32) put(__uint_as_float(v[i]), at + i);
+      else {
+        put(__uint_as_float(v[i] << 16), at + 2 * i);
+        put(__uint_as_float(v[i] & 0xffff0000u), at + 2 * i + 1);
+      }
+    }
+  };
+  for (; base - (int64_t)threadIdx.x * VE + U * STEP <= V; base += U * STEP) {
+    u32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load16((const char*)row + (base + u * STEP) * (F32 ? 4 : 2));
+#pragma unroll
+    for (int u = 0; u < U; ++u) each(v[u], base + u * STEP);
+  }
+  for (; base < V; base += STEP) {
+    if (base + VE <= V) each(load16((const char*)row + base * (F32 ? 4 : 2)), base);
+    else
+      for (int64_t i = base; i < V; ++i) put(logit<F32>(row, i), i);
+  }
+}
+
+// A thread's entries of a tile; minus infinity behind the row.
+template <bool F32>
+__device__ __forceinline__ void load_tile(float (&z)[kEach], const void* row, int64_t V, int64_t at) {
+  static_assert(kEach == 8, "one or two loads");
+  if (at + kEach <= V) {
+#pragma unroll
+    for (int h = 0; h < (F32 ? 2 : 1); ++h) {
+      const u32x4_t v = load16((const char*)row + at * (F32 ? 4 : 2) + 16 * h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (F32) z[4 * h + i] = __uint_as_float(v[i]);
+        else {
+          z[2 * i] = __uint_as_float(v[i] << 16);
+          z[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) z[i] = at + i < V ? logit<F32>(row, at + i) : -__builtin_inff();
+  }
+}
+
+// Bin of a key by its distance from the row's largest: 64 bins to a doubling, so fine near the top whatever the logits' scale.
+__device__ __forceinline__ uint32_t near_bin(uint32_t distance) {
+  if (distance < 64) return distance;
+  const int e = 31 - __clz((int)distance);
+  return (uint32_t)(e - 5) << 6 | (distance >> (e - 6) & 63);
+}
+// The largest distance of a bin.
+__device__ __forceinline__ uint32_t near_end(uint32_t bin) {
+  if (bin < 64) return bin;
+  const int e = (int)(bin >> 6) + 5;
+  return (((bin & 63) + 65) << (e - 6)) - 1;
+}
+
+// A key that at least G of the row's n groups reach, and not many more if the largest are spread a little.
+__device__ __forceinline__ uint32_t bound_of(const uint32_t* group, int64_t n, uint32_t G, uint32_t top, SelectLds& s) {
+  constexpr int PER = (kNear + kSelect - 1) / kSelect;
+  for (int i = threadIdx.x; i < kNear; i += kSelect) s.near_[i] = 0;
+  __syncthreads();
+  for (int64_t i = threadIdx.x; i < n; i += kSelect) atomicAdd(&s.near_[near_bin(top - group[i])], 1u);
+  __syncthreads();
+  uint32_t mine[PER], sum = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = threadIdx.x * PER + i;
+    mine[i] = b < kNear ? s.near_[b] : 0;
+    sum += mine[i];
+  }
+  uint64_t all;
+  uint64_t before = prefix(sum, all, s);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (before < G && before + mine[i] >= G) s.value[0] = threadIdx.x * PER + i;
+    before += mine[i];
+  }
+  __syncthreads();
+  const uint32_t end = near_end((uint32_t)s.value[0]);
+  __syncthreads();
+  return end < top ? top - end : 0;
+}
+
+// Entries of the row that reach `bound` into the list; their number, which may be more than fit (then the list is not whole).
 template <bool F32>
 __device__ __forceinline__ uint32_t gather(const RowsArgs& a, int64_t t, uint32_t bound, SelectLds& s) {
   constexpr int VE = F32 ? 4 : 8;
@@ -235,26 +320,65 @@ __device__ __forceinline__ uint32_t gather(const RowsArgs& a, int64_t t, uint32_
   const int J = a.per_thread / VE;
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
-  for (int64_t g = threadIdx.x; g < n; g += kSelect) {
-    if (group[g] < bound) continue;
-    const int64_t at = g / kRowThreads * ((int64_t)kRowThreads * a.per_thread) + g % kRowThreads * VE;
-    for (int j = 0; j < J; ++j)
-      for (int i = 0; i < VE; ++i) {
-        const int64_t k = at + (int64_t)j * (kRowThreads * VE) + i;
-        if (k >= a.V) break;
-        const uint32_t key = key_of(logit<F32>(row, k));
-        if (key < bound) continue;
-        const uint32_t to = atomicAdd(&s.count, 1u);
-        if (to < (uint32_t)kList) s.list[to] = (uint64_t)key << 32 | (uint32_t)~(uint32_t)k;
+  for (int64_t g = threadIdx.x; g < n; g += kSelect)
+    if (group[g] >= bound) {
+      const uint32_t to = atomicAdd(&s.count, 1u);
+      if (to < (uint32_t)kGroups) s.groups[to] = (uint32_t)g;
+    }
+  __syncthreads();
+  const uint32_t groups = s.count;
+  __syncthreads();
+  if (groups > (uint32_t)kGroups) return ~0u;
+  if (threadIdx.x == 0) s.count = 0;
+  __syncthreads();
+  for (uint32_t q = threadIdx.x; q < groups * J; q += kSelect) {
+    const uint32_t g = s.groups[q / J], j = q % J;
+    const int64_t at = ((int64_t)(g / kRowThreads) * a.per_thread + j * VE) * kRowThreads + g % kRowThreads * VE;
+    if (at >= a.V) continue;
+    float z[VE];
+    if (at + VE <= a.V) {
+      const u32x4_t v = load16((const char*)row + at * (F32 ? 4 : 2));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (F32) z[i] = __uint_as_float(v[i]);
+        else {
+          z[(2 * i) % VE] = __uint_as_float(v[i] << 16);
+          z[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
+        }
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) z[i] = at + i < a.V ? logit<F32>(row, at + i) : -__builtin_inff();
+    }
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+      const uint32_t key = key_of(z[i]);
+      if (key < bound) continue;
+      const uint32_t to = atomicAdd(&s.count, 1u);
+      if (to < (uint32_t)kList) s.list[to] = (uint64_t)key << 32 | (uint32_t)~(uint32_t)(at + i);
+    }
   }
   __syncthreads();
-  return s.count;
+  const uint32_t found = s.count;
+  __syncthreads();
+  return found;
 }
 
-// Sorts list[0 .. n) in descending order (n at most kList; filled up to a power of two with 0).
+// Sorts list[0 .. n) in descending order (n at most kList; no entry twice).  Short lists: each entry counts the larger ones.
 __device__ __forceinline__ void sort_list(uint32_t n, SelectLds& s) {
-  uint32_t size = 2;
+  if (n <= 256) {
+    uint64_t mine = 0;
+    uint32_t rank = 0;
+    if (threadIdx.x < n) {
+      mine = s.list[threadIdx.x];
+      for (uint32_t i = 0; i < n; ++i) rank += s.list[i] > mine;
+    }
+    __syncthreads();
+    if (threadIdx.x < n) s.list[rank] = mine;
+    __syncthreads();
+    return;
+  }
+  uint32_t size = 512;
   while (size < n) size <<= 1;
   for (uint32_t i = n + threadIdx.x; i < size; i += kSelect) s.list[i] = 0;
   __syncthreads();
@@ -274,21 +398,38 @@ __device__ __forceinline__ void sort_list(uint32_t n, SelectLds& s) {
 
 // ---- the slow way: the last kept entry, as its key and the last index that counts among entries of that key ----
 struct Cut { uint32_t key; int64_t last; };
+constexpr Cut kAll = {0, INT64_MAX};
 
 __device__ __forceinline__ bool inside(const Cut& c, uint32_t key, int64_t i) { return key > c.key || (key == c.key && i <= c.last); }
 
+struct Row {
+  const void* p;
+  int64_t V;
+  float top;             // largest entry
+  double scale;          // t = (z - top) scale
+  float bins;            // flat bins to a unit of the logits
+  int bits;              // of a weight
+};
+__device__ __forceinline__ uint64_t row_weight(const Row& r, float z) { return whole(weight(((double)z - (double)r.top) * r.scale, r.bits)); }
+// Bin of an entry by its distance from the largest, all of the entries with a weight of 2^-44 and more in kFlat - 1 of them.
+__device__ __forceinline__ uint32_t flat_bin(const Row& r, float z) {
+  const float x = (r.top - z) * r.bins;
+  return x < (float)(kFlat - 1) ? (uint32_t)x : kFlat - 1;
+}
+
 // Index of the e-th entry (from 1) of this key.
 template <bool F32>
-__device__ __forceinline__ int64_t place_of(const void* row, int64_t V, uint32_t key, uint64_t e, SelectLds& s) {
-  for (int64_t base = 0;; base += kTile) {
+__device__ __forceinline__ int64_t place_of(const Row& r, uint32_t key, uint64_t e, SelectLds& s) {
+  constexpr int STEP = kSelect * 8;
+  for (int64_t base = 0;; base += STEP) {
     const int64_t at = base + threadIdx.x * 8;
     uint32_t hits = 0;
     for (int i = 0; i < 8; ++i)
-      if (at + i < V && key_of(logit<F32>(row, at + i)) == key) hits |= 1u << i;
+      if (at + i < r.V && key_of(logit<F32>(r.p, at + i)) == key) hits |= 1u << i;
     uint64_t all;
     const uint64_t before = prefix(__popc(hits), all, s);
-    if (e <= all || base + kTile >= V) {
-      if (threadIdx.x == 0) s.value[0] = V - 1;
+    if (e <= all || base + STEP >= r.V) {
+      if (threadIdx.x == 0) s.value[0] = r.V - 1;
       __syncthreads();
       if (before < e && e <= before + __popc(hits)) {
         uint64_t left = e - before;
@@ -304,22 +445,21 @@ __device__ __forceinline__ int64_t place_of(const void* row, int64_t V, uint32_t
   }
 }
 
-// The last entry of the fewest, in descending order, whose number (MASS: sum of w) is at least `want` (which the whole row reaches).
+// The last entry of the fewest, in descending order and inside `limit`, whose number (MASS: sum of w) is at least `want` (which those
+// inside reach), by eight bits of the key at a time.
 template <bool F32, bool MASS>
-__device__ __forceinline__ Cut narrow(const void* row, int64_t V, uint64_t want, double zero, double scale, int bits, SelectLds& s) {
+__device__ __forceinline__ Cut narrow(const Row& r, const Cut& limit, uint64_t want, SelectLds& s) {
   uint32_t high = 0;
 #pragma unroll 1
   for (int level = 0; level < 4; ++level) {
     const int shift = 24 - 8 * level;
     for (int i = threadIdx.x; i < 256; i += kSelect) s.bin_mass[i] = 0;
     __syncthreads();
-    for (int64_t i = threadIdx.x; i < V; i += kSelect) {
-      const float z = logit<F32>(row, i);
+    for_row<F32>(r.p, r.V, [&](float z, int64_t i) {
       const uint32_t k = key_of(z);
-      if (level && (k ^ high) >> (shift + 8)) continue;
-      atomicAdd((unsigned long long*)&s.bin_mass[k >> shift & 255],
-                (unsigned long long)(MASS ? weight(((double)z - zero) * scale, s.tab, bits) : 1));
-    }
+      if ((level && (k ^ high) >> (shift + 8)) || !inside(limit, k, i)) return;
+      atomicAdd((unsigned long long*)&s.bin_mass[k >> shift & 255], (unsigned long long)(MASS ? row_weight(r, z) : 1));
+    });
     __syncthreads();
     const uint64_t mine = threadIdx.x < 256 ? s.bin_mass[255 - threadIdx.x] : 0;
     uint64_t all;
@@ -335,23 +475,88 @@ __device__ __forceinline__ Cut narrow(const void* row, int64_t V, uint64_t want,
   }
   uint64_t e = want;
   if (MASS) {
-    const uint64_t w = weight(((double)value_of(high) - zero) * scale, s.tab, bits);
+    const uint64_t w = row_weight(r, value_of(high));
     e = (want + w - 1) / w;
   }
-  return Cut{high, place_of<F32>(row, V, high, e, s)};
+  return Cut{high, place_of<F32>(r, high, e, s)};
+}
+
+// The same by bins of the value: the one that holds the entry goes into the list, is sorted and counted through.  share: `want` is that share
+// of the sum inside `limit` (1: a number of entries).
+template <bool F32, bool MASS>
+__device__ __forceinline__ Cut cut_of(const Row& r, const Cut& limit, uint64_t want, double share, SelectLds& s) {
+  constexpr int PER = kFlat / kSelect;
+  for (int i = threadIdx.x; i < kFlat; i += kSelect) s.flat[i] = 0;
+  __syncthreads();
+  for_row<F32>(r.p, r.V, [&](float z, int64_t i) {
+    const uint32_t k = key_of(z);
+    if (!inside(limit, k, i)) return;
+    const uint64_t w = MASS ? row_weight(r, z) : 1;
+    if (w) atomicAdd((unsigned long long*)&s.flat[flat_bin(r, z)], (unsigned long long)w);
+  });
+  __syncthreads();
+  uint64_t mine[PER], sum = 0, all;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) sum += mine[i] = s.flat[threadIdx.x * PER + i];
+  uint64_t before = prefix(sum, all, s);
+  if (MASS) {
+    want = (uint64_t)ceil(share * (double)all);
+    want = want < 1 ? 1 : want < all ? want : all;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (before < want && before + mine[i] >= want) {
+      s.value[0] = threadIdx.x * PER + i;
+      s.value[1] = before;
+    }
+    before += mine[i];
+  }
+  if (threadIdx.x == 0) s.count = 0;
+  __syncthreads();
+  const uint32_t bin = (uint32_t)s.value[0];
+  const uint64_t left = want - s.value[1];
+  for_row<F32>(r.p, r.V, [&](float z, int64_t i) {
+    if (flat_bin(r, z) != bin) return;
+    const uint32_t k = key_of(z);
+    if (!inside(limit, k, i)) return;
+    const uint32_t to = atomicAdd(&s.count, 1u);
+    if (to < (uint32_t)kList) s.list[to] = (uint64_t)k << 32 | (uint32_t)~(uint32_t)i;
+  });
+  __syncthreads();
+  const uint32_t n = s.count;
+  __syncthreads();
+  if (n > (uint32_t)kList) return narrow<F32, MASS>(r, limit, want, s);
+  sort_list(n, s);
+  const uint32_t per = (n + kSelect - 1) / kSelect, i0 = threadIdx.x * per;
+  auto of = [&](uint32_t i) { return MASS ? row_weight(r, value_of((uint32_t)(s.list[i] >> 32))) : (uint64_t)1; };
+  uint64_t part = 0;
+  for (uint32_t i = i0; i < i0 + per && i < n; ++i) part += of(i);
+  uint64_t x = prefix(part, all, s);
+  if (x < left && x + part >= left)
+    for (uint32_t i = i0; i < i0 + per && i < n; ++i) {
+      x += of(i);
+      if (x >= left) {
+        s.value[0] = s.list[i];
+        break;
+      }
+    }
+  __syncthreads();
+  const uint64_t e = s.value[0];
+  __syncthreads();
+  return Cut{(uint32_t)(e >> 32), (int64_t)(uint32_t)~(uint32_t)e};
 }
 
 // ------------------------------------------------------------------------------------------------
 // top logits
 // ------------------------------------------------------------------------------------------------
 template <bool F32>
-__device__ __forceinline__ void put_top(const RowsArgs& a, int64_t t, int at, uint32_t key, int64_t index) {
+__device__ __forceinline__ void put_top(const RowsArgs& a, int64_t t, int at, uint64_t entry) {
+  const uint32_t key = (uint32_t)(entry >> 32), index = ~(uint32_t)entry;
   const bool there = key > kKeyMinusInf;
   const int64_t to = t * a.K + at;
-  const float z = there ? (F32 ? ((const float*)row_of<true>(a, t))[index] : 0.f) : -__builtin_inff();
-  if (F32) ((float*)a.top)[to] = z;
+  if (F32) ((float*)a.top)[to] = there ? ((const float*)row_of<true>(a, t))[index] : -__builtin_inff();
   else ((uint16_t*)a.top)[to] = there ? ((const uint16_t*)row_of<false>(a, t))[index] : (uint16_t)0xff80;
-  if (a.index64) ((int64_t*)a.index)[to] = there ? index : -1;
+  if (a.index64) ((int64_t*)a.index)[to] = there ? (int64_t)index : -1;
   else ((int32_t*)a.index)[to] = there ? (int32_t)index : -1;
 }
 
@@ -361,18 +566,9 @@ __global__ __launch_bounds__(kSelect) void top_select_kernel(const RowsArgs a) {
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
   const int64_t n = (int64_t)a.chunks * kRowThreads;
-  const void* const row = row_of<F32>(a, t);
+  const uint32_t key = largest_key(a, t, s);
   if (a.lse) {
     // the chunks' sums at the row's largest entry, in a fixed order
-    uint32_t key = 0;
-    for (int c = tid; c < a.chunks; c += kSelect) key = max(key, a.chunk[t * a.chunks + c].key);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) key = max(key, (uint32_t)__shfl_xor((int)key, o, 64));
-    if ((tid & 63) == 0) s.bin[tid >> 6] = key;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kSelect / 64; ++w) key = max(key, s.bin[w]);
-    __syncthreads();
     const double top = value_of(key);
     double sum = 0;
     for (int c = tid; c < a.chunks; c += kSelect) {
@@ -381,48 +577,39 @@ __global__ __launch_bounds__(kSelect) void top_select_kernel(const RowsArgs a) {
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
-    if ((tid & 63) == 0) s.tab[tid >> 6] = sum;
+    if ((tid & 63) == 0) s.part[tid >> 6] = sum;
     __syncthreads();
     if (tid == 0) {
       sum = 0;
-      for (int w = 0; w < kSelect / 64; ++w) sum += s.tab[w];
+      for (int w = 0; w < kSelect / 64; ++w) sum += s.part[w];
       a.lse[t] = key == kKeyNaN ? __builtin_nanf("") : key == kKeyInf ? __builtin_inff() : key <= kKeyMinusInf ? -__builtin_inff()
                  : (float)(top / (double)a.tau + log(sum));
     }
   }
   // (entries of minus infinity are no entries: the lowest bound is above them)
   uint32_t bound = kKeyMinusInf + 1;
-  if ((int64_t)a.K < n) bound = max(bound, bound_of(a.group + t * n, n, (uint32_t)a.K, s));
-  const uint32_t found = gather<F32>(a, t, bound, s);
-  if (found <= (uint32_t)kList) {
-    sort_list(found, s);
-    for (int i = tid; i < a.K; i += kSelect) {
-      const uint64_t x = i < (int)found ? s.list[i] : 0;
-      put_top<F32>(a, t, i, (uint32_t)(x >> 32), (int64_t)(uint32_t)~(uint32_t)x);
-    }
-    return;
+  if ((int64_t)a.K < n) bound = max(bound, bound_of(a.group + t * n, n, (uint32_t)a.K, key, s));
+  uint32_t found = gather<F32>(a, t, bound, s);
+  if (found > (uint32_t)kList) {
+    const Row r{row_of<F32>(a, t), a.V, value_of(key), 0, 0.f, 0};
+    const Cut cut = narrow<F32, false>(r, kAll, (uint64_t)a.K, s);
+    if (tid == 0) s.count = 0;
+    __syncthreads();
+    for_row<F32>(r.p, r.V, [&](float z, int64_t i) {
+      const uint32_t k = key_of(z);
+      if (k > kKeyMinusInf && inside(cut, k, i)) s.list[atomicAdd(&s.count, 1u)] = (uint64_t)k << 32 | (uint32_t)~(uint32_t)i;
+    });
+    __syncthreads();
+    found = s.count;
   }
-  const Cut cut = narrow<F32, false>(row, a.V, (uint64_t)a.K, 0, 0, 0, s);
-  if (tid == 0) s.count = 0;
-  __syncthreads();
-  for (int64_t i = tid; i < a.V; i += kSelect) {
-    const uint32_t key = key_of(logit<F32>(row, i));
-    if (key <= kKeyMinusInf || !inside(cut, key, i)) continue;
-    s.list[atomicAdd(&s.count, 1u)] = (uint64_t)key << 32 | (uint32_t)~(uint32_t)i;
-  }
-  __syncthreads();
-  const uint32_t kept = s.count;
-  sort_list(kept, s);
-  for (int i = tid; i < a.K; i += kSelect) {
-    const uint64_t x = i < (int)kept ? s.list[i] : 0;
-    put_top<F32>(a, t, i, (uint32_t)(x >> 32), (int64_t)(uint32_t)~(uint32_t)x);
-  }
+  sort_list(found, s);
+  for (int i = tid; i < a.K; i += kSelect) put_top<F32>(a, t, i, i < (int)found ? s.list[i] : 0);
 }
 
 // ------------------------------------------------------------------------------------------------
 // sampling
 // ------------------------------------------------------------------------------------------------
-// The largest whole number that is not above u total.
+// The largest whole number that is not above u total, and less than it.
 __device__ __forceinline__ uint64_t target_of(float u, uint64_t total) {
   const uint64_t x = (uint64_t)((double)u * (double)total);
   return x < total ? x : total - 1;
@@ -438,17 +625,7 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
   const float top_p = a.top_p_rows ? a.top_p_rows[t] : a.top_p, min_p = a.min_p_rows ? a.min_p_rows[t] : a.min_p;
   const int64_t top_k = a.top_k_rows ? a.top_k_rows[t] : a.top_k;
   const bool greedy = tau == 0.f, all_k = !greedy && (top_k == 0 || top_k >= V);
-  fill_table(s.tab);
-  // the row's largest entry
-  uint32_t key = 0;
-  for (int c = tid; c < a.chunks; c += kSelect) key = max(key, a.chunk[t * a.chunks + c].key);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) key = max(key, (uint32_t)__shfl_xor((int)key, o, 64));
-  if ((tid & 63) == 0) s.bin[tid >> 6] = key;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSelect / 64; ++w) key = max(key, s.bin[w]);
-  __syncthreads();
+  const uint32_t key = largest_key(a, t, s);
   auto answer = [&](int64_t token, float logp) {
     if (a.index64) ((int64_t*)a.token)[t] = token;
     else ((int32_t*)a.token)[t] = (int32_t)token;
@@ -460,10 +637,10 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     if (tid == 0) answer(-1, __builtin_nanf(""));
     return;
   }
-  const double top = value_of(key), scale = 32 * kLog2e / (greedy ? 1. : (double)tau);
+  const double top = value_of(key), scale = kLog2e / (greedy ? 1. : (double)tau);
   const int row_bits = min(kChunkBits, 62 - (64 - __clzll((unsigned long long)V)));      // V entries of at most 2^row_bits
-  auto log_p = [&](int64_t token, uint64_t total, int bits) {
-    return greedy ? 0.f : (float)(((double)logit<F32>(row, token) - top) / (double)tau - log(ldexp((double)total, -bits)));
+  auto log_p = [&](float z, uint64_t total, int bits) {
+    return greedy ? 0.f : (float)(((double)z - top) / (double)tau - log(ldexp((double)total, -bits)));
   };
 
   uint64_t row_total = 0;
@@ -474,7 +651,7 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     auto chunk_mass = [&](int c) {
       const RowChunk& r = a.chunk[t * a.chunks + c];
       if (r.key <= kKeyMinusInf) return (uint64_t)0;
-      return (uint64_t)rint(ldexp((double)r.sum, row_bits - kChunkBits) * exp2(((double)value_of(r.key) - top) * (scale / 32)));
+      return whole(ldexp((double)r.sum, row_bits - kChunkBits) * exp2(((double)value_of(r.key) - top) * scale));
     };
     for (int c = c0; c < c0 + per && c < a.chunks; ++c) part += chunk_mass(c);
     const uint64_t before = prefix(part, row_total, s);
@@ -496,23 +673,23 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
       const int c = (int)s.value[0];
       const RowChunk r = a.chunk[t * a.chunks + c];
       // that chunk again, with its own sums
-      const double zero = value_of(r.key);
-      const double inner = ldexp((double)s.value[1], kChunkBits - row_bits) * exp2((top - zero) * (scale / 32));
-      const uint64_t want = inner < (double)r.sum ? (uint64_t)inner : r.sum - 1;
+      const double z0 = value_of(r.key), inner = ldexp((double)s.value[1], kChunkBits - row_bits) * exp2((top - z0) * scale);
       const int64_t begin = (int64_t)c * kRowThreads * a.per_thread, end = min(V, begin + (int64_t)kRowThreads * a.per_thread);
       const int each = (int)((end - begin + kSelect - 1) / kSelect);
       const int64_t i0 = begin + (int64_t)tid * each;
+      auto w_at = [&](int64_t i) { return whole(weight(((double)logit<F32>(row, i) - z0) * scale, kChunkBits)); };
       uint64_t mine = 0;
       for (int i = 0; i < each; ++i)
-        if (i0 + i < end) mine += weight(((double)logit<F32>(row, i0 + i) - zero) * scale, s.tab, kChunkBits);
+        if (i0 + i < end) mine += w_at(i0 + i);
       uint64_t all;
       const uint64_t ahead = prefix(mine, all, s);
+      const uint64_t want = inner < (double)all ? (uint64_t)inner : all - 1;
       if (ahead <= want && want < ahead + mine) {
         uint64_t x = ahead;
         for (int i = 0; i < each; ++i) {
-          x += weight(((double)logit<F32>(row, i0 + i) - zero) * scale, s.tab, kChunkBits);
+          x += w_at(i0 + i);
           if (x > want) {
-            answer(i0 + i, log_p(i0 + i, row_total, row_bits));
+            answer(i0 + i, log_p(logit<F32>(row, i0 + i), row_total, row_bits));
             break;
           }
         }
@@ -525,8 +702,8 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
   const int64_t k = greedy ? 1 : all_k ? V : top_k;
   const uint32_t reach = (uint32_t)(k <= kReach ? k : kReachAll);
   uint32_t bound = kKeyMinusInf + 1;
-  if ((int64_t)reach < n) bound = max(bound, bound_of(a.group + t * n, n, reach, s));
-  const bool whole = bound == kKeyMinusInf + 1;
+  if ((int64_t)reach < n) bound = max(bound, bound_of(a.group + t * n, n, reach, key, s));
+  const bool all_listed = bound == kKeyMinusInf + 1;
   const uint32_t found = gather<F32>(a, t, bound, s);
   if (found <= (uint32_t)kList) {
     sort_list(found, s);
@@ -538,12 +715,13 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     // thread i has entries i per .. + per - 1 of the list
     const uint32_t per = (found + kSelect - 1) / kSelect, i0 = tid * per;
     const double floor_w = ldexp((double)min_p, kChunkBits);
-    auto w_at = [&](uint32_t i) { return weight(((double)value_of((uint32_t)(s.list[i] >> 32)) - top) * scale, s.tab, kChunkBits); };
+    auto w_key = [&](uint32_t k_) { return whole(weight(((double)value_of(k_) - top) * scale, kChunkBits)); };
+    auto w_at = [&](uint32_t i) { return w_key((uint32_t)(s.list[i] >> 32)); };
     uint64_t part = 0;
     for (uint32_t i = i0; i < i0 + per && i < limit; ++i) part += w_at(i);
     uint64_t listed;
     uint64_t x = prefix(part, listed, s);
-    const bool reaches_k = whole || k <= (int64_t)found;
+    const bool reaches_k = all_listed || k <= (int64_t)found;
     // sum over the first top_k
     const double base = all_k ? ldexp((double)row_total, kChunkBits - row_bits) : (double)listed;
     const bool p_known = top_p == 1.f || all_k || reaches_k;
@@ -560,24 +738,22 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     // the list says it all if it is the whole row, or holds the first top_k, or an entry of it that is not kept
     if (p_known && (reaches_k || n_kept < found)) {
       // kept entries in order of their index
-      for (uint32_t i = tid; i < n_kept; i += kSelect) {
+      const uint32_t m = (uint32_t)n_kept, each = (m + kSelect - 1) / kSelect, j0 = tid * each;
+      for (uint32_t i = tid; i < m; i += kSelect) {
         const uint64_t e = s.list[i];
-        s.list[i] = (e & 0xffffffffu) << 32 | e >> 32;           // (complement of the index: descending is reversed below)
+        s.list[i] = e << 32 | e >> 32;                 // (the index's complement in front: descending is by ascending index)
       }
       __syncthreads();
-      sort_list((uint32_t)n_kept, s);
-      const uint32_t m = (uint32_t)n_kept, each = (m + kSelect - 1) / kSelect, j0 = tid * each;
-      auto w_of = [&](uint32_t j) { return weight(((double)value_of((uint32_t)s.list[j]) - top) * scale, s.tab, kChunkBits); };
+      sort_list(m, s);
       uint64_t mine = 0, total;
-      for (uint32_t j = j0; j < j0 + each && j < m; ++j) mine += w_of(j);
+      for (uint32_t j = j0; j < j0 + each && j < m; ++j) mine += w_key((uint32_t)s.list[j]);
       uint64_t y = prefix(mine, total, s);
       const uint64_t target = target_of(u, total);
       if (y <= target && target < y + mine)
         for (uint32_t j = j0; j < j0 + each && j < m; ++j) {
-          y += w_of(j);
+          y += w_key((uint32_t)s.list[j]);
           if (y > target) {
-            const int64_t token = (int64_t)(uint32_t)~(uint32_t)(s.list[j] >> 32);
-            answer(token, log_p(token, total, kChunkBits));
+            answer((int64_t)(uint32_t)~(uint32_t)(s.list[j] >> 32), log_p(value_of((uint32_t)s.list[j]), total, kChunkBits));
             break;
           }
         }
@@ -586,56 +762,64 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
   }
 
   // the slow way
-  Cut cut{0, V};
-  if (k < V) cut = narrow<F32, false>(row, V, (uint64_t)k, 0, 0, 0, s);
-  if (top_p < 1.f) {
-    uint64_t mine = 0, total;
-    for (int64_t i = tid; i < V; i += kSelect) {
-      const float z = logit<F32>(row, i);
-      if (inside(cut, key_of(z), i)) mine += weight(((double)z - top) * scale, s.tab, row_bits);
-    }
-    prefix(mine, total, s);
-    const uint64_t want = (uint64_t)ceil((double)top_p * (double)total);
-    const Cut p = narrow<F32, true>(row, V, want < 1 ? 1 : want < total ? want : total, top, scale, row_bits, s);
-    if (p.key > cut.key || (p.key == cut.key && p.last < cut.last)) cut = p;
-  }
+  __syncthreads();
+  const Row r{row, V, (float)top, scale, (float)((kFlat - 1) / 44. * scale), row_bits};
+  Cut cut = kAll;
+  if (k < V) cut = cut_of<F32, false>(r, kAll, (uint64_t)k, 1., s);
+  if (top_p < 1.f) cut = cut_of<F32, true>(r, cut, 0, (double)top_p, s);
   const double floor_w = ldexp((double)min_p, row_bits);
-  auto w_kept = [&](int64_t i) {
-    const float z = logit<F32>(row, i);
+  auto w_kept = [&](float z, int64_t i) {
     if (!inside(cut, key_of(z), i)) return (uint64_t)0;
-    const uint64_t w = weight(((double)z - top) * scale, s.tab, row_bits);
+    const uint64_t w = row_weight(r, z);
     return (double)w >= floor_w ? w : (uint64_t)0;
   };
   // the tile in which the sum passes the target, and the entry in the tile
-  const int64_t tiles = (V + kTile - 1) / kTile;
-  uint64_t total = 0;
+  const int tiles = (int)((V + kTile - 1) / kTile);
+  for (int i = tid; i < tiles; i += kSelect) s.mass[i] = 0;
   __syncthreads();
-  for (int64_t b = 0; b < tiles; ++b) {
-    uint64_t mine = 0, all;
-    for (int i = 0; i < 8; ++i) {
-      const int64_t at = b * kTile + i * kSelect + tid;
-      if (at < V) mine += w_kept(at);
+  for (int b = 0; b < tiles; b += kTilesAtOnce) {
+    float z[kTilesAtOnce][kEach];
+#pragma unroll
+    for (int j = 0; j < kTilesAtOnce; ++j) load_tile<F32>(z[j], row, V, (int64_t)(b + j) * kTile + tid * kEach);
+#pragma unroll
+    for (int j = 0; j < kTilesAtOnce; ++j) {
+      uint64_t w = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) w += w_kept(z[j][i], (int64_t)(b + j) * kTile + tid * kEach + i);
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) w += __shfl_xor((unsigned long long)w, o, 64);
+      if ((tid & 63) == 0 && w) atomicAdd((unsigned long long*)&s.mass[b + j], (unsigned long long)w);
     }
-    prefix(mine, all, s);
-    if (tid == 0) s.mass[b] = all;
-    total += all;
   }
   __syncthreads();
-  uint64_t target = target_of(u, total);
-  const uint64_t sum = total;
-  int64_t b = 0;
-  while (b + 1 < tiles && target >= s.mass[b]) target -= s.mass[b++];
-  const int64_t at = b * kTile + tid * 8;
+  const int per = (tiles + kSelect - 1) / kSelect, b0 = tid * per;
+  uint64_t part = 0, total;
+  for (int b = b0; b < b0 + per && b < tiles; ++b) part += s.mass[b];
+  uint64_t x = prefix(part, total, s);
+  const uint64_t target = target_of(u, total);
+  if (x <= target && target < x + part)
+    for (int b = b0; b < b0 + per && b < tiles; ++b) {
+      if (target < x + s.mass[b]) {
+        s.value[0] = b;
+        s.value[1] = target - x;
+        break;
+      }
+      x += s.mass[b];
+    }
+  __syncthreads();
+  const int64_t at = (int64_t)s.value[0] * kTile + tid * kEach;
+  const uint64_t want = s.value[1];
   uint64_t mine = 0, all;
-  for (int i = 0; i < 8; ++i)
-    if (at + i < V) mine += w_kept(at + i);
+  for (int i = 0; i < kEach; ++i)
+    if (at + i < V) mine += w_kept(logit<F32>(row, at + i), at + i);
   uint64_t y = prefix(mine, all, s);
-  if (y <= target && target < y + mine)
-    for (int i = 0; i < 8; ++i) {
+  if (y <= want && want < y + mine)
+    for (int i = 0; i < kEach; ++i) {
       if (at + i >= V) break;
-      y += w_kept(at + i);
-      if (y > target) {
-        answer(at + i, log_p(at + i, sum, row_bits));
+      const float z = logit<F32>(row, at + i);
+      y += w_kept(z, at + i);
+      if (y > want) {
+        answer(at + i, log_p(z, total, row_bits));
         break;
       }
     }
