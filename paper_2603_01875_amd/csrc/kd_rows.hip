@@ -35,7 +35,7 @@ __device__ __forceinline__ const void* row_of(const RowsArgs& a, int64_t t) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// w = 2^t in 64 bits, t <= 0, times 2^bits
+// w = 2^t in 64 bits, t <= 0
 //
 // t = n + x with a whole number n and |x| <= 1/2; 2^x is the polynomial of degree 8 that meets it at the Chebyshev nodes of [-1/2, 1/2] (1 at 0; off by
 // 2^-39.7 at most), 2^n is added to its exponent.  n comes out of the low bits of t + 1.5 2^52: no conversion, no table.  13 instructions in 64 bits; an exp
@@ -44,7 +44,7 @@ __device__ __forceinline__ const void* row_of(const RowsArgs& a, int64_t t) {
 constexpr double kLog2e = 1.44269504088896340736;
 constexpr int kChunkBits = 48;         // a chunk's sums: 2^14 entries of at most 2^48
 
-__device__ __forceinline__ double weight(double t, int bits) {
+__device__ __forceinline__ double weight(double t) {
   t = fmax(t, -80.);                                   // (2^-80 and less count as nothing; also for a NaN, where a chunk is empty)
   const double m = t + 0x1.8p52, x = t - (m - 0x1.8p52);
   double p = 0x1.63d1363930791p-20;
@@ -56,11 +56,13 @@ __device__ __forceinline__ double weight(double t, int bits) {
   p = fma(p, x, 0x1.ebfbdff823cedp-3);
   p = fma(p, x, 0x1.62e42fef84cf0p-1);
   p = fma(p, x, 1.);
-  const uint64_t v = __double_as_longlong(p);
-  const uint32_t high = (uint32_t)(v >> 32) + (((uint32_t)__double_as_longlong(m) + (uint32_t)bits) << 20);
-  return __longlong_as_double((long long)((uint64_t)high << 32 | (uint32_t)v));
+  return __hiloint2double(__double2hiint(p) + (__double2loint(m) << 20), __double2loint(p));
 }
-__device__ __forceinline__ uint64_t whole(double v) { return (uint64_t)rint(v); }
+// A weight (or a sum of some) as a whole number of 2^-bits.
+__device__ __forceinline__ uint64_t whole(double w, int bits) { return (uint64_t)rint(ldexp(w, bits)); }
+
+// A chunk's weights are 2^(z scale - zero) with zero = top scale, rounded: off by the same factor 2^offset all of them, offset = top scale - zero.
+__device__ __forceinline__ double chunk_offset(double top, double scale) { return fma(top, scale, -(top * scale)); }
 
 // ------------------------------------------------------------------------------------------------
 // first kernel
@@ -79,28 +81,46 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
   const void* const row = row_of<F32>(a, t);
   const int64_t at = (int64_t)c * (NT * E) + tid * VE;
   float z[E];
+  auto unpack = [&](int j, const u32x4_t& v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (F32) z[j * VE + i] = __uint_as_float(v[i]);
+      else {
+        z[j * VE + (2 * i) % VE] = __uint_as_float(v[i] << 16);
+        z[j * VE + (2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
+      }
+    }
+  };
   if ((int64_t)(c + 1) * (NT * E) <= a.V) {
     u32x4_t v[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) v[j] = load16((const char*)row + (at + j * (NT * VE)) * (F32 ? 4 : 2));
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (F32) z[j * VE + i] = __uint_as_float(v[j][i]);
-        else {
-          z[j * VE + (2 * i) % VE] = __uint_as_float(v[j][i] << 16);
-          z[j * VE + (2 * i + 1) % VE] = __uint_as_float(v[j][i] & 0xffff0000u);
-        }
-      }
+    for (int j = 0; j < J; ++j) unpack(j, v[j]);
   } else {
+    // the row's end: whole loads as far as they go (an address that is surely there where they do not), then the entries behind the last one,
+    // all under way together as well
+    u32x4_t v[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j) {
+      const int64_t k = at + j * (NT * VE);
+      v[j] = a.V >= VE ? load16((const char*)row + (k + VE <= a.V ? k : 0) * (F32 ? 4 : 2)) : u32x4_t{0, 0, 0, 0};
+    }
 #pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const int64_t k = at + j * (NT * VE) + i;
-        z[j * VE + i] = k < a.V ? logit<F32>(row, k) : -__builtin_inff();
+    for (int j = 0; j < J; ++j) {
+      const int64_t k = at + j * (NT * VE);
+      unpack(j, v[j]);
+      if (k + VE > a.V)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) z[j * VE + i] = -__builtin_inff();
+      if (k < a.V && k + VE > a.V) {
+        float e[VE];
+#pragma unroll
+        for (int i = 0; i < VE; ++i) e[i] = logit<F32>(row, k + i < a.V ? k + i : a.V - 1);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) z[j * VE + i] = k + i < a.V ? e[i] : -__builtin_inff();
       }
+    }
   }
   float m = z[0];
   bool nan = m != m;
@@ -123,11 +143,11 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
     const float tau = row_temperature(a, t);
     uint64_t s = 0;
     if (tau > 0.f) {
-      const double scale = kLog2e / (double)tau, zero = (double)top;
+      const double scale = kLog2e / (double)tau, zero = (double)top * scale;      // (rounded: see chunk_offset)
       double w = 0;
 #pragma unroll
-      for (int i = 0; i < E; ++i) w += weight(((double)z[i] - zero) * scale, kChunkBits);
-      s = whole(w);
+      for (int i = 0; i < E; ++i) w += weight(fma((double)z[i], scale, -zero));
+      s = whole(w, kChunkBits);
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) s += __shfl_xor((unsigned long long)s, o, 64);
@@ -410,7 +430,7 @@ struct Row {
   float bins;            // flat bins to a unit of the logits
   int bits;              // of a weight
 };
-__device__ __forceinline__ uint64_t row_weight(const Row& r, float z) { return whole(weight(((double)z - (double)r.top) * r.scale, r.bits)); }
+__device__ __forceinline__ uint64_t row_weight(const Row& r, float z) { return whole(weight(((double)z - (double)r.top) * r.scale), r.bits); }
 // Bin of an entry by its distance from the largest, all of the entries with a weight of 2^-44 and more in kFlat - 1 of them.
 __device__ __forceinline__ uint32_t flat_bin(const Row& r, float z) {
   const float x = (r.top - z) * r.bins;
@@ -651,7 +671,8 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     auto chunk_mass = [&](int c) {
       const RowChunk& r = a.chunk[t * a.chunks + c];
       if (r.key <= kKeyMinusInf) return (uint64_t)0;
-      return whole(ldexp((double)r.sum, row_bits - kChunkBits) * exp2(((double)value_of(r.key) - top) * scale));
+      const double z0 = value_of(r.key);
+      return whole((double)r.sum * exp2((z0 - top) * scale - chunk_offset(z0, scale)), row_bits - kChunkBits);
     };
     for (int c = c0; c < c0 + per && c < a.chunks; ++c) part += chunk_mass(c);
     const uint64_t before = prefix(part, row_total, s);
@@ -673,26 +694,60 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
       const int c = (int)s.value[0];
       const RowChunk r = a.chunk[t * a.chunks + c];
       // that chunk again, with its own sums
-      const double z0 = value_of(r.key), inner = ldexp((double)s.value[1], kChunkBits - row_bits) * exp2((top - z0) * scale);
-      const int64_t begin = (int64_t)c * kRowThreads * a.per_thread, end = min(V, begin + (int64_t)kRowThreads * a.per_thread);
-      const int each = (int)((end - begin + kSelect - 1) / kSelect);
+      const double z0 = value_of(r.key), z0_scaled = z0 * scale;
+      const double inner = ldexp((double)s.value[1], kChunkBits - row_bits) * exp2((top - z0) * scale + chunk_offset(z0, scale));
+      // thread i has `each` entries from the i-th on
+      constexpr int VE = F32 ? 4 : 8, MOST = 32;
+      const int64_t begin = (int64_t)c * kRowThreads * a.per_thread;
+      const int each = max(VE, a.per_thread * kRowThreads / kSelect), entries = kRowThreads * a.per_thread;
       const int64_t i0 = begin + (int64_t)tid * each;
-      auto w_at = [&](int64_t i) { return whole(weight(((double)logit<F32>(row, i) - z0) * scale, kChunkBits)); };
+      float z[MOST];
+#pragma unroll
+      for (int j = 0; j < MOST; j += VE) {
+        const bool here = j < each && (tid + 1) * each <= entries;
+        float e[VE];
+        if (here && i0 + j + VE <= V) {
+          const u32x4_t v = load16((const char*)row + (i0 + j) * (F32 ? 4 : 2));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (F32) e[i] = __uint_as_float(v[i]);
+            else {
+              e[(2 * i) % VE] = __uint_as_float(v[i] << 16);
+              e[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < VE; ++i) e[i] = here && i0 + j + i < V ? logit<F32>(row, i0 + j + i) : -__builtin_inff();
+        }
+#pragma unroll
+        for (int i = 0; i < VE; ++i) z[j + i] = e[i];
+      }
+      auto w_of = [&](float v) { return whole(weight(fma((double)v, scale, -z0_scaled)), kChunkBits); };
       uint64_t mine = 0;
-      for (int i = 0; i < each; ++i)
-        if (i0 + i < end) mine += w_at(i0 + i);
+#pragma unroll
+      for (int i = 0; i < MOST; ++i)
+        if (i < each) mine += w_of(z[i]);
       uint64_t all;
       const uint64_t ahead = prefix(mine, all, s);
       const uint64_t want = inner < (double)all ? (uint64_t)inner : all - 1;
       if (ahead <= want && want < ahead + mine) {
         uint64_t x = ahead;
-        for (int i = 0; i < each; ++i) {
-          x += w_at(i0 + i);
-          if (x > want) {
-            answer(i0 + i, log_p(logit<F32>(row, i0 + i), row_total, row_bits));
-            break;
+        int at = 0;
+        float found = 0.f;
+        bool done = false;
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) {
+          if (i < each && !done) {
+            x += w_of(z[i]);
+            if (x > want) {
+              at = i;
+              found = z[i];
+              done = true;
+            }
           }
         }
+        answer(i0 + at, log_p(found, row_total, row_bits));
       }
       return;
     }
@@ -715,7 +770,7 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     // thread i has entries i per .. + per - 1 of the list
     const uint32_t per = (found + kSelect - 1) / kSelect, i0 = tid * per;
     const double floor_w = ldexp((double)min_p, kChunkBits);
-    auto w_key = [&](uint32_t k_) { return whole(weight(((double)value_of(k_) - top) * scale, kChunkBits)); };
+    auto w_key = [&](uint32_t k_) { return whole(weight(((double)value_of(k_) - top) * scale), kChunkBits); };
     auto w_at = [&](uint32_t i) { return w_key((uint32_t)(s.list[i] >> 32)); };
     uint64_t part = 0;
     for (uint32_t i = i0; i < i0 + per && i < limit; ++i) part += w_at(i);
