@@ -42,7 +42,7 @@ __device__ __forceinline__ const void* row_of(const RowsArgs& a, int64_t t) {
 // in 32 bits would be off by 2^-24 in every sum that a uniform number is compared with: one token in some thousand would be another one.
 // ------------------------------------------------------------------------------------------------
 constexpr double kLog2e = 1.44269504088896340736;
-constexpr int kChunkBits = 48;         // a chunk's sums: 2^14 entries of at most 2^48
+constexpr int kChunkBits = 48;         // a chunk's sums: 2^14 entries of at most 2^48 (0x1p48 below)
 
 __device__ __forceinline__ double weight(double t) {
   t = fmax(t, -80.);                                   // (2^-80 and less count as nothing; also for a NaN, where a chunk is empty)
@@ -60,6 +60,10 @@ __device__ __forceinline__ double weight(double t) {
 }
 // A weight (or a sum of some) as a whole number of 2^-bits.
 __device__ __forceinline__ uint64_t whole(double w, int bits) { return (uint64_t)rint(ldexp(w, bits)); }
+// The same of a single one (less than 2^52 of them, so that they are the low bits of what 2^52 is added to); scale = 2^bits.
+__device__ __forceinline__ uint64_t whole_one(double w, double scale) {
+  return (uint64_t)(__double_as_longlong(fma(w, scale, 0x1p52)) - __double_as_longlong(0x1p52));
+}
 
 // A chunk's weights are 2^(z scale - zero) with zero = top scale, rounded: off by the same factor 2^offset all of them, offset = top scale - zero.
 __device__ __forceinline__ double chunk_offset(double top, double scale) { return fma(top, scale, -(top * scale)); }
@@ -180,7 +184,7 @@ constexpr int kList = 4096;            // entries of the list at most
 constexpr int kGroups = 1536;          // groups that are read again at most
 constexpr int kNear = 1792;            // bins by the distance from the largest key
 constexpr int kFlat = 2048;            // bins by the distance from the largest value
-constexpr int kTile = 4096, kEach = kTile / kSelect, kTilesAtOnce = 4;      // entries whose sum the slow way keeps
+constexpr int kTile = 4096, kEach = kTile / kSelect, kTilesAtOnce = 2;      // entries whose sum the slow way keeps
 // Sampling: groups that the list takes, for a top-k of at most kReach as many, else (top-p and min-p, mostly) kReachAll.
 constexpr int kReach = 1024, kReachAll = 512;
 
@@ -238,32 +242,48 @@ __device__ __forceinline__ uint32_t largest_key(const RowsArgs& a, int64_t t, Se
   return key;
 }
 
-// Entries of a row, 16 bytes a thread and several of them in flight: put(value, index).
+// Entries of a row, 16 bytes a thread and several of them in flight, the next ones while these are put: put(values, index of the first,
+// how many).
 template <bool F32, class Put>
 __device__ __forceinline__ void for_row(const void* row, int64_t V, Put&& put) {
   constexpr int VE = F32 ? 4 : 8, U = 4, STEP = kSelect * VE;
   int64_t base = (int64_t)threadIdx.x * VE;
   auto each = [&](const u32x4_t& v, int64_t at) {
+    float z[VE];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (F32) put(__uint_as_float(v[i]), at + i);
+      if (F32) z[i] = __uint_as_float(v[i]);
       else {
-        put(__uint_as_float(v[i] << 16), at + 2 * i);
-        put(__uint_as_float(v[i] & 0xffff0000u), at + 2 * i + 1);
+        z[(2 * i) % VE] = __uint_as_float(v[i] << 16);
+        z[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
       }
     }
+    put(z, (uint32_t)at, VE);
   };
-  for (; base - (int64_t)threadIdx.x * VE + U * STEP <= V; base += U * STEP) {
+  const int64_t rounds = V / (U * STEP);
+  u32x4_t next[U];
+  if (rounds)
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = load16((const char*)row + (base + u * STEP) * (F32 ? 4 : 2));
+  for (int64_t r = 0; r < rounds; ++r) {
     u32x4_t v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load16((const char*)row + (base + u * STEP) * (F32 ? 4 : 2));
+    for (int u = 0; u < U; ++u) v[u] = next[u];
+    const int64_t ahead = r + 1 < rounds ? base + U * STEP : base;
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = load16((const char*)row + (ahead + u * STEP) * (F32 ? 4 : 2));
 #pragma unroll
     for (int u = 0; u < U; ++u) each(v[u], base + u * STEP);
+    base += U * STEP;
   }
   for (; base < V; base += STEP) {
     if (base + VE <= V) each(load16((const char*)row + base * (F32 ? 4 : 2)), base);
-    else
-      for (int64_t i = base; i < V; ++i) put(logit<F32>(row, i), i);
+    else {
+      float z[VE];
+#pragma unroll
+      for (int i = 0; i < VE; ++i) z[i] = logit<F32>(row, base + i < V ? base + i : V - 1);
+      put(z, (uint32_t)base, (int)(V - base));
+    }
   }
 }
 
@@ -416,11 +436,11 @@ __device__ __forceinline__ void sort_list(uint32_t n, SelectLds& s) {
     }
 }
 
-// ---- the slow way: the last kept entry, as its key and the last index that counts among entries of that key ----
-struct Cut { uint32_t key; int64_t last; };
-constexpr Cut kAll = {0, INT64_MAX};
-
-__device__ __forceinline__ bool inside(const Cut& c, uint32_t key, int64_t i) { return key > c.key || (key == c.key && i <= c.last); }
+// ---- the slow way: the last kept entry, as its value and the last index that counts among entries of that value ----
+struct Cut { float z; uint32_t last; };
+__device__ __forceinline__ Cut cut_all() { return Cut{-__builtin_inff(), ~0u}; }
+// (bit operations: nothing branches around the weights of eight entries, which are computed side by side.  A NaN is inside.)
+__device__ __forceinline__ bool inside(const Cut& c, float z, uint32_t i) { return !((z < c.z) | ((z == c.z) & (i > c.last))); }
 
 struct Row {
   const void* p;
@@ -428,9 +448,9 @@ struct Row {
   float top;             // largest entry
   double scale;          // t = (z - top) scale
   float bins;            // flat bins to a unit of the logits
-  int bits;              // of a weight
+  double one;            // 2^bits, a weight of 1
 };
-__device__ __forceinline__ uint64_t row_weight(const Row& r, float z) { return whole(weight(((double)z - (double)r.top) * r.scale), r.bits); }
+__device__ __forceinline__ uint64_t row_weight(const Row& r, float z) { return whole_one(weight(((double)z - (double)r.top) * r.scale), r.one); }
 // Bin of an entry by its distance from the largest, all of the entries with a weight of 2^-44 and more in kFlat - 1 of them.
 __device__ __forceinline__ uint32_t flat_bin(const Row& r, float z) {
   const float x = (r.top - z) * r.bins;
@@ -469,16 +489,23 @@ __device__ __forceinline__ int64_t place_of(const Row& r, uint32_t key, uint64_t
 // inside reach), by eight bits of the key at a time.
 template <bool F32, bool MASS>
 __device__ __forceinline__ Cut narrow(const Row& r, const Cut& limit, uint64_t want, SelectLds& s) {
+  constexpr int VE = F32 ? 4 : 8;
   uint32_t high = 0;
 #pragma unroll 1
   for (int level = 0; level < 4; ++level) {
     const int shift = 24 - 8 * level;
     for (int i = threadIdx.x; i < 256; i += kSelect) s.bin_mass[i] = 0;
     __syncthreads();
-    for_row<F32>(r.p, r.V, [&](float z, int64_t i) {
-      const uint32_t k = key_of(z);
-      if ((level && (k ^ high) >> (shift + 8)) || !inside(limit, k, i)) return;
-      atomicAdd((unsigned long long*)&s.bin_mass[k >> shift & 255], (unsigned long long)(MASS ? row_weight(r, z) : 1));
+    for_row<F32>(r.p, r.V, [&](const float (&z)[VE], uint32_t at, int n) {
+      uint64_t w[VE];
+#pragma unroll
+      for (int i = 0; i < VE; ++i) w[i] = MASS ? row_weight(r, z[i]) : 1;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const uint32_t k = key_of(z[i]);
+        if (i < n && !(level && (k ^ high) >> (shift + 8)) && inside(limit, z[i], at + i))
+          atomicAdd((unsigned long long*)&s.bin_mass[k >> shift & 255], (unsigned long long)w[i]);
+      }
     });
     __syncthreads();
     const uint64_t mine = threadIdx.x < 256 ? s.bin_mass[255 - threadIdx.x] : 0;
@@ -498,21 +525,26 @@ __device__ __forceinline__ Cut narrow(const Row& r, const Cut& limit, uint64_t w
     const uint64_t w = row_weight(r, value_of(high));
     e = (want + w - 1) / w;
   }
-  return Cut{high, place_of<F32>(r, high, e, s)};
+  return Cut{value_of(high), (uint32_t)place_of<F32>(r, high, e, s)};
 }
 
 // The same by bins of the value: the one that holds the entry goes into the list, is sorted and counted through.  share: `want` is that share
 // of the sum inside `limit` (1: a number of entries).
 template <bool F32, bool MASS>
 __device__ __forceinline__ Cut cut_of(const Row& r, const Cut& limit, uint64_t want, double share, SelectLds& s) {
-  constexpr int PER = kFlat / kSelect;
+  constexpr int PER = kFlat / kSelect, VE = F32 ? 4 : 8;
   for (int i = threadIdx.x; i < kFlat; i += kSelect) s.flat[i] = 0;
   __syncthreads();
-  for_row<F32>(r.p, r.V, [&](float z, int64_t i) {
-    const uint32_t k = key_of(z);
-    if (!inside(limit, k, i)) return;
-    const uint64_t w = MASS ? row_weight(r, z) : 1;
-    if (w) atomicAdd((unsigned long long*)&s.flat[flat_bin(r, z)], (unsigned long long)w);
+  for_row<F32>(r.p, r.V, [&](const float (&z)[VE], uint32_t at, int n) {
+    uint64_t w[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+      w[i] = MASS ? row_weight(r, z[i]) : 1;
+      w[i] = (i < n) & inside(limit, z[i], at + i) ? w[i] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < VE; ++i)
+      if (w[i]) atomicAdd((unsigned long long*)&s.flat[flat_bin(r, z[i])], (unsigned long long)w[i]);
   });
   __syncthreads();
   uint64_t mine[PER], sum = 0, all;
@@ -535,12 +567,13 @@ __device__ __forceinline__ Cut cut_of(const Row& r, const Cut& limit, uint64_t w
   __syncthreads();
   const uint32_t bin = (uint32_t)s.value[0];
   const uint64_t left = want - s.value[1];
-  for_row<F32>(r.p, r.V, [&](float z, int64_t i) {
-    if (flat_bin(r, z) != bin) return;
-    const uint32_t k = key_of(z);
-    if (!inside(limit, k, i)) return;
-    const uint32_t to = atomicAdd(&s.count, 1u);
-    if (to < (uint32_t)kList) s.list[to] = (uint64_t)k << 32 | (uint32_t)~(uint32_t)i;
+  for_row<F32>(r.p, r.V, [&](const float (&z)[VE], uint32_t at, int n) {
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+      if (i >= n || flat_bin(r, z[i]) != bin || !inside(limit, z[i], at + i)) continue;
+      const uint32_t to = atomicAdd(&s.count, 1u);
+      if (to < (uint32_t)kList) s.list[to] = (uint64_t)key_of(z[i]) << 32 | (uint32_t)~(at + i);
+    }
   });
   __syncthreads();
   const uint32_t n = s.count;
@@ -563,7 +596,7 @@ __device__ __forceinline__ Cut cut_of(const Row& r, const Cut& limit, uint64_t w
   __syncthreads();
   const uint64_t e = s.value[0];
   __syncthreads();
-  return Cut{(uint32_t)(e >> 32), (int64_t)(uint32_t)~(uint32_t)e};
+  return Cut{value_of((uint32_t)(e >> 32)), ~(uint32_t)e};
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -611,13 +644,18 @@ __global__ __launch_bounds__(kSelect) void top_select_kernel(const RowsArgs a) {
   if ((int64_t)a.K < n) bound = max(bound, bound_of(a.group + t * n, n, (uint32_t)a.K, key, s));
   uint32_t found = gather<F32>(a, t, bound, s);
   if (found > (uint32_t)kList) {
-    const Row r{row_of<F32>(a, t), a.V, value_of(key), 0, 0.f, 0};
-    const Cut cut = narrow<F32, false>(r, kAll, (uint64_t)a.K, s);
+    const Row r{row_of<F32>(a, t), a.V, value_of(key), 0, 0.f, 0.};
+    constexpr int VE = F32 ? 4 : 8;
+    const Cut cut = narrow<F32, false>(r, cut_all(), (uint64_t)a.K, s);
+    const uint32_t last = key_of(cut.z);               // (by keys: it may be a NaN)
     if (tid == 0) s.count = 0;
     __syncthreads();
-    for_row<F32>(r.p, r.V, [&](float z, int64_t i) {
-      const uint32_t k = key_of(z);
-      if (k > kKeyMinusInf && inside(cut, k, i)) s.list[atomicAdd(&s.count, 1u)] = (uint64_t)k << 32 | (uint32_t)~(uint32_t)i;
+    for_row<F32>(r.p, r.V, [&](const float (&z)[VE], uint32_t at, int n_) {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const uint32_t k = key_of(z[i]);
+        if (i < n_ && k > kKeyMinusInf && (k > last || (k == last && at + i <= cut.last))) s.list[atomicAdd(&s.count, 1u)] = (uint64_t)k << 32 | (uint32_t)~(at + i);
+      }
     });
     __syncthreads();
     found = s.count;
@@ -723,7 +761,7 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
 #pragma unroll
         for (int i = 0; i < VE; ++i) z[j + i] = e[i];
       }
-      auto w_of = [&](float v) { return whole(weight(fma((double)v, scale, -z0_scaled)), kChunkBits); };
+      auto w_of = [&](float v) { return whole_one(weight(fma((double)v, scale, -z0_scaled)), 0x1p48); };
       uint64_t mine = 0;
 #pragma unroll
       for (int i = 0; i < MOST; ++i)
@@ -770,7 +808,7 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     // thread i has entries i per .. + per - 1 of the list
     const uint32_t per = (found + kSelect - 1) / kSelect, i0 = tid * per;
     const double floor_w = ldexp((double)min_p, kChunkBits);
-    auto w_key = [&](uint32_t k_) { return whole(weight(((double)value_of(k_) - top) * scale), kChunkBits); };
+    auto w_key = [&](uint32_t k_) { return whole_one(weight(((double)value_of(k_) - top) * scale), 0x1p48); };
     auto w_at = [&](uint32_t i) { return w_key((uint32_t)(s.list[i] >> 32)); };
     uint64_t part = 0;
     for (uint32_t i = i0; i < i0 + per && i < limit; ++i) part += w_at(i);
@@ -818,24 +856,31 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
 
   // the slow way
   __syncthreads();
-  const Row r{row, V, (float)top, scale, (float)((kFlat - 1) / 44. * scale), row_bits};
-  Cut cut = kAll;
-  if (k < V) cut = cut_of<F32, false>(r, kAll, (uint64_t)k, 1., s);
+  const Row r{row, V, (float)top, scale, (float)((kFlat - 1) / 44. * scale), ldexp(1., row_bits)};
+  Cut cut = cut_all();
+  if (k < V) cut = cut_of<F32, false>(r, cut, (uint64_t)k, 1., s);
   if (top_p < 1.f) cut = cut_of<F32, true>(r, cut, 0, (double)top_p, s);
   const double floor_w = ldexp((double)min_p, row_bits);
+  const uint64_t floor_whole = (uint64_t)ceil(floor_w);
   auto w_kept = [&](float z, int64_t i) {
-    if (!inside(cut, key_of(z), i)) return (uint64_t)0;
     const uint64_t w = row_weight(r, z);
-    return (double)w >= floor_w ? w : (uint64_t)0;
+    return inside(cut, z, (uint32_t)i) & (w >= floor_whole) ? w : (uint64_t)0;
   };
   // the tile in which the sum passes the target, and the entry in the tile
   const int tiles = (int)((V + kTile - 1) / kTile);
   for (int i = tid; i < tiles; i += kSelect) s.mass[i] = 0;
   __syncthreads();
+  float ahead[kTilesAtOnce][kEach];
+#pragma unroll
+  for (int j = 0; j < kTilesAtOnce; ++j) load_tile<F32>(ahead[j], row, V, (int64_t)j * kTile + tid * kEach);
   for (int b = 0; b < tiles; b += kTilesAtOnce) {
     float z[kTilesAtOnce][kEach];
 #pragma unroll
-    for (int j = 0; j < kTilesAtOnce; ++j) load_tile<F32>(z[j], row, V, (int64_t)(b + j) * kTile + tid * kEach);
+    for (int j = 0; j < kTilesAtOnce; ++j) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) z[j][i] = ahead[j][i];
+      load_tile<F32>(ahead[j], row, V, (int64_t)(b + kTilesAtOnce + j) * kTile + tid * kEach);
+    }
 #pragma unroll
     for (int j = 0; j < kTilesAtOnce; ++j) {
       uint64_t w = 0;

@@ -88,6 +88,19 @@ def test_top_logits_of_rows_that_have_none_or_no_numbers():
         check_top(z.to(dtype), 9, 1.0, out)
 
 
+def test_top_logits_of_rows_with_more_equal_ones_than_a_list_holds():
+    z = torch.randn(6, 20_000)
+    z[0, 5000:] = float("nan")
+    z[1, ::2] = 9.0
+    z[2, 3000:] = float("inf")
+    z[3, ::3], z[3, 1::3] = 0.0, -0.0
+    z[4] = float(torch.finfo(torch.float32).min)
+    z[5, 100:] = -float("inf")
+    for dtype in (torch.float32, torch.bfloat16):
+        for K_ in (1, 700, 1024):
+            check_top(z.to(dtype), K_, 1.0, K.kd_top_logits(z.to(dtype).cuda(), K_))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("offset,ld", [(1, 2100), (3, 2051), (8, 4096)])
 def test_rows_of_a_wider_array_at_an_odd_offset(dtype, offset, ld):
