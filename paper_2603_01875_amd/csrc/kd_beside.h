@@ -38,6 +38,13 @@ struct RowChunk {
   float part;        // top logits: the same in fp32
   uint32_t key;      // the largest entry's
 };
+// Sampling under top-p or min-p alone, at most kWideRows rows of more than a list: sums by bins, sums of tiles (kWideTile entries), and the entries of
+// the bin in which the last kept one lies.
+constexpr int kWideRows = 1024, kWideBins = 2048, kWideList = 4096, kWideTile = 4096;
+struct RowWide {
+  uint64_t bins[kWideBins], list[kWideList];
+  uint32_t count, reserved[3];
+};
 struct RowsArgs {
   const void* logits;
   int64_t T, V, ld;
@@ -58,6 +65,9 @@ struct RowsArgs {
   // workspace
   RowChunk* chunk;            // [T][chunks]
   uint32_t* group;            // [T][chunks * kRowThreads]
+  RowWide* wide;              // [T], null unless the wide kernels are launched
+  uint64_t* wide_mass;        // [T][tiles]
+  int wide_parts;             // workgroups a row
 };
 hipError_t launch_top_logits(const RowsArgs& r, hipStream_t st);
 hipError_t launch_sample(const RowsArgs& r, hipStream_t st);

@@ -60,7 +60,7 @@ kd::ProductArgs product_args(const kd_linear_params& p, const uint8_t* a, const 
 }
 
 // ---- rows of logits ----
-struct RowsLayout { size_t chunk, group, total; };
+struct RowsLayout { size_t chunk, group, wide, mass, total; };
 
 // Entries per thread of the first kernel: the most that leave two workgroups a CU and four groups for each entry of a list of `reach`;
 // rows have at most 1024 chunks.
@@ -108,6 +108,13 @@ kd_status plan(const kd_sample_params* p, kd::RowsArgs& r, RowsLayout& L) {
   r.T = p->T; r.V = p->V; r.ld = p->ld; r.f32 = p->in_dtype == KD_F32; r.index64 = p->index_dtype == KD_I64;
   r.tau = p->temperature; r.top_k = p->top_k; r.top_p = p->top_p; r.min_p = p->min_p;
   plan_rows(r, L, 256);
+  if (r.T <= kd::kWideRows && r.V > kd::kWideList) {
+    const int64_t tiles = (r.V + kd::kWideTile - 1) / kd::kWideTile, parts = 4 * kd::kNumCU / r.T;
+    r.wide_parts = (int)(parts < 1 ? 1 : parts < tiles ? parts : tiles);
+    L.wide = L.total;
+    L.mass = (size_t)round_up((int64_t)L.wide + r.T * (int64_t)sizeof(kd::RowWide), 256);
+    L.total = (size_t)round_up((int64_t)L.mass + r.T * tiles * 8, 256);
+  }
   return KD_OK;
 }
 
@@ -282,6 +289,11 @@ kd_status kd_sample(const kd_sample_params* params, const void* logits, const fl
   // (who draws from all entries needs no groups)
   const bool same = !temperature_rows && !top_k_rows && !top_p_rows && !min_p_rows;
   if (same && r.tau > 0.f && (r.top_k == 0 || r.top_k >= r.V) && r.top_p == 1.f && r.min_p == 0.f) r.group = nullptr;
+  const bool all_k = r.top_k_rows || r.top_k == 0 || r.top_k >= r.V, cuts = r.top_p_rows || r.min_p_rows || r.top_p < 1.f || r.min_p > 0.f;
+  if (r.wide_parts && all_k && cuts) {
+    r.wide = reinterpret_cast<kd::RowWide*>(static_cast<char*>(workspace) + L.wide);
+    r.wide_mass = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + L.mass);
+  }
   KD_TRY(kd::launch_sample(r, static_cast<hipStream_t>(hip_stream)));
   return KD_OK;
 }

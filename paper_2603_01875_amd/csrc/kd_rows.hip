@@ -1,12 +1,15 @@
 // Rows of logits: the top logits of each (kd_top_logits), one token sampled from each (kd_sample).
 //
 // Both read the logits once.  A first kernel, a workgroup to a piece of a row (a chunk), leaves the chunk's sum of w = exp((z - largest of
-// the chunk) / tau) and, per thread, the largest entry of its share (a group).  A second, a workgroup to a row, works on these: the
+// the chunk) / tau) and, per thread, the largest entry of its share (a group).  The last, a workgroup to a row, works on these: the
 // G-th largest of the groups' largest entries is a bound that at least G entries reach, and only groups that reach it hold entries
 // that do, so that a few hundred groups are read again, and a short list is sorted.  Sampling from all of a row needs the sums alone: the
-// chunk in which the sum of w passes u times the whole is read again.  A list that does not fit, or does not reach far enough (thousands of
-// equal entries, a flat distribution under top-p), sends its row down the slow way: passes over the row that narrow the last kept
-// entry down by eight bits of its key at a time.
+// chunk in which the sum of w passes u times the whole is read again.
+// Sampling under top-p or min-p without a top-k may keep any number of entries.  There two kernels come between, again many workgroups
+// to a row (wide): one adds up w by bins of the logit, the other the w above the bin in which the sum passes top-p of the whole, tile by tile, and
+// lists that bin's entries.
+// A list that does not fit (thousands of equal entries), a top-k of more than a list, and very many rows go the slow way: passes of the last kernel
+// over the row that narrow the last kept entry down.
 #include <hip/hip_runtime.h>
 
 #include "kd_beside.h"
@@ -141,6 +144,10 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) key = max(key, keys[w]);
+  if (SAMPLE && a.wide && c == 0) {                    // (the wide kernels add to these)
+    for (int i = tid; i < kWideBins; i += NT) a.wide[t].bins[i] = 0;
+    if (tid == 0) a.wide[t].count = 0;
+  }
   const float top = value_of(key);
   RowChunk out{0, 0.f, key};
   if (SAMPLE) {
@@ -180,11 +187,11 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
 // second kernel: pieces
 // ------------------------------------------------------------------------------------------------
 constexpr int kSelect = 512;           // threads
-constexpr int kList = 4096;            // entries of the list at most
+constexpr int kList = kWideList;       // entries of the list at most
 constexpr int kGroups = 1536;          // groups that are read again at most
 constexpr int kNear = 1792;            // bins by the distance from the largest key
-constexpr int kFlat = 2048;            // bins by the distance from the largest value
-constexpr int kTile = 4096, kEach = kTile / kSelect, kTilesAtOnce = 2;      // entries whose sum the slow way keeps
+constexpr int kFlat = kWideBins;       // bins by the distance from the largest value
+constexpr int kTile = kWideTile, kEach = kTile / kSelect;      // entries whose sum the slow way keeps
 // Sampling: groups that the list takes, for a top-k of at most kReach as many, else (top-p and min-p, mostly) kReachAll.
 constexpr int kReach = 1024, kReachAll = 512;
 
@@ -667,6 +674,140 @@ __global__ __launch_bounds__(kSelect) void top_select_kernel(const RowsArgs a) {
 // ------------------------------------------------------------------------------------------------
 // sampling
 // ------------------------------------------------------------------------------------------------
+// A row's settings, and whether it can be drawn from.
+struct Draw {
+  float u, tau, top_p, min_p;
+  int64_t top_k;
+  bool greedy, all_k, valid;
+  // top-p and min-p over all entries, for which the wide kernels work
+  __device__ __forceinline__ bool wide() const { return valid && all_k && (top_p < 1.f || min_p > 0.f); }
+};
+__device__ __forceinline__ Draw draw_of(const RowsArgs& a, int64_t t, uint32_t key) {
+  Draw d;
+  d.u = a.u[t];
+  d.tau = row_temperature(a, t);
+  d.top_p = a.top_p_rows ? a.top_p_rows[t] : a.top_p;
+  d.min_p = a.min_p_rows ? a.min_p_rows[t] : a.min_p;
+  d.top_k = a.top_k_rows ? a.top_k_rows[t] : a.top_k;
+  d.greedy = d.tau == 0.f;
+  d.all_k = !d.greedy && (d.top_k == 0 || d.top_k >= a.V);
+  d.valid = d.u >= 0.f && d.u < 1.f && (d.greedy || (d.tau >= 1e-6f && d.tau <= 1e6f)) && d.top_k >= 0 && d.top_p > 0.f && d.top_p <= 1.f &&
+            d.min_p >= 0.f && d.min_p <= 1.f && key > kKeyMinusInf && key < kKeyInf;
+  return d;
+}
+// Bits of a weight in sums over a whole row: V entries of at most 2^bits.
+__device__ __forceinline__ int bits_of_row(int64_t V) { return min(kChunkBits, 62 - (64 - __clzll((unsigned long long)V))); }
+__device__ __forceinline__ Row row_for(const void* row, int64_t V, float top, double scale) {
+  return Row{row, V, top, scale, (float)((kFlat - 1) / 44. * scale), ldexp(1., bits_of_row(V))};
+}
+
+// The part of a row that a workgroup of the wide kernels has: tiles first .. last - 1.
+struct Part { int64_t t; int first, last; };
+__device__ __forceinline__ Part part_of(const RowsArgs& a) {
+  const int64_t piece = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const int tiles = (int)((a.V + kTile - 1) / kTile);
+  Part p;
+  p.t = piece / a.wide_parts;
+  const int i = (int)(piece - p.t * a.wide_parts), per = (tiles + a.wide_parts - 1) / a.wide_parts;
+  p.first = i * per;
+  p.last = min(tiles, p.first + per);
+  return p;
+}
+
+// w by bins, added to the row's (which the first kernel has cleared): whole numbers, so in any order.
+template <bool F32>
+__global__ __launch_bounds__(kSelect) void sample_bins_kernel(const RowsArgs a) {
+  __shared__ SelectLds s;
+  const Part p = part_of(a);
+  if (p.t >= a.T || p.first >= p.last) return;
+  const int tid = threadIdx.x;
+  const uint32_t key = largest_key(a, p.t, s);
+  const Draw d = draw_of(a, p.t, key);
+  if (!d.wide() || d.top_p == 1.f) return;
+  const Row r = row_for(row_of<F32>(a, p.t), a.V, value_of(key), kLog2e / (double)d.tau);
+  for (int i = tid; i < kFlat; i += kSelect) s.flat[i] = 0;
+  __syncthreads();
+  for (int b = p.first; b < p.last; ++b) {
+    float z[kEach];
+    uint64_t w[kEach];
+    load_tile<F32>(z, r.p, a.V, (int64_t)b * kTile + tid * kEach);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) w[i] = row_weight(r, z[i]);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (w[i]) atomicAdd((unsigned long long*)&s.flat[flat_bin(r, z[i])], (unsigned long long)w[i]);
+  }
+  __syncthreads();
+  for (int i = tid; i < kFlat; i += kSelect)
+    if (s.flat[i]) atomicAdd((unsigned long long*)&a.wide[p.t].bins[i], (unsigned long long)s.flat[i]);
+}
+
+// The bin in which the sum over the bins passes `share` of the whole, the sum in front of it and what is left to reach in it.
+struct Border { uint32_t bin; uint64_t left; };
+__device__ __forceinline__ Border border_of(const uint64_t* bins, double share, SelectLds& s) {
+  constexpr int PER = kFlat / kSelect;
+  uint64_t mine[PER], sum = 0, all;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) sum += mine[i] = bins[threadIdx.x * PER + i];
+  uint64_t before = prefix(sum, all, s);
+  uint64_t want = (uint64_t)ceil(share * (double)all);
+  want = want < 1 ? 1 : want < all ? want : all;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (before < want && before + mine[i] >= want) {
+      s.value[0] = threadIdx.x * PER + i;
+      s.value[1] = want - before;
+    }
+    before += mine[i];
+  }
+  __syncthreads();
+  const Border b{(uint32_t)s.value[0], s.value[1]};
+  __syncthreads();
+  return b;
+}
+
+// Each tile's sum of the kept w above that bin, and the bin's entries (as many as there is room for, and their number).
+template <bool F32>
+__global__ __launch_bounds__(kSelect) void sample_tiles_kernel(const RowsArgs a) {
+  __shared__ SelectLds s;
+  const Part p = part_of(a);
+  if (p.t >= a.T || p.first >= p.last) return;
+  const int tid = threadIdx.x;
+  const uint32_t key = largest_key(a, p.t, s);
+  const Draw d = draw_of(a, p.t, key);
+  if (!d.wide()) return;
+  const Row r = row_for(row_of<F32>(a, p.t), a.V, value_of(key), kLog2e / (double)d.tau);
+  const uint32_t bin = d.top_p < 1.f ? border_of(a.wide[p.t].bins, (double)d.top_p, s).bin : ~0u;
+  const uint64_t least = (uint64_t)ceil((double)d.min_p * r.one);
+  for (int b = p.first; b < p.last; ++b) {
+    const int64_t at = (int64_t)b * kTile + tid * kEach;
+    float z[kEach];
+    load_tile<F32>(z, r.p, a.V, at);
+    uint64_t sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const uint64_t w = row_weight(r, z[i]);
+      sum += (flat_bin(r, z[i]) < bin) & (w >= least) ? w : 0;
+    }
+    if (bin != ~0u) {
+      uint32_t hits = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) hits |= (uint32_t)(flat_bin(r, z[i]) == bin && at + i < a.V) << i;
+      if (hits) {
+        uint32_t to = atomicAdd(&a.wide[p.t].count, (uint32_t)__popc(hits));
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+          if (hits >> i & 1) {
+            if (to < (uint32_t)kWideList) a.wide[p.t].list[to] = (uint64_t)key_of(z[i]) << 32 | (uint32_t)~(uint32_t)(at + i);
+            ++to;
+          }
+      }
+    }
+    prefix(sum, all, s);
+    if (tid == 0) a.wide_mass[p.t * ((a.V + kTile - 1) / kTile) + b] = all;
+  }
+}
+
 // The largest whole number that is not above u total, and less than it.
 __device__ __forceinline__ uint64_t target_of(float u, uint64_t total) {
   const uint64_t x = (uint64_t)((double)u * (double)total);
@@ -679,24 +820,21 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
   const int64_t t = blockIdx.x, n = (int64_t)a.chunks * kRowThreads, V = a.V;
   const int tid = threadIdx.x;
   const void* const row = row_of<F32>(a, t);
-  const float u = a.u[t], tau = row_temperature(a, t);
-  const float top_p = a.top_p_rows ? a.top_p_rows[t] : a.top_p, min_p = a.min_p_rows ? a.min_p_rows[t] : a.min_p;
-  const int64_t top_k = a.top_k_rows ? a.top_k_rows[t] : a.top_k;
-  const bool greedy = tau == 0.f, all_k = !greedy && (top_k == 0 || top_k >= V);
   const uint32_t key = largest_key(a, t, s);
+  const Draw d = draw_of(a, t, key);
+  const float u = d.u, tau = d.tau, top_p = d.top_p, min_p = d.min_p;
+  const bool greedy = d.greedy, all_k = d.all_k;
   auto answer = [&](int64_t token, float logp) {
     if (a.index64) ((int64_t*)a.token)[t] = token;
     else ((int32_t*)a.token)[t] = (int32_t)token;
     if (a.logp) a.logp[t] = logp;
   };
-  const bool valid = u >= 0.f && u < 1.f && (tau == 0.f || (tau >= 1e-6f && tau <= 1e6f)) && top_k >= 0 && top_p > 0.f && top_p <= 1.f &&
-                     min_p >= 0.f && min_p <= 1.f && key > kKeyMinusInf && key < kKeyInf;
-  if (!valid) {
+  if (!d.valid) {
     if (tid == 0) answer(-1, __builtin_nanf(""));
     return;
   }
   const double top = value_of(key), scale = kLog2e / (greedy ? 1. : (double)tau);
-  const int row_bits = min(kChunkBits, 62 - (64 - __clzll((unsigned long long)V)));      // V entries of at most 2^row_bits
+  const int row_bits = bits_of_row(V);
   auto log_p = [&](float z, uint64_t total, int bits) {
     return greedy ? 0.f : (float)(((double)z - top) / (double)tau - log(ldexp((double)total, -bits)));
   };
@@ -791,8 +929,101 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     }
   }
 
+  const Row r = row_for(row, V, (float)top, scale);
+  const int tiles = (int)((V + kTile - 1) / kTile);
+  const uint64_t least = (uint64_t)ceil((double)min_p * r.one);
+  Cut cut = cut_all();
+  // The tile in which the sum of the kept w passes the target, and the entry in the tile; s.mass holds the tiles' sums.
+  auto finish = [&]() {
+    const int per = (tiles + kSelect - 1) / kSelect, b0 = tid * per;
+    uint64_t part = 0, total;
+    for (int b = b0; b < b0 + per && b < tiles; ++b) part += s.mass[b];
+    uint64_t x = prefix(part, total, s);
+    const uint64_t target = target_of(u, total);
+    if (x <= target && target < x + part)
+      for (int b = b0; b < b0 + per && b < tiles; ++b) {
+        if (target < x + s.mass[b]) {
+          s.value[0] = b;
+          s.value[1] = target - x;
+          break;
+        }
+        x += s.mass[b];
+      }
+    __syncthreads();
+    const int64_t at = (int64_t)s.value[0] * kTile + tid * kEach;
+    const uint64_t want = s.value[1];
+    float z[kEach];
+    uint64_t w[kEach], mine = 0, all;
+    load_tile<F32>(z, row, V, at);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      w[i] = row_weight(r, z[i]);
+      w[i] = inside(cut, z[i], (uint32_t)(at + i)) & (w[i] >= least) ? w[i] : 0;
+      mine += w[i];
+    }
+    uint64_t y = prefix(mine, all, s);
+    if (y <= want && want < y + mine) {
+      bool done = false;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        y += w[i];
+        if (y > want && !done) {
+          answer(at + i, log_p(z[i], total, row_bits));
+          done = true;
+        }
+      }
+    }
+  };
+
+  if (a.wide && d.wide()) {
+    const RowWide& wide = a.wide[t];
+    const uint64_t* const mass = a.wide_mass + t * tiles;
+    const uint32_t listed = top_p < 1.f ? wide.count : 0;
+    if (listed <= (uint32_t)kList) {
+      constexpr int HELD = kList / kSelect;
+      uint64_t held[HELD];                             // the thread's entries, in descending order
+      const uint32_t per = (listed + kSelect - 1) / kSelect, i0 = tid * per;
+      if (top_p < 1.f) {
+        const uint64_t left = border_of(wide.bins, (double)top_p, s).left;
+        for (uint32_t i = tid; i < listed; i += kSelect) s.list[i] = wide.list[i];
+        __syncthreads();
+        sort_list(listed, s);
+        uint64_t part = 0, all;
+        for (uint32_t i = i0; i < i0 + per && i < listed; ++i) part += row_weight(r, value_of((uint32_t)(s.list[i] >> 32)));
+        uint64_t x = prefix(part, all, s);
+        if (x < left && x + part >= left)
+          for (uint32_t i = i0; i < i0 + per && i < listed; ++i) {
+            x += row_weight(r, value_of((uint32_t)(s.list[i] >> 32)));
+            if (x >= left) {
+              s.value[0] = s.list[i];
+              break;
+            }
+          }
+        __syncthreads();
+        cut = Cut{value_of((uint32_t)(s.value[0] >> 32)), ~(uint32_t)s.value[0]};
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) held[i] = (uint32_t)i < per && i0 + i < listed ? s.list[i0 + i] : 0;
+        __syncthreads();
+      }
+      for (int i = tid; i < tiles; i += kSelect) s.mass[i] = mass[i];
+      __syncthreads();
+      if (top_p < 1.f)
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+          if (!held[i]) continue;
+          const float z = value_of((uint32_t)(held[i] >> 32));
+          const uint32_t at = ~(uint32_t)held[i];
+          const uint64_t w = row_weight(r, z);
+          if (inside(cut, z, at) && w >= least) atomicAdd((unsigned long long*)&s.mass[at / kTile], (unsigned long long)w);
+        }
+      __syncthreads();
+      finish();
+      return;
+    }
+  }
+
   // a short list of the largest entries
-  const int64_t k = greedy ? 1 : all_k ? V : top_k;
+  const int64_t k = greedy ? 1 : all_k ? V : d.top_k;
   const uint32_t reach = (uint32_t)(k <= kReach ? k : kReachAll);
   uint32_t bound = kKeyMinusInf + 1;
   if ((int64_t)reach < n) bound = max(bound, bound_of(a.group + t * n, n, reach, key, s));
@@ -856,73 +1087,30 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
 
   // the slow way
   __syncthreads();
-  const Row r{row, V, (float)top, scale, (float)((kFlat - 1) / 44. * scale), ldexp(1., row_bits)};
-  Cut cut = cut_all();
   if (k < V) cut = cut_of<F32, false>(r, cut, (uint64_t)k, 1., s);
   if (top_p < 1.f) cut = cut_of<F32, true>(r, cut, 0, (double)top_p, s);
-  const double floor_w = ldexp((double)min_p, row_bits);
-  const uint64_t floor_whole = (uint64_t)ceil(floor_w);
-  auto w_kept = [&](float z, int64_t i) {
-    const uint64_t w = row_weight(r, z);
-    return inside(cut, z, (uint32_t)i) & (w >= floor_whole) ? w : (uint64_t)0;
-  };
-  // the tile in which the sum passes the target, and the entry in the tile
-  const int tiles = (int)((V + kTile - 1) / kTile);
   for (int i = tid; i < tiles; i += kSelect) s.mass[i] = 0;
   __syncthreads();
-  float ahead[kTilesAtOnce][kEach];
+  float ahead[kEach];
+  load_tile<F32>(ahead, row, V, tid * kEach);
+  for (int b = 0; b < tiles; ++b) {
+    const int64_t at = (int64_t)b * kTile + tid * kEach;
+    float z[kEach];
+    uint64_t sum = 0;
 #pragma unroll
-  for (int j = 0; j < kTilesAtOnce; ++j) load_tile<F32>(ahead[j], row, V, (int64_t)j * kTile + tid * kEach);
-  for (int b = 0; b < tiles; b += kTilesAtOnce) {
-    float z[kTilesAtOnce][kEach];
+    for (int i = 0; i < kEach; ++i) z[i] = ahead[i];
+    load_tile<F32>(ahead, row, V, at + kTile);
 #pragma unroll
-    for (int j = 0; j < kTilesAtOnce; ++j) {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) z[j][i] = ahead[j][i];
-      load_tile<F32>(ahead[j], row, V, (int64_t)(b + kTilesAtOnce + j) * kTile + tid * kEach);
+    for (int i = 0; i < kEach; ++i) {
+      const uint64_t w = row_weight(r, z[i]);
+      sum += inside(cut, z[i], (uint32_t)(at + i)) & (w >= least) ? w : 0;
     }
 #pragma unroll
-    for (int j = 0; j < kTilesAtOnce; ++j) {
-      uint64_t w = 0;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) w += w_kept(z[j][i], (int64_t)(b + j) * kTile + tid * kEach + i);
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) w += __shfl_xor((unsigned long long)w, o, 64);
-      if ((tid & 63) == 0 && w) atomicAdd((unsigned long long*)&s.mass[b + j], (unsigned long long)w);
-    }
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor((unsigned long long)sum, o, 64);
+    if ((tid & 63) == 0 && sum) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)sum);
   }
   __syncthreads();
-  const int per = (tiles + kSelect - 1) / kSelect, b0 = tid * per;
-  uint64_t part = 0, total;
-  for (int b = b0; b < b0 + per && b < tiles; ++b) part += s.mass[b];
-  uint64_t x = prefix(part, total, s);
-  const uint64_t target = target_of(u, total);
-  if (x <= target && target < x + part)
-    for (int b = b0; b < b0 + per && b < tiles; ++b) {
-      if (target < x + s.mass[b]) {
-        s.value[0] = b;
-        s.value[1] = target - x;
-        break;
-      }
-      x += s.mass[b];
-    }
-  __syncthreads();
-  const int64_t at = (int64_t)s.value[0] * kTile + tid * kEach;
-  const uint64_t want = s.value[1];
-  uint64_t mine = 0, all;
-  for (int i = 0; i < kEach; ++i)
-    if (at + i < V) mine += w_kept(logit<F32>(row, at + i), at + i);
-  uint64_t y = prefix(mine, all, s);
-  if (y <= want && want < y + mine)
-    for (int i = 0; i < kEach; ++i) {
-      if (at + i >= V) break;
-      const float z = logit<F32>(row, at + i);
-      y += w_kept(z, at + i);
-      if (y > want) {
-        answer(at + i, log_p(z, total, row_bits));
-        break;
-      }
-    }
+  finish();
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -949,12 +1137,23 @@ hipError_t launch_top_logits(const RowsArgs& r, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_sample(const RowsArgs& r, hipStream_t st) {
-  const hipError_t e = r.f32 ? scan<true, true>(r, st) : scan<false, true>(r, st);
+template <bool F32>
+static hipError_t sample(const RowsArgs& r, hipStream_t st) {
+  hipError_t e = scan<F32, true>(r, st);
   if (e != hipSuccess) return e;
-  if (r.f32) hipLaunchKernelGGL(sample_select_kernel<true>, dim3((uint32_t)r.T), dim3(kSelect), 0, st, r);
-  else hipLaunchKernelGGL(sample_select_kernel<false>, dim3((uint32_t)r.T), dim3(kSelect), 0, st, r);
+  if (r.wide) {
+    const FlatGrid g = flat_grid(r.T * r.wide_parts);
+    if (r.top_p_rows || r.top_p < 1.f) {
+      hipLaunchKernelGGL(sample_bins_kernel<F32>, dim3(g.x, g.y), dim3(kSelect), 0, st, r);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(sample_tiles_kernel<F32>, dim3(g.x, g.y), dim3(kSelect), 0, st, r);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(sample_select_kernel<F32>, dim3((uint32_t)r.T), dim3(kSelect), 0, st, r);
   return hipGetLastError();
 }
+
+hipError_t launch_sample(const RowsArgs& r, hipStream_t st) { return r.f32 ? sample<true>(r, st) : sample<false>(r, st); }
 
 }  // namespace kd
