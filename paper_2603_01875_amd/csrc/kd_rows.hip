@@ -330,12 +330,28 @@ __device__ __forceinline__ uint32_t near_end(uint32_t bin) {
   return (((bin & 63) + 65) << (e - 6)) - 1;
 }
 
+// Keys of a row's groups (a multiple of 256), 16 bytes a thread and several of them in flight: put(key, number).
+template <class Put>
+__device__ __forceinline__ void for_groups(const uint32_t* group, int64_t n, Put&& put) {
+  constexpr int U = 4, STEP = kSelect * 4;
+  for (int64_t base = (int64_t)threadIdx.x * 4; base < n; base += U * STEP) {
+    u32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = *(const u32x4_t*)(group + (base + u * STEP < n ? base + u * STEP : base));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (base + u * STEP < n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) put(v[u][i], (uint32_t)(base + u * STEP + i));
+  }
+}
+
 // A key that at least G of the row's n groups reach, and not many more if the largest are spread a little.
 __device__ __forceinline__ uint32_t bound_of(const uint32_t* group, int64_t n, uint32_t G, uint32_t top, SelectLds& s) {
   constexpr int PER = (kNear + kSelect - 1) / kSelect;
   for (int i = threadIdx.x; i < kNear; i += kSelect) s.near_[i] = 0;
   __syncthreads();
-  for (int64_t i = threadIdx.x; i < n; i += kSelect) atomicAdd(&s.near_[near_bin(top - group[i])], 1u);
+  for_groups(group, n, [&](uint32_t key, uint32_t) { atomicAdd(&s.near_[near_bin(top - key)], 1u); });
   __syncthreads();
   uint32_t mine[PER], sum = 0;
 #pragma unroll
@@ -367,11 +383,11 @@ __device__ __forceinline__ uint32_t gather(const RowsArgs& a, int64_t t, uint32_
   const int J = a.per_thread / VE;
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
-  for (int64_t g = threadIdx.x; g < n; g += kSelect)
-    if (group[g] >= bound) {
-      const uint32_t to = atomicAdd(&s.count, 1u);
-      if (to < (uint32_t)kGroups) s.groups[to] = (uint32_t)g;
-    }
+  for_groups(group, n, [&](uint32_t key, uint32_t g) {
+    if (key < bound) return;
+    const uint32_t to = atomicAdd(&s.count, 1u);
+    if (to < (uint32_t)kGroups) s.groups[to] = g;
+  });
   __syncthreads();
   const uint32_t groups = s.count;
   __syncthreads();
@@ -439,8 +455,15 @@ __device__ __forceinline__ void sort_list(uint32_t n, SelectLds& s) {
           s.list[hi] = x;
         }
       }
-      __syncthreads();
+      // pairs up to 64 apart lie in 128 entries that one wave has from step to step: it waits for itself alone
+      const uint32_t after = j > 1 ? j >> 1 : k;
+      if (j > 64 || after > 64) __syncthreads();
+      else {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+      }
     }
+  __syncthreads();
 }
 
 // ---- the slow way: the last kept entry, as its value and the last index that counts among entries of that value ----
@@ -621,7 +644,7 @@ __device__ __forceinline__ void put_top(const RowsArgs& a, int64_t t, int at, ui
 }
 
 template <bool F32>
-__global__ __launch_bounds__(kSelect) void top_select_kernel(const RowsArgs a) {
+__global__ __launch_bounds__(kSelect, 8) void top_select_kernel(const RowsArgs a) {
   __shared__ SelectLds s;
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
@@ -1061,26 +1084,44 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     prefix(kept, n_kept, s);
     // the list says it all if it is the whole row, or holds the first top_k, or an entry of it that is not kept
     if (p_known && (reaches_k || n_kept < found)) {
-      // kept entries in order of their index
-      const uint32_t m = (uint32_t)n_kept, each = (m + kSelect - 1) / kSelect, j0 = tid * each;
-      for (uint32_t i = tid; i < m; i += kSelect) {
-        const uint64_t e = s.list[i];
-        s.list[i] = e << 32 | e >> 32;                 // (the index's complement in front: descending is by ascending index)
-      }
-      __syncthreads();
-      sort_list(m, s);
-      uint64_t mine = 0, total;
-      for (uint32_t j = j0; j < j0 + each && j < m; ++j) mine += w_key((uint32_t)s.list[j]);
-      uint64_t y = prefix(mine, total, s);
-      const uint64_t target = target_of(u, total);
-      if (y <= target && target < y + mine)
-        for (uint32_t j = j0; j < j0 + each && j < m; ++j) {
-          y += w_key((uint32_t)s.list[j]);
-          if (y > target) {
-            answer((int64_t)(uint32_t)~(uint32_t)(s.list[j] >> 32), log_p(value_of((uint32_t)s.list[j]), total, kChunkBits));
-            break;
-          }
+      const uint32_t m = (uint32_t)n_kept;
+      if (m <= (uint32_t)kSelect) {
+        // a thread's entry and its w; what lies in front of it in order of the index
+        uint64_t mine = 0, total;
+        uint32_t index = 0;
+        if (tid < (int)m) {
+          mine = w_at(tid);
+          index = ~(uint32_t)s.list[tid];
         }
+        prefix(mine, total, s);
+        const uint32_t value = tid < (int)m ? (uint32_t)(s.list[tid] >> 32) : 0;
+        __syncthreads();
+        if (tid < (int)m) s.list[tid] = (uint64_t)index;
+        uint64_t* const w = s.list + kSelect;
+        if (tid < (int)m) w[tid] = mine;
+        __syncthreads();
+        const uint64_t target = target_of(u, total);
+        if (tid < (int)m) {
+          uint64_t y = 0;
+          for (uint32_t i = 0; i < m; ++i) y += s.list[i] < index ? w[i] : 0;
+          if (y <= target && target < y + mine) answer(index, log_p(value_of(value), total, kChunkBits));
+        }
+        return;
+      }
+      // more of them: by tiles of the row
+      constexpr int HELD = kList / kSelect;
+      uint64_t held[HELD];
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) held[i] = tid + i * kSelect < m ? s.list[tid + i * kSelect] : 0;
+      cut = Cut{value_of((uint32_t)(s.list[m - 1] >> 32)), ~(uint32_t)s.list[m - 1]};
+      __syncthreads();
+      for (int i = tid; i < tiles; i += kSelect) s.mass[i] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (held[i]) atomicAdd((unsigned long long*)&s.mass[~(uint32_t)held[i] / kTile], (unsigned long long)row_weight(r, value_of((uint32_t)(held[i] >> 32))));
+      __syncthreads();
+      finish();
       return;
     }
   }
