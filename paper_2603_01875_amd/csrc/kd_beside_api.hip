@@ -68,7 +68,7 @@ void plan_rows(kd::RowsArgs& r, RowsLayout& L, int64_t reach) {
   int e = 64;
   for (; e > 8; e >>= 1) {
     const int64_t chunks = (r.V + kd::kRowThreads * e - 1) / (kd::kRowThreads * e);
-    if (r.T * chunks >= 2 * kd::kNumCU && r.V / e >= 4 * reach) break;
+    if (r.T * chunks >= 32 && r.V / e >= 4 * reach) break;
     if ((r.V + kd::kRowThreads * e / 2 - 1) / (kd::kRowThreads * e / 2) > 1024) break;
   }
   r.per_thread = e;

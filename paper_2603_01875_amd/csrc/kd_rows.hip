@@ -200,10 +200,10 @@ struct SelectLds {
     uint64_t list[kList];              // key, complement of the index: descending order is the order of the entries
     uint64_t mass[kList];              // chunks' or tiles' sums
     uint64_t flat[kFlat];
-    uint32_t near_[kNear];
   };
   union {
     uint32_t groups[kGroups];
+    uint32_t near_[kNear];
     uint64_t bin_mass[256];
   };
   uint64_t scan[kSelect / 64 + 1];
@@ -213,23 +213,37 @@ struct SelectLds {
   uint64_t value[2];
 };
 
+// v of the lane that a DPP control names, 0 where there is none (or the row mask leaves it out).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t lane_from(uint64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (uint64_t)hi << 32 | lo;
+}
+// Inclusive prefix sum over the wave: within rows of 16 lanes, then the rows' sums (a shuffle through LDS for each step took five times as long).
+__device__ __forceinline__ uint64_t wave_prefix(uint64_t v) {
+  v += lane_from<0x111, 0xf>(v);       // row_shr 1, 2, 4, 8
+  v += lane_from<0x112, 0xf>(v);
+  v += lane_from<0x114, 0xf>(v);
+  v += lane_from<0x118, 0xf>(v);
+  v += lane_from<0x142, 0xa>(v);       // row_bcast 15, into rows 1 and 3
+  v += lane_from<0x143, 0xc>(v);       // row_bcast 31, into rows 2 and 3
+  return v;
+}
+
 // Exclusive prefix sum over the workgroup; total to all.
 __device__ __forceinline__ uint64_t prefix(uint64_t v, uint64_t& total, SelectLds& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t y = __shfl_up((unsigned long long)x, o, 64);
-    if (lane >= o) x += y;
-  }
+  const uint64_t x = wave_prefix(v);
   __syncthreads();                     // (what an earlier call left has been read)
   if (lane == 63) s.scan[wave] = x;
   __syncthreads();
   uint64_t before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kSelect / 64; ++w) {
-    if (w < wave) before += s.scan[w];
-    all += s.scan[w];
+    const uint64_t y = s.scan[w];
+    before += w < wave ? y : 0;
+    all += y;
   }
   total = all;
   return before + x - v;
@@ -330,7 +344,7 @@ __device__ __forceinline__ uint32_t near_end(uint32_t bin) {
   return (((bin & 63) + 65) << (e - 6)) - 1;
 }
 
-// Keys of a row's groups (a multiple of 256), 16 bytes a thread and several of them in flight: put(key, number).
+// Keys of a row's groups (a multiple of 256), 16 bytes a thread and several of them in flight: put(four keys, number of the first).
 template <class Put>
 __device__ __forceinline__ void for_groups(const uint32_t* group, int64_t n, Put&& put) {
   constexpr int U = 4, STEP = kSelect * 4;
@@ -340,9 +354,7 @@ __device__ __forceinline__ void for_groups(const uint32_t* group, int64_t n, Put
     for (int u = 0; u < U; ++u) v[u] = *(const u32x4_t*)(group + (base + u * STEP < n ? base + u * STEP : base));
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (base + u * STEP < n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) put(v[u][i], (uint32_t)(base + u * STEP + i));
+      if (base + u * STEP < n) put(v[u], (uint32_t)(base + u * STEP));
   }
 }
 
@@ -351,7 +363,10 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t* group, int64_t n, u
   constexpr int PER = (kNear + kSelect - 1) / kSelect;
   for (int i = threadIdx.x; i < kNear; i += kSelect) s.near_[i] = 0;
   __syncthreads();
-  for_groups(group, n, [&](uint32_t key, uint32_t) { atomicAdd(&s.near_[near_bin(top - key)], 1u); });
+  for_groups(group, n, [&](const u32x4_t& keys, uint32_t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) atomicAdd(&s.near_[near_bin(top - keys[i])], 1u);
+  });
   __syncthreads();
   uint32_t mine[PER], sum = 0;
 #pragma unroll
@@ -373,6 +388,26 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t* group, int64_t n, u
   return end < top ? top - end : 0;
 }
 
+// Places in a list for what the lanes have to put, N things each: one addition to the count for a wave.
+template <int N>
+__device__ __forceinline__ void places_in(uint32_t* count, const bool (&put)[N], uint32_t (&to)[N]) {
+  uint64_t lanes[N];
+  uint32_t all = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    lanes[i] = __ballot(put[i]);
+    to[i] = all + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes[i], 0));
+    all += (uint32_t)__popcll(lanes[i]);
+  }
+  if (!all) return;
+  uint32_t first = 0;
+  const int leader = __ffsll((unsigned long long)__ballot(1)) - 1;
+  if ((int)(threadIdx.x & 63) == leader) first = atomicAdd(count, all);
+  first = (uint32_t)__builtin_amdgcn_readlane((int)first, leader);
+#pragma unroll
+  for (int i = 0; i < N; ++i) to[i] += first;
+}
+
 // Entries of the row that reach `bound` into the list; their number, which may be more than fit (then the list is not whole).
 template <bool F32>
 __device__ __forceinline__ uint32_t gather(const RowsArgs& a, int64_t t, uint32_t bound, SelectLds& s) {
@@ -383,10 +418,15 @@ __device__ __forceinline__ uint32_t gather(const RowsArgs& a, int64_t t, uint32_
   const int J = a.per_thread / VE;
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
-  for_groups(group, n, [&](uint32_t key, uint32_t g) {
-    if (key < bound) return;
-    const uint32_t to = atomicAdd(&s.count, 1u);
-    if (to < (uint32_t)kGroups) s.groups[to] = g;
+  for_groups(group, n, [&](const u32x4_t& keys, uint32_t g) {
+    bool put[4];
+    uint32_t to[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put[i] = keys[i] >= bound;
+    places_in(&s.count, put, to);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (put[i] && to[i] < (uint32_t)kGroups) s.groups[to[i]] = g + i;
   });
   __syncthreads();
   const uint32_t groups = s.count;
@@ -394,31 +434,46 @@ __device__ __forceinline__ uint32_t gather(const RowsArgs& a, int64_t t, uint32_
   if (groups > (uint32_t)kGroups) return ~0u;
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
-  for (uint32_t q = threadIdx.x; q < groups * J; q += kSelect) {
-    const uint32_t g = s.groups[q / J], j = q % J;
-    const int64_t at = ((int64_t)(g / kRowThreads) * a.per_thread + j * VE) * kRowThreads + g % kRowThreads * VE;
-    if (at >= a.V) continue;
-    float z[VE];
-    if (at + VE <= a.V) {
-      const u32x4_t v = load16((const char*)row + at * (F32 ? 4 : 2));
+  // 16 bytes of a group a thread, U of them in flight
+  constexpr int U = 4;
+  const int shift = 31 - __clz(J);                     // (J is a power of two)
+  const uint32_t pieces = groups << shift;
+  for (uint32_t q0 = threadIdx.x; q0 - threadIdx.x < pieces; q0 += U * kSelect) {
+    u32x4_t v[U];
+    int64_t at[U];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (F32) z[i] = __uint_as_float(v[i]);
-        else {
-          z[(2 * i) % VE] = __uint_as_float(v[i] << 16);
-          z[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < VE; ++i) z[i] = at + i < a.V ? logit<F32>(row, at + i) : -__builtin_inff();
+    for (int u = 0; u < U; ++u) {
+      const uint32_t q = q0 + u * kSelect < pieces ? q0 + u * kSelect : 0;
+      const uint32_t g = s.groups[q >> shift], j = q & (J - 1);
+      at[u] = ((int64_t)(g / kRowThreads) * a.per_thread + j * VE) * kRowThreads + g % kRowThreads * VE;
+      if (q0 + u * kSelect >= pieces) at[u] = a.V;
+      v[u] = a.V >= VE ? load16((const char*)row + (at[u] + VE <= a.V ? at[u] : 0) * (F32 ? 4 : 2)) : u32x4_t{0, 0, 0, 0};
     }
 #pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      const uint32_t key = key_of(z[i]);
-      if (key < bound) continue;
-      const uint32_t to = atomicAdd(&s.count, 1u);
-      if (to < (uint32_t)kList) s.list[to] = (uint64_t)key << 32 | (uint32_t)~(uint32_t)(at + i);
+    for (int u = 0; u < U; ++u) {
+      float z[VE];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (F32) z[i] = __uint_as_float(v[u][i]);
+        else {
+          z[(2 * i) % VE] = __uint_as_float(v[u][i] << 16);
+          z[(2 * i + 1) % VE] = __uint_as_float(v[u][i] & 0xffff0000u);
+        }
+      }
+      if (at[u] + VE > a.V)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) z[i] = at[u] + i < a.V ? logit<F32>(row, at[u] + i) : -__builtin_inff();
+      bool put[VE];
+      uint32_t key[VE], to[VE];
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        key[i] = key_of(z[i]);
+        put[i] = key[i] >= bound;
+      }
+      places_in(&s.count, put, to);
+#pragma unroll
+      for (int i = 0; i < VE; ++i)
+        if (put[i] && to[i] < (uint32_t)kList) s.list[to[i]] = (uint64_t)key[i] << 32 | (uint32_t)~(uint32_t)(at[u] + i);
     }
   }
   __syncthreads();
@@ -427,17 +482,73 @@ __device__ __forceinline__ uint32_t gather(const RowsArgs& a, int64_t t, uint32_
   return found;
 }
 
-// Sorts list[0 .. n) in descending order (n at most kList; no entry twice).  Short lists: each entry counts the larger ones.
-__device__ __forceinline__ void sort_list(uint32_t n, SelectLds& s) {
-  if (n <= 256) {
+// Prefix sums over near_ in place (a bin's first place), the same for all threads afterwards.
+__device__ __forceinline__ void starts_of_bins(SelectLds& s) {
+  constexpr int PER = (kNear + kSelect - 1) / kSelect;
+  uint32_t mine[PER], sum = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = threadIdx.x * PER + i;
+    mine[i] = b < kNear ? s.near_[b] : 0;
+    sum += mine[i];
+  }
+  uint64_t all;
+  uint32_t before = (uint32_t)prefix(sum, all, s);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = threadIdx.x * PER + i;
+    if (b < kNear) s.near_[b] = before;
+    before += mine[i];
+  }
+  __syncthreads();
+}
+
+// Sorts list[0 .. n) in descending order (n at most kList; no entry twice); top: its largest key.  Short lists: each entry counts the larger
+// ones.  Longer ones: by bins of the distance from the top into the list's other half, then each counts the larger ones of its bin.  More
+// than half a list: by exchanges.
+__device__ __forceinline__ void sort_list(uint32_t n, uint32_t top, SelectLds& s) {
+  if (n <= 128) {
     uint64_t mine = 0;
     uint32_t rank = 0;
     if (threadIdx.x < n) {
       mine = s.list[threadIdx.x];
+#pragma unroll 8
       for (uint32_t i = 0; i < n; ++i) rank += s.list[i] > mine;
     }
     __syncthreads();
     if (threadIdx.x < n) s.list[rank] = mine;
+    __syncthreads();
+    return;
+  }
+  if (n <= kList / 2) {
+    constexpr int HELD = kList / 2 / kSelect;
+    for (int i = threadIdx.x; i < kNear; i += kSelect) s.near_[i] = 0;
+    __syncthreads();
+    uint64_t mine[HELD];
+    uint32_t bin[HELD], at[HELD];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+      const uint32_t i = threadIdx.x + h * kSelect;
+      if (i >= n) continue;
+      mine[h] = s.list[i];
+      bin[h] = near_bin(top - (uint32_t)(mine[h] >> 32));
+      at[h] = atomicAdd(&s.near_[bin[h]], 1u);
+    }
+    __syncthreads();
+    starts_of_bins(s);
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+      if (threadIdx.x + h * kSelect < n) s.list[kList / 2 + s.near_[bin[h]] + at[h]] = mine[h];
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+      if (threadIdx.x + h * kSelect >= n) continue;
+      const uint32_t first = s.near_[bin[h]], last = bin[h] + 1 < (uint32_t)kNear ? s.near_[bin[h] + 1] : n;
+      uint32_t rank = first;
+#pragma unroll 4
+      for (uint32_t i = first; i < last; ++i) rank += s.list[kList / 2 + i] > mine[h];
+      s.list[rank] = mine[h];
+    }
     __syncthreads();
     return;
   }
@@ -466,6 +577,67 @@ __device__ __forceinline__ void sort_list(uint32_t n, SelectLds& s) {
   __syncthreads();
 }
 
+// Entries that the threads hold (0: none; entry i of the list is the (i / kSelect)-th of thread i % kSelect).
+constexpr int kHeld = kList / kSelect;
+
+__device__ __forceinline__ void hold(uint64_t (&held)[kHeld], uint32_t n, const SelectLds& s) {
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h) {
+    const uint32_t i = threadIdx.x + h * kSelect;
+    held[h] = i < n ? s.list[i] : 0;
+  }
+}
+
+// The last entry of the fewest, in descending order and not behind `limit`, whose weights' sum is at least `want` (which all of them
+// reach; want > 0), by 11, 11, 10 bits of the key and 12, 12 of the index at a time.  Overwrites the list.  (weight(entry) is computed anew at each step, for
+// the entries that are still in question.)
+template <class Weight>
+__device__ __forceinline__ uint64_t last_of(const uint64_t (&held)[kHeld], uint64_t limit, uint64_t want, SelectLds& s, Weight&& weight) {
+  constexpr int PER = 4096 / kSelect;
+  uint64_t high = 0;
+#pragma unroll 1
+  for (int level = 0; level < 5; ++level) {
+    const int shift = level == 0 ? 53 : level == 1 ? 42 : level == 2 ? 32 : level == 3 ? 12 : 0, bits = level < 2 ? 11 : level == 2 ? 10 : 12;
+    const uint64_t above = level == 3 ? ~0ull << 32 : level ? ~0ull << (shift + bits) : 0;      // (an index has 24 bits, their complement 8 ones in front)
+    const int bins = 1 << bits;
+    __syncthreads();
+    for (int i = threadIdx.x; i < bins; i += kSelect) s.mass[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h)
+      if (held[h] && held[h] >= limit && ((held[h] ^ high) & above) == 0) {
+        const uint64_t w = weight(held[h]);
+        if (w) atomicAdd((unsigned long long*)&s.mass[held[h] >> shift & (bins - 1)], (unsigned long long)w);
+      }
+    __syncthreads();
+    // bins from the largest down, PER of them a thread
+    uint64_t sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int b = bins - 1 - ((int)threadIdx.x * PER + i);
+      sum += b >= 0 ? s.mass[b] : 0;
+    }
+    uint64_t before = prefix(sum, all, s);
+    if (before < want && before + sum >= want)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int b = bins - 1 - ((int)threadIdx.x * PER + i);
+        const uint64_t m = b >= 0 ? s.mass[b] : 0;
+        if (before < want && before + m >= want) {
+          s.value[0] = b;
+          s.value[1] = before;
+        }
+        before += m;
+      }
+    __syncthreads();
+    high |= s.value[0] << shift;
+    if (level >= 3) high |= 0xff000000ull;
+    want -= s.value[1];
+  }
+  __syncthreads();
+  return high;
+}
+
 // ---- the slow way: the last kept entry, as its value and the last index that counts among entries of that value ----
 struct Cut { float z; uint32_t last; };
 __device__ __forceinline__ Cut cut_all() { return Cut{-__builtin_inff(), ~0u}; }
@@ -481,6 +653,7 @@ struct Row {
   double one;            // 2^bits, a weight of 1
 };
 __device__ __forceinline__ uint64_t row_weight(const Row& r, float z) { return whole_one(weight(((double)z - (double)r.top) * r.scale), r.one); }
+__device__ __forceinline__ uint64_t entry_weight(const Row& r, uint64_t entry) { return row_weight(r, value_of((uint32_t)(entry >> 32))); }
 // Bin of an entry by its distance from the largest, all of the entries with a weight of 2^-44 and more in kFlat - 1 of them.
 __device__ __forceinline__ uint32_t flat_bin(const Row& r, float z) {
   const float x = (r.top - z) * r.bins;
@@ -609,23 +782,9 @@ __device__ __forceinline__ Cut cut_of(const Row& r, const Cut& limit, uint64_t w
   const uint32_t n = s.count;
   __syncthreads();
   if (n > (uint32_t)kList) return narrow<F32, MASS>(r, limit, want, s);
-  sort_list(n, s);
-  const uint32_t per = (n + kSelect - 1) / kSelect, i0 = threadIdx.x * per;
-  auto of = [&](uint32_t i) { return MASS ? row_weight(r, value_of((uint32_t)(s.list[i] >> 32))) : (uint64_t)1; };
-  uint64_t part = 0;
-  for (uint32_t i = i0; i < i0 + per && i < n; ++i) part += of(i);
-  uint64_t x = prefix(part, all, s);
-  if (x < left && x + part >= left)
-    for (uint32_t i = i0; i < i0 + per && i < n; ++i) {
-      x += of(i);
-      if (x >= left) {
-        s.value[0] = s.list[i];
-        break;
-      }
-    }
-  __syncthreads();
-  const uint64_t e = s.value[0];
-  __syncthreads();
+  uint64_t held[kHeld];
+  hold(held, n, s);
+  const uint64_t e = last_of(held, 0, left, s, [&](uint64_t entry) { return MASS ? entry_weight(r, entry) : (uint64_t)1; });
   return Cut{value_of((uint32_t)(e >> 32)), ~(uint32_t)e};
 }
 
@@ -690,7 +849,7 @@ __global__ __launch_bounds__(kSelect, 8) void top_select_kernel(const RowsArgs a
     __syncthreads();
     found = s.count;
   }
-  sort_list(found, s);
+  sort_list(found, key, s);
   for (int i = tid; i < a.K; i += kSelect) put_top<F32>(a, t, i, i < (int)found ? s.list[i] : 0);
 }
 
@@ -838,7 +997,7 @@ __device__ __forceinline__ uint64_t target_of(float u, uint64_t total) {
 }
 
 template <bool F32>
-__global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a) {
+__global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArgs a) {
   __shared__ SelectLds s;
   const int64_t t = blockIdx.x, n = (int64_t)a.chunks * kRowThreads, V = a.V;
   const int tid = threadIdx.x;
@@ -954,7 +1113,7 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
 
   const Row r = row_for(row, V, (float)top, scale);
   const int tiles = (int)((V + kTile - 1) / kTile);
-  const uint64_t least = (uint64_t)ceil((double)min_p * r.one);
+  uint64_t least = (uint64_t)ceil((double)min_p * r.one);
   Cut cut = cut_all();
   // The tile in which the sum of the kept w passes the target, and the entry in the tile; s.mass holds the tiles' sums.
   auto finish = [&]() {
@@ -1003,41 +1162,27 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
     const uint64_t* const mass = a.wide_mass + t * tiles;
     const uint32_t listed = top_p < 1.f ? wide.count : 0;
     if (listed <= (uint32_t)kList) {
-      constexpr int HELD = kList / kSelect;
-      uint64_t held[HELD];                             // the thread's entries, in descending order
-      const uint32_t per = (listed + kSelect - 1) / kSelect, i0 = tid * per;
+      uint64_t held[kHeld];
+      auto weight_of = [&](uint64_t entry) { return entry_weight(r, entry); };
       if (top_p < 1.f) {
         const uint64_t left = border_of(wide.bins, (double)top_p, s).left;
-        for (uint32_t i = tid; i < listed; i += kSelect) s.list[i] = wide.list[i];
-        __syncthreads();
-        sort_list(listed, s);
-        uint64_t part = 0, all;
-        for (uint32_t i = i0; i < i0 + per && i < listed; ++i) part += row_weight(r, value_of((uint32_t)(s.list[i] >> 32)));
-        uint64_t x = prefix(part, all, s);
-        if (x < left && x + part >= left)
-          for (uint32_t i = i0; i < i0 + per && i < listed; ++i) {
-            x += row_weight(r, value_of((uint32_t)(s.list[i] >> 32)));
-            if (x >= left) {
-              s.value[0] = s.list[i];
-              break;
-            }
-          }
-        __syncthreads();
-        cut = Cut{value_of((uint32_t)(s.value[0] >> 32)), ~(uint32_t)s.value[0]};
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) held[i] = (uint32_t)i < per && i0 + i < listed ? s.list[i0 + i] : 0;
-        __syncthreads();
+        for (int h = 0; h < kHeld; ++h) {
+          const uint32_t i = tid + h * kSelect;
+          held[h] = i < listed ? wide.list[i] : 0;
+        }
+        const uint64_t e = last_of(held, 0, left, s, weight_of);
+        cut = Cut{value_of((uint32_t)(e >> 32)), ~(uint32_t)e};
       }
       for (int i = tid; i < tiles; i += kSelect) s.mass[i] = mass[i];
       __syncthreads();
       if (top_p < 1.f)
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-          if (!held[i]) continue;
-          const float z = value_of((uint32_t)(held[i] >> 32));
-          const uint32_t at = ~(uint32_t)held[i];
-          const uint64_t w = row_weight(r, z);
-          if (inside(cut, z, at) && w >= least) atomicAdd((unsigned long long*)&s.mass[at / kTile], (unsigned long long)w);
+        for (int h = 0; h < kHeld; ++h) {
+          const uint32_t at = ~(uint32_t)held[h];
+          if (!held[h] || !inside(cut, value_of((uint32_t)(held[h] >> 32)), at)) continue;
+          const uint64_t w = weight_of(held[h]);
+          if (w >= least) atomicAdd((unsigned long long*)&s.mass[at / kTile], (unsigned long long)w);
         }
       __syncthreads();
       finish();
@@ -1053,76 +1198,105 @@ __global__ __launch_bounds__(kSelect) void sample_select_kernel(const RowsArgs a
   const bool all_listed = bound == kKeyMinusInf + 1;
   const uint32_t found = gather<F32>(a, t, bound, s);
   if (found <= (uint32_t)kList) {
-    sort_list(found, s);
+    uint64_t held[kHeld];
+    hold(held, found, s);
+    auto weight_of = [&](uint64_t entry) { return whole_one(weight(((double)value_of((uint32_t)(entry >> 32)) - top) * scale), 0x1p48); };
     if (greedy) {
-      if (tid == 0) answer((int64_t)(uint32_t)~(uint32_t)s.list[0], 0.f);
+      uint64_t most = held[0];
+#pragma unroll
+      for (int h = 1; h < kHeld; ++h) most = max(most, held[h]);
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) most = max(most, (uint64_t)__shfl_xor((unsigned long long)most, o, 64));
+      __syncthreads();
+      if ((tid & 63) == 0) s.scan[tid >> 6] = most;
+      __syncthreads();
+      if (tid == 0) {
+        for (int v = 1; v < kSelect / 64; ++v) most = max(most, s.scan[v]);
+        answer(~(uint32_t)most, 0.f);
+      }
       return;
     }
-    const uint32_t limit = k < (int64_t)found ? (uint32_t)k : found;
-    // thread i has entries i per .. + per - 1 of the list
-    const uint32_t per = (found + kSelect - 1) / kSelect, i0 = tid * per;
-    const double floor_w = ldexp((double)min_p, kChunkBits);
-    auto w_key = [&](uint32_t k_) { return whole_one(weight(((double)value_of(k_) - top) * scale), 0x1p48); };
-    auto w_at = [&](uint32_t i) { return w_key((uint32_t)(s.list[i] >> 32)); };
-    uint64_t part = 0;
-    for (uint32_t i = i0; i < i0 + per && i < limit; ++i) part += w_at(i);
-    uint64_t listed;
-    uint64_t x = prefix(part, listed, s);
+    // The list says it all if it is the whole row, holds the first top_k, or holds an entry that is not kept.
     const bool reaches_k = all_listed || k <= (int64_t)found;
-    // sum over the first top_k
-    const double base = all_k ? ldexp((double)row_total, kChunkBits - row_bits) : (double)listed;
-    const bool p_known = top_p == 1.f || all_k || reaches_k;
-    const double nucleus = top_p == 1.f ? __builtin_inf() : (double)top_p * base;
-    // an entry is kept if what is in front of it is less than the nucleus and its own w is not too small
-    uint32_t kept = 0;
-    for (uint32_t i = i0; i < i0 + per && i < limit; ++i) {
-      const uint64_t w = w_at(i);
-      if ((double)x < nucleus && (double)w >= floor_w) ++kept;
-      x += w;
-    }
-    uint64_t n_kept;
-    prefix(kept, n_kept, s);
-    // the list says it all if it is the whole row, or holds the first top_k, or an entry of it that is not kept
-    if (p_known && (reaches_k || n_kept < found)) {
-      const uint32_t m = (uint32_t)n_kept;
-      if (m <= (uint32_t)kSelect) {
-        // a thread's entry and its w; what lies in front of it in order of the index
-        uint64_t mine = 0, total;
-        uint32_t index = 0;
-        if (tid < (int)m) {
-          mine = w_at(tid);
-          index = ~(uint32_t)s.list[tid];
+    const uint64_t floor_w = (uint64_t)ceil((double)min_p * 0x1p48);
+    if (found <= 128) {
+      // one entry a thread: what is in front of it in descending order, then what is kept in front of it in order of the index
+      uint64_t* const ws = s.list + 128;
+      const uint64_t mine = held[0], my_w = mine ? weight_of(mine) : 0;
+      __syncthreads();
+      if (tid < 128) ws[tid] = my_w;
+      __syncthreads();
+      uint32_t rank = 0;
+      uint64_t before = 0, listed;
+      if (tid < (int)found)
+#pragma unroll 8
+        for (uint32_t i = 0; i < found; ++i) {
+          const bool larger = s.list[i] > mine;
+          rank += larger;
+          before += larger ? ws[i] : 0;
         }
-        prefix(mine, total, s);
-        const uint32_t value = tid < (int)m ? (uint32_t)(s.list[tid] >> 32) : 0;
-        __syncthreads();
-        if (tid < (int)m) s.list[tid] = (uint64_t)index;
-        uint64_t* const w = s.list + kSelect;
-        if (tid < (int)m) w[tid] = mine;
+      prefix(mine && (int64_t)rank < k ? my_w : 0, listed, s);      // the sum over the first top_k
+      const double base = all_k ? ldexp((double)row_total, kChunkBits - row_bits) : (double)listed;
+      const bool keep = mine && (int64_t)rank < k && (top_p == 1.f || (double)before < (double)top_p * base) && my_w >= floor_w;
+      uint64_t total, n_kept;
+      prefix(keep ? my_w : 0, total, s);
+      prefix(keep, n_kept, s);
+      if ((top_p == 1.f || all_k || reaches_k) && (reaches_k || n_kept < found)) {
+        if (tid < 128) ws[tid] = keep ? my_w : 0;
         __syncthreads();
         const uint64_t target = target_of(u, total);
-        if (tid < (int)m) {
+        if (keep) {
           uint64_t y = 0;
-          for (uint32_t i = 0; i < m; ++i) y += s.list[i] < index ? w[i] : 0;
-          if (y <= target && target < y + mine) answer(index, log_p(value_of(value), total, kChunkBits));
+#pragma unroll 8
+          for (uint32_t i = 0; i < found; ++i) y += ~(uint32_t)s.list[i] < ~(uint32_t)mine ? ws[i] : 0;
+          if (y <= target && target < y + my_w) answer(~(uint32_t)mine, log_p(value_of((uint32_t)(mine >> 32)), total, kChunkBits));
         }
         return;
       }
-      // more of them: by tiles of the row
-      constexpr int HELD = kList / kSelect;
-      uint64_t held[HELD];
+    } else {
+      // the last of the first top_k; of those, the last of the nucleus
+      uint64_t limit = 1;
+      if (k < (int64_t)found) limit = last_of(held, 0, (uint64_t)k, s, [](uint64_t) { return (uint64_t)1; });
+      bool settled = top_p == 1.f;
+      if (top_p < 1.f && (all_k || reaches_k)) {
+        uint64_t sum = 0, listed;
 #pragma unroll
-      for (int i = 0; i < HELD; ++i) held[i] = tid + i * kSelect < m ? s.list[tid + i * kSelect] : 0;
-      cut = Cut{value_of((uint32_t)(s.list[m - 1] >> 32)), ~(uint32_t)s.list[m - 1]};
-      __syncthreads();
-      for (int i = tid; i < tiles; i += kSelect) s.mass[i] = 0;
-      __syncthreads();
+        for (int h = 0; h < kHeld; ++h) sum += held[h] >= limit ? weight_of(held[h]) : 0;
+        prefix(sum, listed, s);
+        const double base = all_k ? ldexp((double)row_total, kChunkBits - row_bits) : (double)listed;
+        const uint64_t want = max((uint64_t)1, (uint64_t)ceil((double)top_p * base));
+        if (want <= listed || reaches_k) {
+          limit = last_of(held, limit, min(want, listed), s, weight_of);
+          settled = true;
+        }
+      }
+      // (entries by whose own w they are not kept are taken out)
+      uint64_t kept = 0, n_kept, least_kept = ~0ull;
 #pragma unroll
-      for (int i = 0; i < HELD; ++i)
-        if (held[i]) atomicAdd((unsigned long long*)&s.mass[~(uint32_t)held[i] / kTile], (unsigned long long)row_weight(r, value_of((uint32_t)(held[i] >> 32))));
-      __syncthreads();
-      finish();
-      return;
+      for (int h = 0; h < kHeld; ++h) {
+        const bool keep = held[h] >= limit && weight_of(held[h]) >= max(floor_w, (uint64_t)1);
+        held[h] = keep ? held[h] : 0;
+        kept += keep;
+        least_kept = keep ? min(least_kept, held[h]) : least_kept;
+      }
+      prefix(kept, n_kept, s);
+      if (settled && (reaches_k || n_kept < found)) {
+        // by tiles of the row, with a row's weights
+        for (int i = tid; i < tiles; i += kSelect) s.mass[i] = 0;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) least_kept = min(least_kept, (uint64_t)__shfl_xor((unsigned long long)least_kept, o, 64));
+        __syncthreads();
+        if ((tid & 63) == 0) s.scan[tid >> 6] = least_kept;
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+          if (held[h]) atomicAdd((unsigned long long*)&s.mass[~(uint32_t)held[h] / kTile], (unsigned long long)entry_weight(r, held[h]));
+        __syncthreads();
+        for (int v = 0; v < kSelect / 64; ++v) least_kept = min(least_kept, s.scan[v]);
+        cut = Cut{value_of((uint32_t)(least_kept >> 32)), ~(uint32_t)least_kept};
+        least = 0;                                     // (the cut has it in it)
+        finish();
+        return;
+      }
     }
   }
 
