@@ -38,8 +38,8 @@ struct RowChunk {
   float part;        // top logits: the same in fp32
   uint32_t key;      // the largest entry's
 };
-// Sampling under top-p or min-p alone, at most kWideRows rows of more than a list: sums by bins, sums of tiles (kWideTile entries), and the entries of
-// the bin in which the last kept one lies.
+// Sampling under top-p or min-p alone from rows of more than a list, kWideRows of them at a time: sums by bins, sums of tiles (kWideTile entries), and the
+// entries of the bin in which the last kept one lies.
 constexpr int kWideRows = 1024, kWideBins = 2048, kWideList = 4096, kWideTile = 4096;
 struct RowWide {
   uint64_t bins[kWideBins], list[kWideList];
@@ -65,8 +65,9 @@ struct RowsArgs {
   // workspace
   RowChunk* chunk;            // [T][chunks]
   uint32_t* group;            // [T][chunks * kRowThreads]
-  RowWide* wide;              // [T], null unless the wide kernels are launched
-  uint64_t* wide_mass;        // [T][tiles]
+  RowWide* wide;              // [kWideRows at most], null unless the wide kernels are launched
+  uint64_t* wide_mass;        // [kWideRows at most][tiles]
+  int64_t row0, rows_end;     // rows of this launch
   int wide_parts;             // workgroups a row
 };
 hipError_t launch_top_logits(const RowsArgs& r, hipStream_t st);

@@ -108,12 +108,13 @@ kd_status plan(const kd_sample_params* p, kd::RowsArgs& r, RowsLayout& L) {
   r.T = p->T; r.V = p->V; r.ld = p->ld; r.f32 = p->in_dtype == KD_F32; r.index64 = p->index_dtype == KD_I64;
   r.tau = p->temperature; r.top_k = p->top_k; r.top_p = p->top_p; r.min_p = p->min_p;
   plan_rows(r, L, 256);
-  if (r.T <= kd::kWideRows && r.V > kd::kWideList) {
-    const int64_t tiles = (r.V + kd::kWideTile - 1) / kd::kWideTile, parts = 4 * kd::kNumCU / r.T;
+  if (r.V > kd::kWideList) {
+    const int64_t rows = r.T < kd::kWideRows ? r.T : kd::kWideRows;
+    const int64_t tiles = (r.V + kd::kWideTile - 1) / kd::kWideTile, parts = 4 * kd::kNumCU / rows;
     r.wide_parts = (int)(parts < 1 ? 1 : parts < tiles ? parts : tiles);
     L.wide = L.total;
-    L.mass = (size_t)round_up((int64_t)L.wide + r.T * (int64_t)sizeof(kd::RowWide), 256);
-    L.total = (size_t)round_up((int64_t)L.mass + r.T * tiles * 8, 256);
+    L.mass = (size_t)round_up((int64_t)L.wide + rows * (int64_t)sizeof(kd::RowWide), 256);
+    L.total = (size_t)round_up((int64_t)L.mass + rows * tiles * 8, 256);
   }
   return KD_OK;
 }

@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) key = max(key, keys[w]);
-  if (SAMPLE && a.wide && c == 0) {                    // (the wide kernels add to these)
+  if (SAMPLE && a.wide && c == 0 && t < kWideRows) {   // (the wide kernels add to these; of later rows: wide_clear_kernel)
     for (int i = tid; i < kWideBins; i += NT) a.wide[t].bins[i] = 0;
     if (tid == 0) a.wide[t].count = 0;
   }
@@ -194,6 +194,7 @@ constexpr int kFlat = kWideBins;       // bins by the distance from the largest 
 constexpr int kTile = kWideTile, kEach = kTile / kSelect;      // entries whose sum the slow way keeps
 // Sampling: groups that the list takes, for a top-k of at most kReach as many, else (top-p and min-p, mostly) kReachAll.
 constexpr int kReach = 1024, kReachAll = 512;
+static_assert(kList / kSelect == kEach, "a thread's entries of a list and of a tile");
 
 struct SelectLds {
   union {
@@ -261,51 +262,6 @@ __device__ __forceinline__ uint32_t largest_key(const RowsArgs& a, int64_t t, Se
   for (int w = 0; w < kSelect / 64; ++w) key = max(key, s.word[w]);
   __syncthreads();
   return key;
-}
-
-// Entries of a row, 16 bytes a thread and several of them in flight, the next ones while these are put: put(values, index of the first,
-// how many).
-template <bool F32, class Put>
-__device__ __forceinline__ void for_row(const void* row, int64_t V, Put&& put) {
-  constexpr int VE = F32 ? 4 : 8, U = 4, STEP = kSelect * VE;
-  int64_t base = (int64_t)threadIdx.x * VE;
-  auto each = [&](const u32x4_t& v, int64_t at) {
-    float z[VE];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (F32) z[i] = __uint_as_float(v[i]);
-      else {
-        z[(2 * i) % VE] = __uint_as_float(v[i] << 16);
-        z[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
-      }
-    }
-    put(z, (uint32_t)at, VE);
-  };
-  const int64_t rounds = V / (U * STEP);
-  u32x4_t next[U];
-  if (rounds)
-#pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = load16((const char*)row + (base + u * STEP) * (F32 ? 4 : 2));
-  for (int64_t r = 0; r < rounds; ++r) {
-    u32x4_t v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = next[u];
-    const int64_t ahead = r + 1 < rounds ? base + U * STEP : base;
-#pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = load16((const char*)row + (ahead + u * STEP) * (F32 ? 4 : 2));
-#pragma unroll
-    for (int u = 0; u < U; ++u) each(v[u], base + u * STEP);
-    base += U * STEP;
-  }
-  for (; base < V; base += STEP) {
-    if (base + VE <= V) each(load16((const char*)row + base * (F32 ? 4 : 2)), base);
-    else {
-      float z[VE];
-#pragma unroll
-      for (int i = 0; i < VE; ++i) z[i] = logit<F32>(row, base + i < V ? base + i : V - 1);
-      put(z, (uint32_t)base, (int)(V - base));
-    }
-  }
 }
 
 // A thread's entries of a tile; minus infinity behind the row.
@@ -577,22 +533,42 @@ __device__ __forceinline__ void sort_list(uint32_t n, uint32_t top, SelectLds& s
   __syncthreads();
 }
 
-// Entries that the threads hold (0: none; entry i of the list is the (i / kSelect)-th of thread i % kSelect).
-constexpr int kHeld = kList / kSelect;
+struct Row {
+  const void* p;
+  int64_t V;
+  float top;             // largest entry
+  double scale;          // t = (z - top) scale
+  float bins;            // flat bins to a unit of the logits
+  double one;            // 2^bits, a weight of 1
+};
+__device__ __forceinline__ uint64_t row_weight(const Row& r, float z) { return whole_one(weight(((double)z - (double)r.top) * r.scale), r.one); }
+// Bin of an entry by its distance from the largest, all of the entries with a weight of 2^-44 and more in kFlat - 1 of them.
+__device__ __forceinline__ uint32_t flat_bin(const Row& r, float z) {
+  const float x = (r.top - z) * r.bins;
+  return x < (float)(kFlat - 1) ? (uint32_t)x : kFlat - 1;
+}
+// An entry: its key, the complement of its index.  Descending order is the order of the entries.
+__device__ __forceinline__ uint64_t entry_of(float z, uint32_t i) { return (uint64_t)key_of(z) << 32 | (uint32_t)~i; }
+__device__ __forceinline__ float entry_value(uint64_t e) { return value_of((uint32_t)(e >> 32)); }
+__device__ __forceinline__ uint32_t entry_index(uint64_t e) { return ~(uint32_t)e; }
 
-__device__ __forceinline__ void hold(uint64_t (&held)[kHeld], uint32_t n, const SelectLds& s) {
+// Entries that the threads hold (0: none).
+constexpr int kHeld = kList / kSelect;
+__device__ __forceinline__ void hold(uint64_t (&held)[kHeld], const uint64_t* list, uint32_t n) {
 #pragma unroll
   for (int h = 0; h < kHeld; ++h) {
     const uint32_t i = threadIdx.x + h * kSelect;
-    held[h] = i < n ? s.list[i] : 0;
+    held[h] = i < n ? list[i] : 0;
   }
 }
 
-// The last entry of the fewest, in descending order and not behind `limit`, whose weights' sum is at least `want` (which all of them
-// reach; want > 0), by 11, 11, 10 bits of the key and 12, 12 of the index at a time.  Overwrites the list.  (weight(entry) is computed anew at each step, for
-// the entries that are still in question.)
-template <class Weight>
-__device__ __forceinline__ uint64_t last_of(const uint64_t (&held)[kHeld], uint64_t limit, uint64_t want, SelectLds& s, Weight&& weight) {
+// The last entry of the fewest, in descending order and not behind `limit`, of those that are held or of the whole row, whose number (by_weight: sum
+// of w) is at least `want`, which all of them reach; want > 0.  By 11, 11, 10 bits of the key and 12, 12 of the index at a time, the
+// sums over a digit's values in LDS (overwrites the list).  One piece of code for all who ask: this kernel runs through each of its
+// parts once, and what it waits for is its own instructions (198 KB of them, with a copy of everything for each use, took twice as long).
+template <bool F32>
+__device__ __forceinline__ uint64_t last_of(const uint64_t (&held)[kHeld], bool whole_row, const Row& r, uint64_t limit, uint64_t want, bool by_weight,
+                                            SelectLds& s) {
   constexpr int PER = 4096 / kSelect;
   uint64_t high = 0;
 #pragma unroll 1
@@ -603,12 +579,35 @@ __device__ __forceinline__ uint64_t last_of(const uint64_t (&held)[kHeld], uint6
     __syncthreads();
     for (int i = threadIdx.x; i < bins; i += kSelect) s.mass[i] = 0;
     __syncthreads();
+    int64_t at = (int64_t)threadIdx.x * kEach;
+#pragma unroll 1
+    for (;;) {
+      uint64_t e[kHeld], w[kHeld];
+      bool in[kHeld], any = false;
+      if (whole_row) {
+        float z[kEach];
+        load_tile<F32>(z, r.p, r.V, at);
 #pragma unroll
-    for (int h = 0; h < kHeld; ++h)
-      if (held[h] && held[h] >= limit && ((held[h] ^ high) & above) == 0) {
-        const uint64_t w = weight(held[h]);
-        if (w) atomicAdd((unsigned long long*)&s.mass[held[h] >> shift & (bins - 1)], (unsigned long long)w);
+        for (int h = 0; h < kHeld; ++h) e[h] = at + h < r.V ? entry_of(z[h], (uint32_t)(at + h)) : 0;
+      } else {
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) e[h] = held[h];
       }
+#pragma unroll
+      for (int h = 0; h < kHeld; ++h) {
+        in[h] = e[h] && e[h] >= limit && ((e[h] ^ high) & above) == 0;
+        any |= in[h];
+        w[h] = 1;
+      }
+      if (any && by_weight)
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) w[h] = row_weight(r, entry_value(e[h]));
+#pragma unroll
+      for (int h = 0; h < kHeld; ++h)
+        if (in[h] && w[h]) atomicAdd((unsigned long long*)&s.mass[e[h] >> shift & (bins - 1)], (unsigned long long)w[h]);
+      at += kTile;
+      if (!whole_row || at - (int64_t)threadIdx.x * kEach >= r.V) break;
+    }
     __syncthreads();
     // bins from the largest down, PER of them a thread
     uint64_t sum = 0, all;
@@ -619,13 +618,13 @@ __device__ __forceinline__ uint64_t last_of(const uint64_t (&held)[kHeld], uint6
     }
     uint64_t before = prefix(sum, all, s);
     if (before < want && before + sum >= want)
-#pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int b = bins - 1 - ((int)threadIdx.x * PER + i);
         const uint64_t m = b >= 0 ? s.mass[b] : 0;
-        if (before < want && before + m >= want) {
+        if (before + m >= want) {
           s.value[0] = b;
           s.value[1] = before;
+          break;
         }
         before += m;
       }
@@ -636,156 +635,6 @@ __device__ __forceinline__ uint64_t last_of(const uint64_t (&held)[kHeld], uint6
   }
   __syncthreads();
   return high;
-}
-
-// ---- the slow way: the last kept entry, as its value and the last index that counts among entries of that value ----
-struct Cut { float z; uint32_t last; };
-__device__ __forceinline__ Cut cut_all() { return Cut{-__builtin_inff(), ~0u}; }
-// (bit operations: nothing branches around the weights of eight entries, which are computed side by side.  A NaN is inside.)
-__device__ __forceinline__ bool inside(const Cut& c, float z, uint32_t i) { return !((z < c.z) | ((z == c.z) & (i > c.last))); }
-
-struct Row {
-  const void* p;
-  int64_t V;
-  float top;             // largest entry
-  double scale;          // t = (z - top) scale
-  float bins;            // flat bins to a unit of the logits
-  double one;            // 2^bits, a weight of 1
-};
-__device__ __forceinline__ uint64_t row_weight(const Row& r, float z) { return whole_one(weight(((double)z - (double)r.top) * r.scale), r.one); }
-__device__ __forceinline__ uint64_t entry_weight(const Row& r, uint64_t entry) { return row_weight(r, value_of((uint32_t)(entry >> 32))); }
-// Bin of an entry by its distance from the largest, all of the entries with a weight of 2^-44 and more in kFlat - 1 of them.
-__device__ __forceinline__ uint32_t flat_bin(const Row& r, float z) {
-  const float x = (r.top - z) * r.bins;
-  return x < (float)(kFlat - 1) ? (uint32_t)x : kFlat - 1;
-}
-
-// Index of the e-th entry (from 1) of this key.
-template <bool F32>
-__device__ __forceinline__ int64_t place_of(const Row& r, uint32_t key, uint64_t e, SelectLds& s) {
-  constexpr int STEP = kSelect * 8;
-  for (int64_t base = 0;; base += STEP) {
-    const int64_t at = base + threadIdx.x * 8;
-    uint32_t hits = 0;
-    for (int i = 0; i < 8; ++i)
-      if (at + i < r.V && key_of(logit<F32>(r.p, at + i)) == key) hits |= 1u << i;
-    uint64_t all;
-    const uint64_t before = prefix(__popc(hits), all, s);
-    if (e <= all || base + STEP >= r.V) {
-      if (threadIdx.x == 0) s.value[0] = r.V - 1;
-      __syncthreads();
-      if (before < e && e <= before + __popc(hits)) {
-        uint64_t left = e - before;
-        for (int i = 0; i < 8; ++i)
-          if (hits >> i & 1 && --left == 0) s.value[0] = at + i;
-      }
-      __syncthreads();
-      const int64_t found = s.value[0];
-      __syncthreads();
-      return found;
-    }
-    e -= all;
-  }
-}
-
-// The last entry of the fewest, in descending order and inside `limit`, whose number (MASS: sum of w) is at least `want` (which those
-// inside reach), by eight bits of the key at a time.
-template <bool F32, bool MASS>
-__device__ __forceinline__ Cut narrow(const Row& r, const Cut& limit, uint64_t want, SelectLds& s) {
-  constexpr int VE = F32 ? 4 : 8;
-  uint32_t high = 0;
-#pragma unroll 1
-  for (int level = 0; level < 4; ++level) {
-    const int shift = 24 - 8 * level;
-    for (int i = threadIdx.x; i < 256; i += kSelect) s.bin_mass[i] = 0;
-    __syncthreads();
-    for_row<F32>(r.p, r.V, [&](const float (&z)[VE], uint32_t at, int n) {
-      uint64_t w[VE];
-#pragma unroll
-      for (int i = 0; i < VE; ++i) w[i] = MASS ? row_weight(r, z[i]) : 1;
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const uint32_t k = key_of(z[i]);
-        if (i < n && !(level && (k ^ high) >> (shift + 8)) && inside(limit, z[i], at + i))
-          atomicAdd((unsigned long long*)&s.bin_mass[k >> shift & 255], (unsigned long long)w[i]);
-      }
-    });
-    __syncthreads();
-    const uint64_t mine = threadIdx.x < 256 ? s.bin_mass[255 - threadIdx.x] : 0;
-    uint64_t all;
-    const uint64_t before = prefix(mine, all, s);
-    if (threadIdx.x < 256 && before < want && before + mine >= want) {
-      s.value[0] = 255 - threadIdx.x;
-      s.value[1] = before;
-    }
-    __syncthreads();
-    high |= (uint32_t)s.value[0] << shift;
-    want -= s.value[1];
-    __syncthreads();
-  }
-  uint64_t e = want;
-  if (MASS) {
-    const uint64_t w = row_weight(r, value_of(high));
-    e = (want + w - 1) / w;
-  }
-  return Cut{value_of(high), (uint32_t)place_of<F32>(r, high, e, s)};
-}
-
-// The same by bins of the value: the one that holds the entry goes into the list, is sorted and counted through.  share: `want` is that share
-// of the sum inside `limit` (1: a number of entries).
-template <bool F32, bool MASS>
-__device__ __forceinline__ Cut cut_of(const Row& r, const Cut& limit, uint64_t want, double share, SelectLds& s) {
-  constexpr int PER = kFlat / kSelect, VE = F32 ? 4 : 8;
-  for (int i = threadIdx.x; i < kFlat; i += kSelect) s.flat[i] = 0;
-  __syncthreads();
-  for_row<F32>(r.p, r.V, [&](const float (&z)[VE], uint32_t at, int n) {
-    uint64_t w[VE];
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      w[i] = MASS ? row_weight(r, z[i]) : 1;
-      w[i] = (i < n) & inside(limit, z[i], at + i) ? w[i] : 0;
-    }
-#pragma unroll
-    for (int i = 0; i < VE; ++i)
-      if (w[i]) atomicAdd((unsigned long long*)&s.flat[flat_bin(r, z[i])], (unsigned long long)w[i]);
-  });
-  __syncthreads();
-  uint64_t mine[PER], sum = 0, all;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) sum += mine[i] = s.flat[threadIdx.x * PER + i];
-  uint64_t before = prefix(sum, all, s);
-  if (MASS) {
-    want = (uint64_t)ceil(share * (double)all);
-    want = want < 1 ? 1 : want < all ? want : all;
-  }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    if (before < want && before + mine[i] >= want) {
-      s.value[0] = threadIdx.x * PER + i;
-      s.value[1] = before;
-    }
-    before += mine[i];
-  }
-  if (threadIdx.x == 0) s.count = 0;
-  __syncthreads();
-  const uint32_t bin = (uint32_t)s.value[0];
-  const uint64_t left = want - s.value[1];
-  for_row<F32>(r.p, r.V, [&](const float (&z)[VE], uint32_t at, int n) {
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      if (i >= n || flat_bin(r, z[i]) != bin || !inside(limit, z[i], at + i)) continue;
-      const uint32_t to = atomicAdd(&s.count, 1u);
-      if (to < (uint32_t)kList) s.list[to] = (uint64_t)key_of(z[i]) << 32 | (uint32_t)~(at + i);
-    }
-  });
-  __syncthreads();
-  const uint32_t n = s.count;
-  __syncthreads();
-  if (n > (uint32_t)kList) return narrow<F32, MASS>(r, limit, want, s);
-  uint64_t held[kHeld];
-  hold(held, n, s);
-  const uint64_t e = last_of(held, 0, left, s, [&](uint64_t entry) { return MASS ? entry_weight(r, entry) : (uint64_t)1; });
-  return Cut{value_of((uint32_t)(e >> 32)), ~(uint32_t)e};
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -833,19 +682,20 @@ __global__ __launch_bounds__(kSelect, 8) void top_select_kernel(const RowsArgs a
   if ((int64_t)a.K < n) bound = max(bound, bound_of(a.group + t * n, n, (uint32_t)a.K, key, s));
   uint32_t found = gather<F32>(a, t, bound, s);
   if (found > (uint32_t)kList) {
-    const Row r{row_of<F32>(a, t), a.V, value_of(key), 0, 0.f, 0.};
-    constexpr int VE = F32 ? 4 : 8;
-    const Cut cut = narrow<F32, false>(r, cut_all(), (uint64_t)a.K, s);
-    const uint32_t last = key_of(cut.z);               // (by keys: it may be a NaN)
+    const Row r{row_of<F32>(a, t), a.V, 0.f, 0, 0.f, 0.};
+    const uint64_t none[kHeld] = {}, last = last_of<F32>(none, true, r, 0, (uint64_t)a.K, false, s);
     if (tid == 0) s.count = 0;
     __syncthreads();
-    for_row<F32>(r.p, r.V, [&](const float (&z)[VE], uint32_t at, int n_) {
+#pragma unroll 1
+    for (int64_t at = (int64_t)tid * kEach; at - (int64_t)tid * kEach < a.V; at += kTile) {
+      float z[kEach];
+      load_tile<F32>(z, r.p, a.V, at);
 #pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const uint32_t k = key_of(z[i]);
-        if (i < n_ && k > kKeyMinusInf && (k > last || (k == last && at + i <= cut.last))) s.list[atomicAdd(&s.count, 1u)] = (uint64_t)k << 32 | (uint32_t)~(at + i);
+      for (int i = 0; i < kEach; ++i) {
+        const uint64_t e = entry_of(z[i], (uint32_t)(at + i));
+        if (at + i < a.V && e >= last && (uint32_t)(e >> 32) > kKeyMinusInf) s.list[atomicAdd(&s.count, 1u)] = e;
       }
-    });
+    }
     __syncthreads();
     found = s.count;
   }
@@ -884,16 +734,21 @@ __device__ __forceinline__ Row row_for(const void* row, int64_t V, float top, do
 }
 
 // The part of a row that a workgroup of the wide kernels has: tiles first .. last - 1.
-struct Part { int64_t t; int first, last; };
+struct Part { int64_t t; int first, last; };      // (t >= a.rows_end: none)
 __device__ __forceinline__ Part part_of(const RowsArgs& a) {
   const int64_t piece = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   const int tiles = (int)((a.V + kTile - 1) / kTile);
   Part p;
-  p.t = piece / a.wide_parts;
-  const int i = (int)(piece - p.t * a.wide_parts), per = (tiles + a.wide_parts - 1) / a.wide_parts;
+  p.t = a.row0 + piece / a.wide_parts;
+  const int i = (int)(piece % a.wide_parts), per = (tiles + a.wide_parts - 1) / a.wide_parts;
   p.first = i * per;
   p.last = min(tiles, p.first + per);
   return p;
+}
+
+__global__ __launch_bounds__(256) void wide_clear_kernel(const RowsArgs a) {
+  for (int i = threadIdx.x; i < kWideBins; i += 256) a.wide[blockIdx.x].bins[i] = 0;
+  if (threadIdx.x == 0) a.wide[blockIdx.x].count = 0;
 }
 
 // w by bins, added to the row's (which the first kernel has cleared): whole numbers, so in any order.
@@ -901,7 +756,7 @@ template <bool F32>
 __global__ __launch_bounds__(kSelect) void sample_bins_kernel(const RowsArgs a) {
   __shared__ SelectLds s;
   const Part p = part_of(a);
-  if (p.t >= a.T || p.first >= p.last) return;
+  if (p.t >= a.rows_end || p.first >= p.last) return;
   const int tid = threadIdx.x;
   const uint32_t key = largest_key(a, p.t, s);
   const Draw d = draw_of(a, p.t, key);
@@ -921,7 +776,7 @@ __global__ __launch_bounds__(kSelect) void sample_bins_kernel(const RowsArgs a) 
   }
   __syncthreads();
   for (int i = tid; i < kFlat; i += kSelect)
-    if (s.flat[i]) atomicAdd((unsigned long long*)&a.wide[p.t].bins[i], (unsigned long long)s.flat[i]);
+    if (s.flat[i]) atomicAdd((unsigned long long*)&a.wide[p.t - a.row0].bins[i], (unsigned long long)s.flat[i]);
 }
 
 // The bin in which the sum over the bins passes `share` of the whole, the sum in front of it and what is left to reach in it.
@@ -953,13 +808,13 @@ template <bool F32>
 __global__ __launch_bounds__(kSelect) void sample_tiles_kernel(const RowsArgs a) {
   __shared__ SelectLds s;
   const Part p = part_of(a);
-  if (p.t >= a.T || p.first >= p.last) return;
+  if (p.t >= a.rows_end || p.first >= p.last) return;
   const int tid = threadIdx.x;
   const uint32_t key = largest_key(a, p.t, s);
   const Draw d = draw_of(a, p.t, key);
   if (!d.wide()) return;
   const Row r = row_for(row_of<F32>(a, p.t), a.V, value_of(key), kLog2e / (double)d.tau);
-  const uint32_t bin = d.top_p < 1.f ? border_of(a.wide[p.t].bins, (double)d.top_p, s).bin : ~0u;
+  const uint32_t bin = d.top_p < 1.f ? border_of(a.wide[p.t - a.row0].bins, (double)d.top_p, s).bin : ~0u;
   const uint64_t least = (uint64_t)ceil((double)d.min_p * r.one);
   for (int b = p.first; b < p.last; ++b) {
     const int64_t at = (int64_t)b * kTile + tid * kEach;
@@ -976,17 +831,17 @@ __global__ __launch_bounds__(kSelect) void sample_tiles_kernel(const RowsArgs a)
 #pragma unroll
       for (int i = 0; i < kEach; ++i) hits |= (uint32_t)(flat_bin(r, z[i]) == bin && at + i < a.V) << i;
       if (hits) {
-        uint32_t to = atomicAdd(&a.wide[p.t].count, (uint32_t)__popc(hits));
+        uint32_t to = atomicAdd(&a.wide[p.t - a.row0].count, (uint32_t)__popc(hits));
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
           if (hits >> i & 1) {
-            if (to < (uint32_t)kWideList) a.wide[p.t].list[to] = (uint64_t)key_of(z[i]) << 32 | (uint32_t)~(uint32_t)(at + i);
+            if (to < (uint32_t)kWideList) a.wide[p.t - a.row0].list[to] = (uint64_t)key_of(z[i]) << 32 | (uint32_t)~(uint32_t)(at + i);
             ++to;
           }
       }
     }
     prefix(sum, all, s);
-    if (tid == 0) a.wide_mass[p.t * ((a.V + kTile - 1) / kTile) + b] = all;
+    if (tid == 0) a.wide_mass[(p.t - a.row0) * ((a.V + kTile - 1) / kTile) + b] = all;
   }
 }
 
@@ -999,13 +854,10 @@ __device__ __forceinline__ uint64_t target_of(float u, uint64_t total) {
 template <bool F32>
 __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArgs a) {
   __shared__ SelectLds s;
-  const int64_t t = blockIdx.x, n = (int64_t)a.chunks * kRowThreads, V = a.V;
+  const int64_t t = a.row0 + blockIdx.x, n = (int64_t)a.chunks * kRowThreads, V = a.V;
   const int tid = threadIdx.x;
-  const void* const row = row_of<F32>(a, t);
   const uint32_t key = largest_key(a, t, s);
   const Draw d = draw_of(a, t, key);
-  const float u = d.u, tau = d.tau, top_p = d.top_p, min_p = d.min_p;
-  const bool greedy = d.greedy, all_k = d.all_k;
   auto answer = [&](int64_t token, float logp) {
     if (a.index64) ((int64_t*)a.token)[t] = token;
     else ((int32_t*)a.token)[t] = (int32_t)token;
@@ -1015,29 +867,32 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
     if (tid == 0) answer(-1, __builtin_nanf(""));
     return;
   }
-  const double top = value_of(key), scale = kLog2e / (greedy ? 1. : (double)tau);
-  const int row_bits = bits_of_row(V);
-  auto log_p = [&](float z, uint64_t total, int bits) {
-    return greedy ? 0.f : (float)(((double)z - top) / (double)tau - log(ldexp((double)total, -bits)));
+  const double top = value_of(key), scale = kLog2e / (d.greedy ? 1. : (double)d.tau);
+  const Row r = row_for(row_of<F32>(a, t), V, (float)top, scale);
+  const int row_bits = bits_of_row(V), tiles = (int)((V + kTile - 1) / kTile);
+  auto log_p = [&](float z, uint64_t total) {
+    return d.greedy ? 0.f : (float)(((double)z - top) / (double)d.tau - log(ldexp((double)total, -row_bits)));
   };
 
   uint64_t row_total = 0;
-  if (all_k) {
+  if (d.all_k) {
     // chunks' sums at the row's largest entry
     uint64_t part = 0;
     const int per = (a.chunks + kSelect - 1) / kSelect, c0 = tid * per;
     auto chunk_mass = [&](int c) {
-      const RowChunk& r = a.chunk[t * a.chunks + c];
-      if (r.key <= kKeyMinusInf) return (uint64_t)0;
-      const double z0 = value_of(r.key);
-      return whole((double)r.sum * exp2((z0 - top) * scale - chunk_offset(z0, scale)), row_bits - kChunkBits);
+      const RowChunk& q = a.chunk[t * a.chunks + c];
+      if (q.key <= kKeyMinusInf) return (uint64_t)0;
+      const double z0 = value_of(q.key);
+      return whole((double)q.sum * exp2((z0 - top) * scale - chunk_offset(z0, scale)), row_bits - kChunkBits);
     };
+#pragma unroll 1
     for (int c = c0; c < c0 + per && c < a.chunks; ++c) part += chunk_mass(c);
     const uint64_t before = prefix(part, row_total, s);
-    if (top_p == 1.f && min_p == 0.f) {
-      const uint64_t target = target_of(u, row_total);
+    if (d.top_p == 1.f && d.min_p == 0.f) {
+      const uint64_t target = target_of(d.u, row_total);
       if (before <= target && target < before + part) {
         uint64_t x = before;
+#pragma unroll 1
         for (int c = c0; c < c0 + per && c < a.chunks; ++c) {
           const uint64_t m = chunk_mass(c);
           if (target < x + m) {
@@ -1050,282 +905,237 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
       }
       __syncthreads();
       const int c = (int)s.value[0];
-      const RowChunk r = a.chunk[t * a.chunks + c];
-      // that chunk again, with its own sums
-      const double z0 = value_of(r.key), z0_scaled = z0 * scale;
+      const double z0 = value_of(a.chunk[t * a.chunks + c].key), z0_scaled = z0 * scale;
       const double inner = ldexp((double)s.value[1], kChunkBits - row_bits) * exp2((top - z0) * scale + chunk_offset(z0, scale));
-      // thread i has `each` entries from the i-th on
-      constexpr int VE = F32 ? 4 : 8, MOST = 32;
-      const int64_t begin = (int64_t)c * kRowThreads * a.per_thread;
+      // that chunk again, with its own sums; thread i has `each` entries from the i-th on, VE at a time
+      constexpr int VE = F32 ? 4 : 8, MOST = 32 / VE;
       const int each = max(VE, a.per_thread * kRowThreads / kSelect), entries = kRowThreads * a.per_thread;
-      const int64_t i0 = begin + (int64_t)tid * each;
-      float z[MOST];
+      const int64_t i0 = (int64_t)c * entries + (int64_t)tid * each;
+      const bool here = (tid + 1) * each <= entries;
+      auto load = [&](float (&z)[VE], int j) {
+        const int64_t at = i0 + j * VE;
+        const bool in = here && j * VE < each && at + VE <= V;
+        const u32x4_t v = V >= VE ? load16((const char*)r.p + (in ? at : 0) * (F32 ? 4 : 2)) : u32x4_t{0, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < MOST; j += VE) {
-        const bool here = j < each && (tid + 1) * each <= entries;
-        float e[VE];
-        if (here && i0 + j + VE <= V) {
-          const u32x4_t v = load16((const char*)row + (i0 + j) * (F32 ? 4 : 2));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (F32) e[i] = __uint_as_float(v[i]);
-            else {
-              e[(2 * i) % VE] = __uint_as_float(v[i] << 16);
-              e[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
-            }
+        for (int i = 0; i < 4; ++i) {
+          if (F32) z[i] = __uint_as_float(v[i]);
+          else {
+            z[(2 * i) % VE] = __uint_as_float(v[i] << 16);
+            z[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < VE; ++i) e[i] = here && i0 + j + i < V ? logit<F32>(row, i0 + j + i) : -__builtin_inff();
         }
+        if (!in)
 #pragma unroll
-        for (int i = 0; i < VE; ++i) z[j + i] = e[i];
-      }
+          for (int i = 0; i < VE; ++i) z[i] = here && j * VE < each && at + i < V ? logit<F32>(r.p, at + i) : -__builtin_inff();
+      };
       auto w_of = [&](float v) { return whole_one(weight(fma((double)v, scale, -z0_scaled)), 0x1p48); };
-      uint64_t mine = 0;
+      float z[MOST][VE];
+      uint64_t sums[MOST], mine = 0, all;
 #pragma unroll
-      for (int i = 0; i < MOST; ++i)
-        if (i < each) mine += w_of(z[i]);
-      uint64_t all;
-      const uint64_t ahead = prefix(mine, all, s);
+      for (int j = 0; j < MOST; ++j) load(z[j], j);
+#pragma unroll
+      for (int j = 0; j < MOST; ++j) {
+        sums[j] = 0;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) sums[j] += w_of(z[j][i]);
+        mine += sums[j];
+      }
+      uint64_t x = prefix(mine, all, s);
       const uint64_t want = inner < (double)all ? (uint64_t)inner : all - 1;
-      if (ahead <= want && want < ahead + mine) {
-        uint64_t x = ahead;
+      if (x <= want && want < x + mine) {
         int at = 0;
-        float found = 0.f;
-        bool done = false;
+        bool past = false;
 #pragma unroll
-        for (int i = 0; i < MOST; ++i) {
-          if (i < each && !done) {
-            x += w_of(z[i]);
-            if (x > want) {
-              at = i;
-              found = z[i];
-              done = true;
-            }
+        for (int j = 0; j < MOST; ++j) {
+          past |= want < x + sums[j];
+          if (!past) {
+            x += sums[j];
+            at = j + 1;
           }
         }
-        answer(i0 + at, log_p(found, row_total, row_bits));
+        float v[VE];
+        load(v, at);
+        past = false;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          x += w_of(v[i]);
+          if (x > want && !past) {
+            answer(i0 + at * VE + i, log_p(v[i], row_total));
+            past = true;
+          }
+        }
       }
       return;
     }
   }
 
-  const Row r = row_for(row, V, (float)top, scale);
-  const int tiles = (int)((V + kTile - 1) / kTile);
-  uint64_t least = (uint64_t)ceil((double)min_p * r.one);
-  Cut cut = cut_all();
-  // The tile in which the sum of the kept w passes the target, and the entry in the tile; s.mass holds the tiles' sums.
-  auto finish = [&]() {
-    const int per = (tiles + kSelect - 1) / kSelect, b0 = tid * per;
-    uint64_t part = 0, total;
-    for (int b = b0; b < b0 + per && b < tiles; ++b) part += s.mass[b];
-    uint64_t x = prefix(part, total, s);
-    const uint64_t target = target_of(u, total);
-    if (x <= target && target < x + part)
-      for (int b = b0; b < b0 + per && b < tiles; ++b) {
-        if (target < x + s.mass[b]) {
-          s.value[0] = b;
-          s.value[1] = target - x;
-          break;
-        }
-        x += s.mass[b];
-      }
-    __syncthreads();
-    const int64_t at = (int64_t)s.value[0] * kTile + tid * kEach;
-    const uint64_t want = s.value[1];
-    float z[kEach];
-    uint64_t w[kEach], mine = 0, all;
-    load_tile<F32>(z, row, V, at);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      w[i] = row_weight(r, z[i]);
-      w[i] = inside(cut, z[i], (uint32_t)(at + i)) & (w[i] >= least) ? w[i] : 0;
-      mine += w[i];
-    }
-    uint64_t y = prefix(mine, all, s);
-    if (y <= want && want < y + mine) {
-      bool done = false;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        y += w[i];
-        if (y > want && !done) {
-          answer(at + i, log_p(z[i], total, row_bits));
-          done = true;
-        }
-      }
-    }
-  };
-
+  const uint64_t least = (uint64_t)ceil((double)d.min_p * r.one);
+  const int64_t k = d.greedy ? 1 : d.all_k ? V : d.top_k;
+  uint64_t held[kHeld], limit = 1;      // entries; the last kept one
+  uint32_t found = 0;
+  enum { WIDE, LIST, ROW } from = ROW;  // where the kept entries are: above a bin and in its list; in a list of the largest; anywhere
   if (a.wide && d.wide()) {
-    const RowWide& wide = a.wide[t];
-    const uint64_t* const mass = a.wide_mass + t * tiles;
-    const uint32_t listed = top_p < 1.f ? wide.count : 0;
-    if (listed <= (uint32_t)kList) {
-      uint64_t held[kHeld];
-      auto weight_of = [&](uint64_t entry) { return entry_weight(r, entry); };
-      if (top_p < 1.f) {
-        const uint64_t left = border_of(wide.bins, (double)top_p, s).left;
-#pragma unroll
-        for (int h = 0; h < kHeld; ++h) {
-          const uint32_t i = tid + h * kSelect;
-          held[h] = i < listed ? wide.list[i] : 0;
-        }
-        const uint64_t e = last_of(held, 0, left, s, weight_of);
-        cut = Cut{value_of((uint32_t)(e >> 32)), ~(uint32_t)e};
-      }
-      for (int i = tid; i < tiles; i += kSelect) s.mass[i] = mass[i];
-      __syncthreads();
-      if (top_p < 1.f)
-#pragma unroll
-        for (int h = 0; h < kHeld; ++h) {
-          const uint32_t at = ~(uint32_t)held[h];
-          if (!held[h] || !inside(cut, value_of((uint32_t)(held[h] >> 32)), at)) continue;
-          const uint64_t w = weight_of(held[h]);
-          if (w >= least) atomicAdd((unsigned long long*)&s.mass[at / kTile], (unsigned long long)w);
-        }
-      __syncthreads();
-      finish();
-      return;
+    found = d.top_p < 1.f ? a.wide[t - a.row0].count : 0;
+    if (found <= (uint32_t)kList) {
+      from = WIDE;
+      hold(held, a.wide[t - a.row0].list, found);
     }
-  }
-
-  // a short list of the largest entries
-  const int64_t k = greedy ? 1 : all_k ? V : d.top_k;
-  const uint32_t reach = (uint32_t)(k <= kReach ? k : kReachAll);
-  uint32_t bound = kKeyMinusInf + 1;
-  if ((int64_t)reach < n) bound = max(bound, bound_of(a.group + t * n, n, reach, key, s));
-  const bool all_listed = bound == kKeyMinusInf + 1;
-  const uint32_t found = gather<F32>(a, t, bound, s);
-  if (found <= (uint32_t)kList) {
-    uint64_t held[kHeld];
-    hold(held, found, s);
-    auto weight_of = [&](uint64_t entry) { return whole_one(weight(((double)value_of((uint32_t)(entry >> 32)) - top) * scale), 0x1p48); };
-    if (greedy) {
-      uint64_t most = held[0];
+  } else {
+    const uint32_t reach = (uint32_t)(k <= kReach ? k : kReachAll);
+    uint32_t bound = kKeyMinusInf + 1;
+    if ((int64_t)reach < n) bound = max(bound, bound_of(a.group + t * n, n, reach, key, s));
+    found = gather<F32>(a, t, bound, s);
+    if (found <= (uint32_t)kList) {
+      const bool listed = bound == kKeyMinusInf + 1 || k <= (int64_t)found;      // the whole row, or the first top_k
+      hold(held, s.list, found);
+      if (d.greedy) {
+        uint64_t most = held[0];
 #pragma unroll
-      for (int h = 1; h < kHeld; ++h) most = max(most, held[h]);
+        for (int h = 1; h < kHeld; ++h) most = max(most, held[h]);
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) most = max(most, (uint64_t)__shfl_xor((unsigned long long)most, o, 64));
-      __syncthreads();
-      if ((tid & 63) == 0) s.scan[tid >> 6] = most;
-      __syncthreads();
-      if (tid == 0) {
-        for (int v = 1; v < kSelect / 64; ++v) most = max(most, s.scan[v]);
-        answer(~(uint32_t)most, 0.f);
-      }
-      return;
-    }
-    // The list says it all if it is the whole row, holds the first top_k, or holds an entry that is not kept.
-    const bool reaches_k = all_listed || k <= (int64_t)found;
-    const uint64_t floor_w = (uint64_t)ceil((double)min_p * 0x1p48);
-    if (found <= 128) {
-      // one entry a thread: what is in front of it in descending order, then what is kept in front of it in order of the index
-      uint64_t* const ws = s.list + 128;
-      const uint64_t mine = held[0], my_w = mine ? weight_of(mine) : 0;
-      __syncthreads();
-      if (tid < 128) ws[tid] = my_w;
-      __syncthreads();
-      uint32_t rank = 0;
-      uint64_t before = 0, listed;
-      if (tid < (int)found)
-#pragma unroll 8
-        for (uint32_t i = 0; i < found; ++i) {
-          const bool larger = s.list[i] > mine;
-          rank += larger;
-          before += larger ? ws[i] : 0;
-        }
-      prefix(mine && (int64_t)rank < k ? my_w : 0, listed, s);      // the sum over the first top_k
-      const double base = all_k ? ldexp((double)row_total, kChunkBits - row_bits) : (double)listed;
-      const bool keep = mine && (int64_t)rank < k && (top_p == 1.f || (double)before < (double)top_p * base) && my_w >= floor_w;
-      uint64_t total, n_kept;
-      prefix(keep ? my_w : 0, total, s);
-      prefix(keep, n_kept, s);
-      if ((top_p == 1.f || all_k || reaches_k) && (reaches_k || n_kept < found)) {
-        if (tid < 128) ws[tid] = keep ? my_w : 0;
+        for (int o = 1; o < 64; o <<= 1) most = max(most, (uint64_t)__shfl_xor((unsigned long long)most, o, 64));
         __syncthreads();
-        const uint64_t target = target_of(u, total);
+        if ((tid & 63) == 0) s.scan[tid >> 6] = most;
+        __syncthreads();
+        if (tid == 0) {
+          for (int v = 1; v < kSelect / 64; ++v) most = max(most, s.scan[v]);
+          answer(entry_index(most), 0.f);
+        }
+        return;
+      }
+      if (listed && found <= 128) {
+        // one entry a thread: what is in front of it in descending order, then what is kept in front of it in order of the index
+        uint64_t* const w = s.list + 128;
+        const uint64_t mine = held[0], my_w = mine ? row_weight(r, entry_value(mine)) : 0;
+        __syncthreads();
+        if (tid < 128) w[tid] = my_w;
+        __syncthreads();
+        uint32_t rank = 0;
+        uint64_t before = 0, sum, total;
+        if (tid < (int)found)
+#pragma unroll 8
+          for (uint32_t i = 0; i < found; ++i) {
+            const bool larger = s.list[i] > mine;
+            rank += larger;
+            before += larger ? w[i] : 0;
+          }
+        prefix(mine && (int64_t)rank < k ? my_w : 0, sum, s);      // over the first top_k
+        const bool keep = mine && (int64_t)rank < k && (d.top_p == 1.f || (double)before < (double)d.top_p * (double)sum) && my_w >= least;
+        prefix(keep ? my_w : 0, total, s);
+        if (tid < 128) w[tid] = keep ? my_w : 0;
+        __syncthreads();
+        const uint64_t target = target_of(d.u, total);
         if (keep) {
           uint64_t y = 0;
 #pragma unroll 8
-          for (uint32_t i = 0; i < found; ++i) y += ~(uint32_t)s.list[i] < ~(uint32_t)mine ? ws[i] : 0;
-          if (y <= target && target < y + my_w) answer(~(uint32_t)mine, log_p(value_of((uint32_t)(mine >> 32)), total, kChunkBits));
+          for (uint32_t i = 0; i < found; ++i) y += entry_index(s.list[i]) < entry_index(mine) ? w[i] : 0;
+          if (y <= target && target < y + my_w) answer(entry_index(mine), log_p(entry_value(mine), total));
         }
         return;
       }
-    } else {
-      // the last of the first top_k; of those, the last of the nucleus
-      uint64_t limit = 1;
-      if (k < (int64_t)found) limit = last_of(held, 0, (uint64_t)k, s, [](uint64_t) { return (uint64_t)1; });
-      bool settled = top_p == 1.f;
-      if (top_p < 1.f && (all_k || reaches_k)) {
-        uint64_t sum = 0, listed;
-#pragma unroll
-        for (int h = 0; h < kHeld; ++h) sum += held[h] >= limit ? weight_of(held[h]) : 0;
-        prefix(sum, listed, s);
-        const double base = all_k ? ldexp((double)row_total, kChunkBits - row_bits) : (double)listed;
-        const uint64_t want = max((uint64_t)1, (uint64_t)ceil((double)top_p * base));
-        if (want <= listed || reaches_k) {
-          limit = last_of(held, limit, min(want, listed), s, weight_of);
-          settled = true;
-        }
-      }
-      // (entries by whose own w they are not kept are taken out)
-      uint64_t kept = 0, n_kept, least_kept = ~0ull;
-#pragma unroll
-      for (int h = 0; h < kHeld; ++h) {
-        const bool keep = held[h] >= limit && weight_of(held[h]) >= max(floor_w, (uint64_t)1);
-        held[h] = keep ? held[h] : 0;
-        kept += keep;
-        least_kept = keep ? min(least_kept, held[h]) : least_kept;
-      }
-      prefix(kept, n_kept, s);
-      if (settled && (reaches_k || n_kept < found)) {
-        // by tiles of the row, with a row's weights
-        for (int i = tid; i < tiles; i += kSelect) s.mass[i] = 0;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) least_kept = min(least_kept, (uint64_t)__shfl_xor((unsigned long long)least_kept, o, 64));
-        __syncthreads();
-        if ((tid & 63) == 0) s.scan[tid >> 6] = least_kept;
-#pragma unroll
-        for (int h = 0; h < kHeld; ++h)
-          if (held[h]) atomicAdd((unsigned long long*)&s.mass[~(uint32_t)held[h] / kTile], (unsigned long long)entry_weight(r, held[h]));
-        __syncthreads();
-        for (int v = 0; v < kSelect / 64; ++v) least_kept = min(least_kept, s.scan[v]);
-        cut = Cut{value_of((uint32_t)(least_kept >> 32)), ~(uint32_t)least_kept};
-        least = 0;                                     // (the cut has it in it)
-        finish();
-        return;
-      }
+      if (listed) from = LIST;
     }
   }
 
-  // the slow way
-  __syncthreads();
-  if (k < V) cut = cut_of<F32, false>(r, cut, (uint64_t)k, 1., s);
-  if (top_p < 1.f) cut = cut_of<F32, true>(r, cut, 0, (double)top_p, s);
-  for (int i = tid; i < tiles; i += kSelect) s.mass[i] = 0;
-  __syncthreads();
-  float ahead[kEach];
-  load_tile<F32>(ahead, row, V, tid * kEach);
-  for (int b = 0; b < tiles; ++b) {
-    const int64_t at = (int64_t)b * kTile + tid * kEach;
-    float z[kEach];
-    uint64_t sum = 0;
+  // the last of the first top_k, then of those the last of the nucleus
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    uint64_t want = (uint64_t)k;
+    if (pass == 0) {
+      if (from == WIDE || (from == LIST && k >= (int64_t)found) || k >= V) continue;
+    } else {
+      if (d.top_p == 1.f) continue;
+      if (from == WIDE) {
+        want = border_of(a.wide[t - a.row0].bins, (double)d.top_p, s).left;
+      } else {
+        uint64_t sum = 0, all;
+#pragma unroll 1
+        for (int64_t at = (int64_t)tid * kEach;; at += kTile) {
+          float z[kEach];
+          if (from == ROW) load_tile<F32>(z, r.p, V, at);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) z[i] = ahead[i];
-    load_tile<F32>(ahead, row, V, at + kTile);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint64_t w = row_weight(r, z[i]);
-      sum += inside(cut, z[i], (uint32_t)(at + i)) & (w >= least) ? w : 0;
+          for (int i = 0; i < kEach; ++i) {
+            const uint64_t e = from == ROW ? (at + i < V ? entry_of(z[i], (uint32_t)(at + i)) : 0) : held[i];
+            const uint64_t w = row_weight(r, entry_value(e));
+            sum += e && e >= limit ? w : 0;
+          }
+          if (from != ROW || at + kTile - (int64_t)tid * kEach >= V) break;
+        }
+        prefix(sum, all, s);
+        want = (uint64_t)ceil((double)d.top_p * (double)all);
+        want = want < 1 ? 1 : want < all ? want : all;
+      }
     }
+    limit = last_of<F32>(held, from == ROW, r, limit, want, pass == 1, s);
+  }
+
+  // each tile's sum of the kept w: of the entries, of what the wide kernel summed and the entries, or of the row
+  __syncthreads();
+  for (int i = tid; i < tiles; i += kSelect) s.mass[i] = from == WIDE ? a.wide_mass[(t - a.row0) * tiles + i] : 0;
+  __syncthreads();
+  if (from == ROW) {
+#pragma unroll 1
+    for (int b = 0; b < tiles; ++b) {
+      const int64_t at = (int64_t)b * kTile + tid * kEach;
+      float z[kEach];
+      uint64_t sum = 0;
+      load_tile<F32>(z, r.p, V, at);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor((unsigned long long)sum, o, 64);
-    if ((tid & 63) == 0 && sum) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)sum);
+      for (int i = 0; i < kEach; ++i) {
+        const uint64_t w = row_weight(r, z[i]);
+        sum += (entry_of(z[i], (uint32_t)(at + i)) >= limit) & (w >= least) ? w : 0;
+      }
+      sum = wave_prefix(sum);
+      if ((tid & 63) == 63 && sum) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)sum);
+    }
+  } else if (from == LIST || d.top_p < 1.f) {
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h) {
+      if (!held[h] || held[h] < limit) continue;
+      const uint64_t w = row_weight(r, entry_value(held[h]));
+      if (w >= least) atomicAdd((unsigned long long*)&s.mass[entry_index(held[h]) / kTile], (unsigned long long)w);
+    }
   }
   __syncthreads();
-  finish();
+  // the tile in which the sum passes the target, and the entry in the tile
+  const int per = (tiles + kSelect - 1) / kSelect, b0 = tid * per;
+  uint64_t part = 0, total;
+  for (int b = b0; b < b0 + per && b < tiles; ++b) part += s.mass[b];
+  uint64_t x = prefix(part, total, s);
+  const uint64_t target = target_of(d.u, total);
+  if (x <= target && target < x + part)
+    for (int b = b0; b < b0 + per && b < tiles; ++b) {
+      if (target < x + s.mass[b]) {
+        s.value[0] = b;
+        s.value[1] = target - x;
+        break;
+      }
+      x += s.mass[b];
+    }
+  __syncthreads();
+  const int64_t at = (int64_t)s.value[0] * kTile + tid * kEach;
+  const uint64_t want = s.value[1];
+  float z[kEach];
+  uint64_t w[kEach], mine = 0, all;
+  load_tile<F32>(z, r.p, V, at);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    w[i] = row_weight(r, z[i]);
+    w[i] = (entry_of(z[i], (uint32_t)(at + i)) >= limit) & (w[i] >= least) ? w[i] : 0;
+    mine += w[i];
+  }
+  uint64_t y = prefix(mine, all, s);
+  if (y <= want && want < y + mine) {
+    bool done = false;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      y += w[i];
+      if (y > want && !done) {
+        answer(at + i, log_p(z[i], total));
+        done = true;
+      }
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1352,21 +1162,32 @@ hipError_t launch_top_logits(const RowsArgs& r, hipStream_t st) {
   return hipGetLastError();
 }
 
+// With wide kernels kWideRows rows at a time, which share what those leave.
 template <bool F32>
-static hipError_t sample(const RowsArgs& r, hipStream_t st) {
+static hipError_t sample(RowsArgs r, hipStream_t st) {
   hipError_t e = scan<F32, true>(r, st);
   if (e != hipSuccess) return e;
-  if (r.wide) {
-    const FlatGrid g = flat_grid(r.T * r.wide_parts);
-    if (r.top_p_rows || r.top_p < 1.f) {
-      hipLaunchKernelGGL(sample_bins_kernel<F32>, dim3(g.x, g.y), dim3(kSelect), 0, st, r);
+  const int64_t rows = r.wide ? kWideRows : r.T;
+  for (r.row0 = 0; r.row0 < r.T; r.row0 += rows) {
+    r.rows_end = r.row0 + rows < r.T ? r.row0 + rows : r.T;
+    const int64_t n = r.rows_end - r.row0;
+    if (r.wide) {
+      const FlatGrid g = flat_grid(n * r.wide_parts);
+      if (r.row0) {
+        hipLaunchKernelGGL(wide_clear_kernel, dim3((uint32_t)n), dim3(256), 0, st, r);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+      if (r.top_p_rows || r.top_p < 1.f) {
+        hipLaunchKernelGGL(sample_bins_kernel<F32>, dim3(g.x, g.y), dim3(kSelect), 0, st, r);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+      hipLaunchKernelGGL(sample_tiles_kernel<F32>, dim3(g.x, g.y), dim3(kSelect), 0, st, r);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(sample_tiles_kernel<F32>, dim3(g.x, g.y), dim3(kSelect), 0, st, r);
+    hipLaunchKernelGGL(sample_select_kernel<F32>, dim3((uint32_t)n), dim3(kSelect), 0, st, r);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(sample_select_kernel<F32>, dim3((uint32_t)r.T), dim3(kSelect), 0, st, r);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 hipError_t launch_sample(const RowsArgs& r, hipStream_t st) { return r.f32 ? sample<true>(r, st) : sample<false>(r, st); }

@@ -175,6 +175,15 @@ def test_tokens_with_settings_of_each_row(dtype, T, V):
     check_tokens(z, u, s, K.kd_sample(z.cuda(), u.cuda(), **{k: v.cuda() for k, v in s.items()}), T // 2)
 
 
+@pytest.mark.parametrize("settings", [dict(top_p=0.9), dict(min_p=0.01), dict(top_p=0.7, min_p=0.002)])
+def test_tokens_of_more_rows_than_share_their_sums(settings):
+    T, V = 2100, 4500
+    z = rows(5, T, V, "normal", "bf16")
+    z[::7] = rows(6, 1, V, "equal", "bf16")
+    u = torch.from_numpy(np.random.default_rng(1).random(T).astype(np.float32))
+    check_tokens(z, u, settings, K.kd_sample(z.cuda(), u.cuda(), **settings), T - 400)
+
+
 def test_every_token_of_a_row_is_drawn_where_the_uniform_numbers_say():
     """A sweep of u over one row: the borders lie where the reference has them."""
     V, T = 700, 4000
