@@ -15,7 +15,7 @@ namespace kd {
 // ------------------------------------------------------------------------------------------------
 template <bool F32, bool TILE>
 __global__ __launch_bounds__(256) void quantize_blocks_kernel(const BlocksArgs a) {
-  __shared__ float lds[4][128];
+  __shared__ uint32_t lds[4][128];
   const int tid = threadIdx.x, tc = tid & 15, tr = tid >> 4, wave = tid >> 6;
   const int64_t n_cb = (a.cols + 127) / 128, n_rb = (a.rows + 127) / 128;
   const int64_t rb = blockIdx.x, cb = blockIdx.y;
@@ -29,57 +29,56 @@ __global__ __launch_bounds__(256) void quantize_blocks_kernel(const BlocksArgs a
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
   }
-  float rm[8], cm[8];               // largest magnitude of the thread's rows' and columns' blocks
+  uint32_t rm[8], cm[8];            // largest magnitude of the thread's rows' and columns' blocks
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    rm[i] = kLeastBlock;
+  for (int i = 0; i < 8; ++i) rm[i] = cm[i] = kLeastBlock;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) rm[i] = block_max(rm[i], fabsf(x[i][j]));
-  }
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t u = magnitude(x[i][j]);
+      rm[i] = max(rm[i], u);
+      if (!TILE) cm[j] = max(cm[j], u);
+    }
+  Divisor one;
   if (TILE) {
-    float m = rm[0];
+    uint32_t m = rm[0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) m = block_max(m, rm[i]);
+    for (int i = 1; i < 8; ++i) m = max(m, rm[i]);
+    m = row_max(m);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) m = block_max(m, __shfl_xor(m, o, 64));
+    for (int o = 16; o < 64; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
     lds[wave][0] = m;
     __syncthreads();
-    m = block_max(block_max(lds[0][0], lds[1][0]), block_max(lds[2][0], lds[3][0]));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) rm[i] = cm[i] = m;
+    m = max(max(lds[0][0], lds[1][0]), max(lds[2][0], lds[3][0]));
+    one = divisor_of(m);
     if (tid == 0) {
       if (a.scales) a.scales[rb * n_cb + cb] = scale_of(m);
       if (a.scales_t) a.scales_t[cb * n_rb + rb] = scale_of(m);
     }
   } else {
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) rm[i] = block_max(rm[i], __shfl_xor(rm[i], o, 64));
+    for (int i = 0; i < 8; ++i) rm[i] = row_max(rm[i]);
     if (a.scales && tc < 8 && r0 + tc < a.rows) {
-      float m = rm[0];
+      uint32_t m = rm[0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) m = tc == i ? rm[i] : m;
       a.scales[(r0 + tc) * n_cb + cb] = scale_of(m);
     }
     if (a.codes_t) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        cm[j] = kLeastBlock;
+      for (int o = 16; o < 64; o <<= 1)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) cm[j] = block_max(cm[j], fabsf(x[i][j]));
-#pragma unroll
-        for (int o = 16; o < 64; o <<= 1) cm[j] = block_max(cm[j], __shfl_xor(cm[j], o, 64));
-      }
+        for (int j = 0; j < 8; ++j) cm[j] = max(cm[j], (uint32_t)__shfl_xor((int)cm[j], o, 64));
       if ((tid & 63) < 16)
 #pragma unroll
         for (int j = 0; j < 8; ++j) lds[wave][tc * 8 + j] = cm[j];
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        cm[j] = block_max(block_max(lds[0][tc * 8 + j], lds[1][tc * 8 + j]), block_max(lds[2][tc * 8 + j], lds[3][tc * 8 + j]));
+        cm[j] = max(max(lds[0][tc * 8 + j], lds[1][tc * 8 + j]), max(lds[2][tc * 8 + j], lds[3][tc * 8 + j]));
       if (tr < 8 && c0 + tr < a.cols) {
-        float m = cm[0];
+        uint32_t m = cm[0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) m = tr == j ? cm[j] : m;
         a.scales_t[(c0 + tr) * n_rb + rb] = scale_of(m);
@@ -88,22 +87,22 @@ __global__ __launch_bounds__(256) void quantize_blocks_kernel(const BlocksArgs a
   }
   if (a.codes && c0 < ldc)
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (r0 + i < a.rows) {
-        float m[8];
+    for (int i = 0; i < 8; ++i) {
+      const Divisor d = TILE ? one : divisor_of(rm[i]);
+      float q[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m[j] = rm[i];
-        *(uint2*)(a.codes + (r0 + i) * ldc + c0) = codes_of(x[i], m);
-      }
+      for (int j = 0; j < 8; ++j) q[j] = quotient(x[i][j], d);
+      if (r0 + i < a.rows) *(uint2*)(a.codes + (r0 + i) * ldc + c0) = codes_of(q);
+    }
   if (a.codes_t && r0 < ldt)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c0 + j < a.cols) {
-        float v[8], m[8];
+    for (int j = 0; j < 8; ++j) {
+      const Divisor d = TILE ? one : divisor_of(cm[j]);
+      float q[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { v[i] = x[i][j]; m[i] = cm[j]; }
-        *(uint2*)(a.codes_t + (c0 + j) * ldt + r0) = codes_of(v, m);
-      }
+      for (int i = 0; i < 8; ++i) q[i] = quotient(x[i][j], d);
+      if (c0 + j < a.cols) *(uint2*)(a.codes_t + (c0 + j) * ldt + r0) = codes_of(q);
+    }
 }
 
 hipError_t launch_quantize_blocks(const BlocksArgs& a, hipStream_t st) {

@@ -4,19 +4,28 @@
 
 namespace kd {
 
-constexpr float kLeastBlock = 448.f * 0x1p-126f;
+// Largest magnitude of a block, as bits: an infinity or a NaN is larger than every number.
+constexpr uint32_t kLeastBlock = 0x04e00000u;        // 448 2^-126
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ float scale_of(uint32_t m) { return m < 0x7f800000u ? __uint_as_float(m) / 448.f : __builtin_nanf(""); }
 
-__device__ __forceinline__ float block_max(float a, float b) { return a != a || b != b ? __builtin_nanf("") : fmaxf(a, b); }
-__device__ __forceinline__ float scale_of(float m) { return m < __builtin_inff() ? m / 448.f : __builtin_nanf(""); }
-
-// codes of 8 values of blocks whose largest magnitudes are m[i] (a block with an infinity or a NaN: anything, its scale is NaN; 7 m / 16 is
-// rounded for fp32, so that 448 may come out one step larger)
-__device__ __forceinline__ uint2 codes_of(const float (&x)[8], const float (&m)[8]) {
-  float q[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    q[i] = fminf(fmaxf(x[i] * 0.4375f / m[i] * 1024.f, -448.f), 448.f);
-  }
+// 448 x / m, rounded as 448 x and its quotient by m are:  m = 2^e f with 1 <= f < 2, a = (448 2^-e) x, q = a (1 / f), and then the remainder's share,
+// (a - q f) (1 / f), added in one rounding, which gives the quotient that a division gives (448 x is exact for bf16).  A division for every element took
+// three times as many instructions.
+struct Divisor { float c, f, inv; };
+__device__ __forceinline__ Divisor divisor_of(uint32_t m) {
+  Divisor d;
+  d.c = __uint_as_float(0x83600000u - (m & 0x7f800000u));      // 448 2^-e: normal, as e is -118 to 127
+  d.f = __uint_as_float((m & 0x007fffffu) | 0x3f800000u);
+  d.inv = 1.f / d.f;
+  return d;
+}
+__device__ __forceinline__ float quotient(float x, const Divisor& d) {
+  const float a = x * d.c, q = a * d.inv;
+  return __builtin_amdgcn_fmed3f(fmaf(fmaf(-q, d.f, a), d.inv, q), -448.f, 448.f);      // (448 may come out one step larger)
+}
+// codes of 8 values of blocks with these divisors (a block with an infinity or a NaN: anything, its scale is NaN)
+__device__ __forceinline__ uint2 codes_of(const float (&q)[8]) {
   uint2 w;
   int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
   lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
@@ -25,6 +34,13 @@ __device__ __forceinline__ uint2 codes_of(const float (&x)[8], const float (&m)[
   w.x = (uint32_t)lo;
   w.y = (uint32_t)hi;
   return w;
+}
+// The largest of 16 lanes (a row), in all of them.
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, true));      // row_ror 1, 2, 4, 8
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, true));
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true));
 }
 
 template <bool F32>

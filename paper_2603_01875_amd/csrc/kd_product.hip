@@ -379,15 +379,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(const FewAr
       float x[8];
       if (f.x_f32) load_row8<true>(x, (const float*)f.x + (int64_t)m * p.K, c, p.K);
       else load_row8<false>(x, (const uint16_t*)f.x + (int64_t)m * p.K, c, p.K);
-      float top = kLeastBlock;
+      uint32_t top = kLeastBlock;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = block_max(top, fabsf(x[e]));
+      for (int e = 0; e < 8; ++e) top = max(top, magnitude(x[e]));
+      top = row_max(top);
+      const Divisor d = divisor_of(top);
 #pragma unroll
-      for (int o = 1; o < 16; o <<= 1) top = block_max(top, __shfl_xor(top, o, 64));
-      float tops[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) tops[e] = top;
-      *(uint2*)(codes + m * row + c) = codes_of(x, tops);
+      for (int e = 0; e < 8; ++e) x[e] = quotient(x[e], d);
+      *(uint2*)(codes + m * row + c) = codes_of(x);
       if ((tid & 15) == 0) scales[i] = scale_of(top);
     }
   } else {
