@@ -23,7 +23,10 @@ struct ProductArgs {
   void* out;
   int64_t M, N, K;
   int out_f32, b_tile, accumulate;
+  float* sums;                  // [product_parts][M][N], if that is more than one
+  int parts;                    // (launch_product's own)
 };
+int product_parts(int64_t M, int64_t N, int64_t K, int out_f32);
 hipError_t launch_product(const ProductArgs& p, hipStream_t st);
 // whether a is so small that the product's workgroups quantise it themselves; p.a and p.a_scales are then not read
 bool product_quantises(int64_t M, int64_t K);

@@ -43,20 +43,23 @@ kd_status check(const kd_linear_params* p) {
   return p->reserved[0] == 0 && p->reserved[1] == 0 ? KD_OK : KD_ERR_PARAM;
 }
 
-struct LinearLayout { size_t codes, scales, total; };
+struct LinearLayout { size_t codes, scales, sums, total; };
 LinearLayout linear_layout(const kd_linear_params& p) {
   LinearLayout L{};
   size_t off = 0;
   auto take = [&](int64_t bytes) { size_t o = off; off = (size_t)round_up((int64_t)off + bytes, 256); return o; };
   L.codes = take(p.M * round_up(p.K, 16));
   L.scales = take(p.M * ((p.K + 127) / 128) * 4);
+  const int parts = kd::product_parts(p.M, p.N, p.K, p.out_dtype == KD_F32);
+  L.sums = take(parts > 1 ? parts * p.M * p.N * 4 : 0);
   L.total = off;
   return L;
 }
 
 kd::ProductArgs product_args(const kd_linear_params& p, const uint8_t* a, const float* a_scales, const uint8_t* b, const float* b_scales,
-                             void* out) {
-  return kd::ProductArgs{a, b, a_scales, b_scales, out, p.M, p.N, p.K, p.out_dtype == KD_F32, p.b_block == KD_BLOCK_TILE, p.accumulate};
+                             void* out, void* workspace) {
+  float* const sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + linear_layout(p).sums);
+  return kd::ProductArgs{a, b, a_scales, b_scales, out, p.M, p.N, p.K, p.out_dtype == KD_F32, p.b_block == KD_BLOCK_TILE, p.accumulate, sums, 1};
 }
 
 // ---- rows of logits ----
@@ -223,7 +226,7 @@ kd_status kd_matmul_e4m3(const kd_linear_params* params, const uint8_t* a, const
       !aligned(workspace, 256))
     return KD_ERR_ALIGN;
   if (workspace_bytes < linear_layout(*params).total) return KD_ERR_WORKSPACE;
-  KD_TRY(kd::launch_product(product_args(*params, a, a_scales, b, b_scales, out), static_cast<hipStream_t>(hip_stream)));
+  KD_TRY(kd::launch_product(product_args(*params, a, a_scales, b, b_scales, out, workspace), static_cast<hipStream_t>(hip_stream)));
   return KD_OK;
 }
 
@@ -242,12 +245,12 @@ kd_status kd_linear_e4m3(const kd_linear_params* params, const void* x, const ui
   uint8_t* const codes = static_cast<uint8_t*>(workspace) + L.codes;
   float* const scales = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.scales);
   if (kd::product_quantises(params->M, params->K)) {
-    KD_TRY(kd::launch_linear_few(product_args(*params, nullptr, nullptr, w, w_scales, out), x, params->in_dtype == KD_F32, st));
+    KD_TRY(kd::launch_linear_few(product_args(*params, nullptr, nullptr, w, w_scales, out, workspace), x, params->in_dtype == KD_F32, st));
     return KD_OK;
   }
   const kd::BlocksArgs q{x, params->M, params->K, params->K, params->in_dtype == KD_F32, 0, codes, nullptr, scales, nullptr};
   KD_TRY(kd::launch_quantize_blocks(q, st));
-  KD_TRY(kd::launch_product(product_args(*params, codes, scales, w, w_scales, out), st));
+  KD_TRY(kd::launch_product(product_args(*params, codes, scales, w, w_scales, out, workspace), st));
   return KD_OK;
 }
 

@@ -109,6 +109,7 @@ __device__ __forceinline__ void store_row(const ProductArgs& p, int64_t m, int64
 // ------------------------------------------------------------------------------------------------
 // tiles
 //
+// (K in parts: a workgroup does its part of one tile and leaves fp32 sums, which product_join_kernel adds in the parts' order.)
 // WN x WM waves, each with NB x MB blocks of 16 x 16 results.  A k-step is one block of 128: the tile's rows of b and a, 128 bytes each, and
 // their scales, loaded straight into LDS while the step before is multiplied (two stages).  16-byte chunks of a row are permuted by
 // XOR with bits of its number, and a lane takes chunks g and g + 4 (which of a block's codes an instruction contracts together does not
@@ -152,15 +153,17 @@ __device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wn = wave % Tile::WN, wm = wave / Tile::WN;
   const int l = lane & 15, g = lane >> 4;
   const int n_mt = (int)((p.M + BM - 1) / BM), n_nt = (int)((p.N + BN - 1) / BN), tiles = n_mt * n_nt;
-  const int ld = (int)((p.K + 15) / 16 * 16), nk = (int)((p.K + 127) / 128), steps = nk < 2 ? 2 : nk;
-  const int my = xcd_logical_id(blockIdx.x, gridDim.x), mine = (tiles - my + (int)gridDim.x - 1) / (int)gridDim.x;      // (the grid is not larger)
+  const int ld = (int)((p.K + 15) / 16 * 16), nk = (int)((p.K + 127) / 128);
+  const int part = blockIdx.x % p.parts, grid = gridDim.x / p.parts, part_steps = (nk + p.parts - 1) / p.parts, k0 = part * part_steps;
+  const int last = nk - k0 < part_steps ? nk - k0 : part_steps, steps = last < 2 ? 2 : last;      // (behind nk: 0; a part that is not the last has two)
+  const int my = xcd_logical_id(blockIdx.x / p.parts, grid), mine = (tiles - my + grid - 1) / grid;      // (the grid is not larger)
   const bool b_scales = wave * 64 < BN;
   static_assert(BN % 64 == 0 && Tile::SCALE_LOADS == 1, "a wave loads scales of one matrix");
 
   auto rows_of = [&](int round) {
     TileRows<Tile> r;
     int tm, tn;
-    tile_of(my + round * (int)gridDim.x, n_mt, n_nt, tm, tn);
+    tile_of(my + round * grid, n_mt, n_nt, tm, tn);
     r.n0 = (int64_t)tn * BN;
     r.m0 = (int64_t)tm * BM;
     const int64_t n = p.N - r.n0 < BN ? p.N - r.n0 : BN, m = p.M - r.m0 < BM ? p.M - r.m0 : BM;
@@ -178,7 +181,8 @@ __device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) 
   const uint32_t at = (uint32_t)row * ld + chunk * 16, step = (uint32_t)Tile::LOAD_ROWS * ld;
   const int scale_row = b_scales ? (B_TILE ? tid / 128 : tid) : tid - BN;
   const uint32_t scale_at = scale_row < (b_scales ? BN : BM) ? (uint32_t)scale_row * (nk * 4) : BEHIND;
-  auto load = [&](int stage, const TileRows<Tile>& r, int k) {
+  auto load = [&](int stage, const TileRows<Tile>& r, int step_k) {
+    const int k = k0 + step_k;
     char* const to = smem + stage * Tile::STAGE + wave * 1024;
     const uint32_t from = at | (k * 128 + chunk * 16 < ld ? 0u : BEHIND);
 #pragma unroll
@@ -205,7 +209,9 @@ __device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) 
   // What a step multiplies by: codes and scales of the wave's rows of a, and 16 rows of b after the other.
   Codes<CUT> y[MB], x[2];
   float s[MB], s_next[MB];
-  f32x4 t[2];
+  constexpr int PRODUCTS = NB * MB, LATE = 3, TS = MB - 1 + LATE < 2 * MB ? 2 : 4;      // TS: a block's scales stay until its last result is added
+  static_assert(NB % TS == 0 && MB - 1 + LATE < TS * MB, "places of t");
+  f32x4 t[TS];
   auto read_a = [&](const char* base, int j) {
     const float* const scales = (const float*)(base + (BN + BM) * 128);
     y[j] = read(base + BN * 128 + wm * (MB * 16 * 128), j);
@@ -214,19 +220,19 @@ __device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) 
   };
   auto read_b = [&](const char* base, int i) { x[i & 1] = read(base + wn * (NB * 16 * 128), i); };
   auto read_t = [&](const char* base, int i) {
-    if (!B_TILE) t[i & 1] = *(const f32x4*)((const float*)(base + (BN + BM) * 128) + wn * (NB * 16) + i * 16 + 4 * g);
+    if (!B_TILE) t[i % TS] = *(const f32x4*)((const float*)(base + (BN + BM) * 128) + wn * (NB * 16) + i * 16 + 4 * g);
   };
   // A product's result is scaled and added three products later, so that nothing waits for the matrix pipe.
-  constexpr int PRODUCTS = NB * MB, LATE = 3;
-  static_assert(NB % 4 == 0 && PRODUCTS % 4 == 0 && PRODUCTS > 4, "places of x, t and c");
+  static_assert(NB % 2 == 0 && PRODUCTS % 4 == 0 && PRODUCTS > 4, "places of x and c");
   f32x4 c[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) c[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  t[0] = t[1] = c[0];
+#pragma unroll
+  for (int i = 0; i < TS; ++i) t[i] = c[0];
   auto add = [&](int q) {
     const int i = q / MB, j = q % MB;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(c[q & 3][r], B_TILE ? s[j] : s[j] * t[i & 1][r], acc[i][j][r]);
+    for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(c[q & 3][r], B_TILE ? s[j] : s[j] * t[i % TS][r], acc[i][j][r]);
   };
 
   int stage = 0;
@@ -287,14 +293,21 @@ __device__ __forceinline__ void product_tiles(const ProductArgs& p, char* smem) 
     // (what the next tile's first sums add is 0 times these, which may be NaN)
 #pragma unroll
     for (int j = 0; j < MB; ++j) s[j] = 0.f;
-    t[1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (p.accumulate) {
+#pragma unroll
+    for (int i = 0; i < TS; ++i) t[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (p.accumulate || p.parts > 1) {
+      ProductArgs to = p;
+      if (p.parts > 1) {
+        to.out = p.sums + part * p.M * p.N;
+        to.out_f32 = 1;
+        to.accumulate = 0;
+      }
 #pragma unroll
       for (int j = 0; j < MB; ++j)
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           const int64_t m = m0 + wm * (MB * 16) + j * 16 + l, n = n0 + wn * (NB * 16) + i * 16 + 4 * g;
-          if (m < p.M && n < p.N) store4(p, m, n, acc[i][j]);
+          if (m < p.M && n < p.N) store4(to, m, n, acc[i][j]);
         }
     } else {
       // 16 rows at a time through LDS, so that 128 bytes of a row go out together (32 at a time, as a lane has them, cost 340 of 2520 us
@@ -331,15 +344,40 @@ __global__ __launch_bounds__(Tile::NT) void product_tile_kernel(const ProductArg
   product_tiles<Tile, CUT, B_TILE>(p, smem);
 }
 
+// out = the parts' sums one after the other, four columns a thread
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void product_join_kernel(const ProductArgs p) {
+  const int64_t quads = (p.N + 3) / 4, i = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x, m = i / quads, n = (i - m * quads) * 4;
+  if (m >= p.M) return;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int part = 0; part < p.parts; ++part) {
+    const float* const from = p.sums + (part * p.M + m) * p.N + n;
+    if (n + 4 <= p.N) {
+      const u32x4_t w = load16(from);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] += __uint_as_float(w[r]);
+    } else {
+      for (int r = 0; n + r < p.N; ++r) v[r] += from[r];
+    }
+  }
+  store4(p, m, n, v);
+}
+
+template <class Tile> static int64_t tiles_of(int64_t M, int64_t N) { return (M + Tile::BM - 1) / Tile::BM * ((N + Tile::BN - 1) / Tile::BN); }
+template <class Tile> constexpr int kResident = 160 * 1024 / Tile::SMEM * kNumCU;      // workgroups
+
 template <class Tile, bool CUT>
-static hipError_t launch_tiles(const ProductArgs& p, hipStream_t st) {
-  const int64_t tiles = (p.M + Tile::BM - 1) / Tile::BM * ((p.N + Tile::BN - 1) / Tile::BN);
+static hipError_t launch_tiles(ProductArgs p, hipStream_t st, int parts = 1) {
+  const int64_t tiles = tiles_of<Tile>(p.M, p.N);
   if (tiles > INT32_MAX / 2) return hipErrorInvalidValue;
-  constexpr int resident = 160 * 1024 / Tile::SMEM * kNumCU;
-  const int grid = tiles < resident ? (int)tiles : resident;
-  void* args = const_cast<ProductArgs*>(&p);
-  return p.b_tile ? launch_big<product_tile_kernel<Tile, CUT, true>>(grid, Tile::NT, Tile::SMEM, st, args)
-                  : launch_big<product_tile_kernel<Tile, CUT, false>>(grid, Tile::NT, Tile::SMEM, st, args);
+  p.parts = parts;
+  const int grid = parts * (tiles < kResident<Tile> ? (int)tiles : kResident<Tile>);
+  void* args = &p;
+  const hipError_t e = p.b_tile ? launch_big<product_tile_kernel<Tile, CUT, true>>(grid, Tile::NT, Tile::SMEM, st, args)
+                                : launch_big<product_tile_kernel<Tile, CUT, false>>(grid, Tile::NT, Tile::SMEM, st, args);
+  if (e != hipSuccess || parts == 1) return e;
+  product_join_kernel<<<dim3((unsigned)((p.M * ((p.N + 3) / 4) + kJoinThreads - 1) / kJoinThreads)), dim3(kJoinThreads), 0, st>>>(p);
+  return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -490,12 +528,36 @@ bool product_is_few(int64_t M, int64_t K) { return M <= 32 && few_smem(M, K, M <
 bool product_quantises(int64_t M, int64_t K) { return product_is_few(M, K) && M * K <= 8192; }
 hipError_t launch_linear_few(const ProductArgs& p, const void* x, int x_f32, hipStream_t st) { return launch_few(p, x, x_f32, st); }
 
+using TileBig = ProductTile<8, 4, 2, 4>;        // 256 x 256
+using TileMid = ProductTile<4, 4, 2, 2>;        // 128 x 128
+using TileSmall = ProductTile<4, 2, 2, 2>;      // 64 rows of a x 128 of b
+
+// At 4096 x 4096 x 4096 (bf16 results, us) 256 x 256 takes 65, 128 x 128 87 and 64 x 128 102; but a CU wants a tile: 2048 x 4096 x 4096
+// takes 64, 45 and 57.  128 x 128 pays with two tiles a CU, as many as fit, and where 64 x 128 would not save rows: two of those
+// take 1.25 times as long (fp32 results: 4096 x 4096 x 4096 135 and 168; 777 x 5003 x 1008 23.7 and 20.1; 300 x 1000 x 4096 41 and 27).
+static bool takes_big(int64_t M, int64_t N, int out_f32) { return !out_f32 && tiles_of<TileBig>(M, N) >= kNumCU; }
+static bool takes_mid(int64_t M, int64_t N) {
+  const int64_t mid = tiles_of<TileMid>(M, N);
+  return mid >= kResident<TileMid> && 8 * mid <= 5 * tiles_of<TileSmall>(M, N);
+}
+
+// Few tiles of many steps: K in parts, workgroups of their own, with eight steps or more each.  (us with one part, with this many and with parts of four steps:
+// 256 x 4096 x 16384 98, 51, 51 for fp32 and 67, 35, 35 for bf16 results; 48 x 4096 x 4096 27, 14, 15; 300 x 1000 x 4096 27, 16, 18;
+// 1024 x 1024 x 1024 12, 12, 15: the join is a launch.)
+int product_parts(int64_t M, int64_t N, int64_t K, int out_f32) {
+  if (product_is_few(M, K) || takes_big(M, N, out_f32) || takes_mid(M, N)) return 1;
+  const int64_t tiles = tiles_of<TileSmall>(M, N), nk = (K + 127) / 128;
+  int parts = 1;
+  while (parts < 16 && 2 * parts * tiles <= kResident<TileSmall> && nk >= 16 * parts) parts *= 2;
+  return parts;
+}
+
 hipError_t launch_product(const ProductArgs& p, hipStream_t st) {
   if (product_is_few(p.M, p.K)) return launch_few(p, nullptr, 0, st);
-  if (p.out_f32) return launch_tiles<ProductTile<4, 4, 2, 2>, false>(p, st);
-  const int64_t big = (p.M + 255) / 256 * ((p.N + 255) / 256);
-  if (big >= kNumCU) return launch_tiles<ProductTile<8, 4, 2, 4>, true>(p, st);
-  return launch_tiles<ProductTile<4, 4, 2, 2>, true>(p, st);
+  if (takes_big(p.M, p.N, p.out_f32)) return launch_tiles<TileBig, true>(p, st);
+  if (takes_mid(p.M, p.N)) return p.out_f32 ? launch_tiles<TileMid, false>(p, st) : launch_tiles<TileMid, true>(p, st);
+  const int parts = product_parts(p.M, p.N, p.K, p.out_f32);
+  return p.out_f32 ? launch_tiles<TileSmall, false>(p, st, parts) : launch_tiles<TileSmall, true>(p, st, parts);
 }
 
 }  // namespace kd

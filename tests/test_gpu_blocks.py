@@ -129,6 +129,15 @@ def test_product(M, N, K_, tile, out):
     check_product(into, ref, size, K_, out, before)
 
 
+@pytest.mark.parametrize("M,N,K_", [(40, 217, 2100), (33, 1, 2048), (64, 130, 4200), (70, 131, 16_400), (500, 1027, 2176), (130, 64, 40_000),
+                                    (3000, 3001, 200)])
+@pytest.mark.parametrize("tile", [True, False])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_product_of_a_long_axis_in_parts(M, N, K_, tile, out):
+    """Parts that are shorter than the others, or empty (16,400: 129 blocks are 15 parts of nine); the last size has none, in 128 x 128 tiles."""
+    test_product(M, N, K_, tile, out)
+
+
 @pytest.mark.parametrize("tile", [True, False])
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("M,N,K_", [(4096, 5000, 128), (4000, 4800, 100), (2300, 9000, 272), (20_000, 300, 130)])
