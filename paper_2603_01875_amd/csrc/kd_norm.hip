@@ -55,7 +55,7 @@ template <bool MAX>
 __device__ __forceinline__ void put(double& s, float x) {
   if (MAX) {
     const double a = fabs((double)x);
-    s = !(a <= s) ? a : s;              // (a NaN stays)
+    s = a > s || a != a ? a : s;        // (a NaN stays: nothing is larger)
   } else {
     s = fma((double)x, (double)x, s);
   }
@@ -90,7 +90,13 @@ __device__ __forceinline__ void add_piece(double& s, const Piece& p) {
 #pragma unroll
     for (int j = 0; j < kNormUnroll; ++j) add_vector<MAX, F32>(s, x[j]);
   }
-  for (; i < nv; i += kNormThreads) add_vector<MAX, F32>(s, v[i]);
+  if (i < nv) {                         // (the last ones too are on their way together)
+    u32x4_t x[kNormUnroll];
+#pragma unroll
+    for (int j = 0; j < kNormUnroll; ++j) x[j] = i + j * kNormThreads < nv ? v[i + j * kNormThreads] : u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < kNormUnroll; ++j) add_vector<MAX, F32>(s, x[j]);
+  }
   if (rest + (int)threadIdx.x < p.n) put<MAX>(s, element(p.in, F32, rest + threadIdx.x));
 }
 
@@ -127,6 +133,14 @@ __global__ __launch_bounds__(1024) void grad_total_kernel(const double* partials
   if (threadIdx.x == 0) *total = s;
 }
 
+// Results pass the caches by: no part of this call reads them again, and what is still to be read stays (16 bytes at a time, in and out: 100 million elements
+// of bf16 79 to 61 us, 3.2 million of fp32 8.7 to 7.6; no difference at 1.7 billion).
+template <class V>
+__device__ __forceinline__ void stream_out(global_t p, const V& v) {
+  typedef V Any __attribute__((aligned(2)));
+  __builtin_nontemporal_store(v, (KD_GLOBAL Any*)p);
+}
+
 template <bool IN32, bool OUT32>
 __device__ __forceinline__ void scale_piece(const Piece& p, global_t out, float f) {
   constexpr int VE = IN32 ? 4 : 8;
@@ -152,11 +166,11 @@ __device__ __forceinline__ void scale_piece(const Piece& p, global_t out, float 
     if (OUT32) {
 #pragma unroll
       for (int k = 0; k < VE; k += 4)
-        store16(o + ((int64_t)i * VE + k) * 4, u32x4_t{__float_as_uint(y[k]), __float_as_uint(y[k + 1]), __float_as_uint(y[k + 2]), __float_as_uint(y[k + 3])});
+        stream_out(o + ((int64_t)i * VE + k) * 4, u32x4_t{__float_as_uint(y[k]), __float_as_uint(y[k + 1]), __float_as_uint(y[k + 2]), __float_as_uint(y[k + 3])});
     } else if (VE == 8) {
-      store16(o + (int64_t)i * 16, u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4 % VE], y[5 % VE]), bf16_pair(y[6 % VE], y[7 % VE])});
+      stream_out(o + (int64_t)i * 16, u32x4_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4 % VE], y[5 % VE]), bf16_pair(y[6 % VE], y[7 % VE])});
     } else {
-      store8(o + (int64_t)i * 8, u32x2_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])});
+      stream_out(o + (int64_t)i * 8, u32x2_t{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])});
     }
   };
   int i = threadIdx.x;
@@ -167,7 +181,14 @@ __device__ __forceinline__ void scale_piece(const Piece& p, global_t out, float 
 #pragma unroll
     for (int j = 0; j < kNormUnroll; ++j) many(i + j * kNormThreads, x[j]);
   }
-  for (; i < nv; i += kNormThreads) many(i, v[i]);
+  if (i < nv) {
+    u32x4_t x[kNormUnroll];
+#pragma unroll
+    for (int j = 0; j < kNormUnroll; ++j) x[j] = i + j * kNormThreads < nv ? v[i + j * kNormThreads] : u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < kNormUnroll; ++j)
+      if (i + j * kNormThreads < nv) many(i + j * kNormThreads, x[j]);
+  }
   if (rest + (int)threadIdx.x < p.n) one(rest + threadIdx.x);
 }
 

@@ -79,6 +79,15 @@ def test_magnitudes_whose_squares_no_float_holds():
                 assert (np.abs(np64(o) - r) <= (HALF[o.dtype] + 3 * 2.0 ** -24) * np.abs(r)).all()
 
 
+@pytest.mark.parametrize("at", [0, 1, 1023, 2048, 20_000, 38_000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", [K.NORM_L2, K.NORM_MAX])
+def test_a_nan_in_front_of_numbers_is_not_forgotten(at, dtype, kind):
+    gs = tensors(2, [40_000], [dtype])
+    gs[0][at] = float("nan")
+    assert torch.isnan(K.kd_grad_norm(gs, kind))
+
+
 @pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
 @pytest.mark.parametrize("kind", [K.NORM_L2, K.NORM_MAX])
 def test_a_norm_that_is_not_finite_leaves_the_gradients(bad, kind):
