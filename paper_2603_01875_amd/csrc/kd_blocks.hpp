@@ -20,21 +20,16 @@ __device__ __forceinline__ Divisor divisor_of(uint32_t m) {
   d.inv = 1.f / d.f;
   return d;
 }
+template <bool F32>
 __device__ __forceinline__ float quotient(float x, const Divisor& d) {
-  const float a = x * d.c, q = a * d.inv;
-  return __builtin_amdgcn_fmed3f(fmaf(fmaf(-q, d.f, a), d.inv, q), -448.f, 448.f);      // (448 may come out one step larger)
+  const float a = x * d.c, q = a * d.inv, y = fmaf(fmaf(-q, d.f, a), d.inv, q);
+  return F32 ? __builtin_amdgcn_fmed3f(y, -448.f, 448.f) : y;      // (448 x rounded may be one step more than 448 m)
 }
-// codes of 8 values of blocks with these divisors (a block with an infinity or a NaN: anything, its scale is NaN)
-__device__ __forceinline__ uint2 codes_of(const float (&q)[8]) {
-  uint2 w;
-  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
-  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], 0, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], hi, true);
-  w.x = (uint32_t)lo;
-  w.y = (uint32_t)hi;
-  return w;
+// codes of quotients (of a block with an infinity or a NaN: anything, its scale is NaN)
+__device__ __forceinline__ uint32_t codes_of4(float a, float b, float c, float d) {
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
+__device__ __forceinline__ uint2 codes_of(const float (&q)[8]) { return make_uint2(codes_of4(q[0], q[1], q[2], q[3]), codes_of4(q[4], q[5], q[6], q[7])); }
 // The largest of 16 lanes (a row), in all of them.
 __device__ __forceinline__ uint32_t row_max(uint32_t v) {
   v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, true));      // row_ror 1, 2, 4, 8

@@ -423,7 +423,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few_kernel(const FewAr
       top = row_max(top);
       const Divisor d = divisor_of(top);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = quotient(x[e], d);
+      for (int e = 0; e < 8; ++e) x[e] = quotient<true>(x[e], d);
       *(uint2*)(codes + m * row + c) = codes_of(x);
       if ((tid & 15) == 0) scales[i] = scale_of(top);
     }
