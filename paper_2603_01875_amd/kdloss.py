@@ -765,7 +765,7 @@ def kd_topk_fwd(top_logits, top_index, h_s, W_s, lse=None, mask=None, tau=1.0, t
 # ------------------------------------------------------------------------------------------------
 # beside the losses: e4m3 in blocks of 128, top logits, sampling, the norm of the gradients
 # ------------------------------------------------------------------------------------------------
-def _call(name, dev, args, stream):
+def _call(name, dev, args, stream=None):
     """Makes a call on the device of its tensors, whatever the current one is, on `stream` or that device's current one (asked for by its
     handle alone: torch.cuda.current_stream() makes an object around it, 2.9 us, a quarter of what a small call takes the host)."""
     import torch
@@ -826,7 +826,7 @@ def make_blocks_params(rows, cols, ld=None, src_dtype=BF16, block=BLOCK_ROW):
     return KdBlocksParams(int(rows), int(cols), int(cols if ld is None else ld), int(src_dtype), int(block))
 
 
-def quantize_e4m3_blocks(x, block=BLOCK_ROW, transpose=False, both=False, stream=None):
+def quantize_e4m3_blocks(x, block=BLOCK_ROW, transpose=False, both=False):
     """E4m3Blocks of a bf16 or fp32 matrix with contiguous rows: a scale per row and 128 columns (BLOCK_ROW) or per 128 x 128
     (BLOCK_TILE).  transpose: of x's transpose instead; both: (x's, its transpose's) from one reading.  Other than quantize_e4m3, which
     multiplies by a reciprocal, it divides: code = e4m3(448 x / largest of the block), rounded once before."""
@@ -843,7 +843,7 @@ def quantize_e4m3_blocks(x, block=BLOCK_ROW, transpose=False, both=False, stream
     q = None if transpose and not both else made(rows, cols)
     qt = made(cols, rows) if transpose or both else None
     args = [_ptr(t) for y in (q, qt) for t in ((None, None) if y is None else (y.codes, y.scales))]
-    _call("kd_quantize_e4m3_blocks", x.device, [ctypes.byref(p), _ptr(x)] + args, stream)
+    _call("kd_quantize_e4m3_blocks", x.device, [ctypes.byref(p), _ptr(x)] + args)
     return (q, qt) if both else qt if transpose else q
 
 
@@ -1055,7 +1055,7 @@ def _grad_list(grads):
     return grads if isinstance(grads, GradList) else GradList(grads)
 
 
-def kd_grad_norm(grads, norm_kind=NORM_L2, workspace=None, stream=None):
+def kd_grad_norm(grads, norm_kind=NORM_L2, workspace=None):
     """The sum of all squares (NORM_L2) or the largest magnitude (NORM_MAX) over a GradList or a list of tensors, as one float64 on the
     device.  A program with gradients spread over ranks all-reduces it and goes on with kd_grad_clip."""
     import torch
@@ -1064,11 +1064,11 @@ def kd_grad_norm(grads, norm_kind=NORM_L2, workspace=None, stream=None):
     ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=g.device) if workspace is None else workspace
     _check_workspace(ws, g.device)
     _call("kd_grad_norm", g.device, [g.n, g._in[0], g.counts, g._in[1], int(norm_kind), _ptr(total), _ptr(ws),
-                                     ctypes.c_size_t(_nbytes(ws))], stream)
+                                     ctypes.c_size_t(_nbytes(ws))])
     return total
 
 
-def kd_grad_clip(grads, total, max_norm, norm_kind=NORM_L2, stream=None):
+def kd_grad_clip(grads, total, max_norm, norm_kind=NORM_L2):
     """Scales all gradients (into the list's out, or in place) by min(1, max_norm / norm), the norm being that of `total` (kd_grad_norm);
     where it is not finite they stay as they are.  Returns the norm, one float32 on the device."""
     import torch
@@ -1076,11 +1076,11 @@ def kd_grad_clip(grads, total, max_norm, norm_kind=NORM_L2, stream=None):
     _check_tensors([("total", total, (torch.float64,), 1, False)], g.device)
     norm = torch.empty((), dtype=torch.float32, device=g.device)
     _call("kd_grad_clip", g.device, [g.n, g._in[0], g.counts, g._in[1], int(norm_kind), _ptr(total), float(max_norm), g._out[0],
-                                     g._out[1], _ptr(norm)], stream)
+                                     g._out[1], _ptr(norm)])
     return norm
 
 
-def kd_clip_grad_norm(grads, max_norm, norm_kind=NORM_L2, workspace=None, stream=None):
+def kd_clip_grad_norm(grads, max_norm, norm_kind=NORM_L2, workspace=None):
     """kd_grad_norm and kd_grad_clip in one: clips all gradients together to the norm max_norm.  Returns the norm they had."""
     g = _grad_list(grads)
-    return kd_grad_clip(g, kd_grad_norm(g, norm_kind, workspace, stream), max_norm, norm_kind, stream)
+    return kd_grad_clip(g, kd_grad_norm(g, norm_kind, workspace), max_norm, norm_kind)
