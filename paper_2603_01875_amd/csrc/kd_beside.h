@@ -79,9 +79,12 @@ hipError_t launch_sample(const RowsArgs& r, hipStream_t st);
 // ---- gradient norm ----
 constexpr int kGradsPerLaunch = 160;
 constexpr int kNormGroups = 2048;      // workgroups of a launch
+// Elements of a piece.  (Norm and clipped copy, us, with 2048, 8192 and 32768: 3.2 million fp32 in 24 arrays 9.3 + 6.7, 7.3 + 6.1, 7.5 + 6.7; 30 million bf16 39 + 26,
+// 17 + 22, 14 + 21; 1.7 billion 1802 + 1505, 587 + 1338, 573 + 1313: finding a piece's array costs as much as some thousand elements.)
+constexpr int kPieceElements = 32768;
 struct GradTable {
   int n;                               // arrays of this launch
-  uint32_t chunks, chunk_elements;     // pieces of all arrays of this launch; elements of a piece
+  uint32_t chunks;                     // pieces of all arrays of this launch
   uint64_t in[kGradsPerLaunch];        // address, bit 0: fp32
   uint64_t count[kGradsPerLaunch];
   uint32_t first[kGradsPerLaunch];     // first piece of the array

@@ -65,13 +65,15 @@ kd::ProductArgs product_args(const kd_linear_params& p, const uint8_t* a, const 
 // ---- rows of logits ----
 struct RowsLayout { size_t chunk, group, wide, mass, total; };
 
-// Entries per thread of the first kernel: the most that leave two workgroups a CU and four groups for each entry of a list of `reach`;
-// rows have at most 1024 chunks.
+// Entries per thread of the first kernel: the most that leave 32 chunks in all and twelve groups for each entry of a list of `reach`;
+// rows have at most 1024 chunks.  Many entries a thread: less is read twice over by the second kernel; few: more workgroups, and groups that hold less beside
+// the list's entries.  us with 8, 16, 32 and 64 entries (T, V): top 20 of (512, 151936) 61, 46, 40, 39; top 256 of it 65, 50, 46, 54, of (64, 128256) 24, 20, 22, 27;
+// a token of (1, 151936) 12, 12, 13, 14, of (7, 32003) 12, 13, 14, 17, of (512, 151936) 89, 78, 71, 73, among the first 700 of (64, 128256) 37, 36, 39, 47.
 void plan_rows(kd::RowsArgs& r, RowsLayout& L, int64_t reach) {
   int e = 64;
   for (; e > 8; e >>= 1) {
     const int64_t chunks = (r.V + kd::kRowThreads * e - 1) / (kd::kRowThreads * e);
-    if (r.T * chunks >= 32 && r.V / e >= 4 * reach) break;
+    if (r.T * chunks >= 32 && r.V / e >= 12 * reach) break;
     if ((r.V + kd::kRowThreads * e / 2 - 1) / (kd::kRowThreads * e / 2) > 1024) break;
   }
   r.per_thread = e;
@@ -110,7 +112,7 @@ kd_status plan(const kd_sample_params* p, kd::RowsArgs& r, RowsLayout& L) {
     return KD_ERR_PARAM;
   r.T = p->T; r.V = p->V; r.ld = p->ld; r.f32 = p->in_dtype == KD_F32; r.index64 = p->index_dtype == KD_I64;
   r.tau = p->temperature; r.top_k = p->top_k; r.top_p = p->top_p; r.min_p = p->min_p;
-  plan_rows(r, L, 256);
+  plan_rows(r, L, p->top_k > 256 && p->top_k <= 1024 ? p->top_k : 256);
   if (r.V > kd::kWideList) {
     const int64_t rows = r.T < kd::kWideRows ? r.T : kd::kWideRows;
     const int64_t tiles = (r.V + kd::kWideTile - 1) / kd::kWideTile, parts = 4 * kd::kNumCU / rows;
@@ -138,15 +140,6 @@ void carve(kd::RowsArgs& r, const RowsLayout& L, void* ws) {
 }
 
 // ---- gradient norm ----
-// Elements of a piece, the same for all launches of a call: large ones cost the least, as long as there are some for every workgroup.
-uint32_t piece_elements(int32_t n, const int64_t* counts) {
-  int64_t all = 0;
-  for (int32_t i = 0; i < n; ++i) all += counts[i];
-  uint32_t e = 32768;
-  while (e > 2048 && all / e < 2 * kd::kNormGroups) e >>= 1;
-  return e;
-}
-
 kd_status check_counts(int32_t n, const int64_t* counts) {
   if (n < 1 || n > KD_GRADS_MAX) return KD_ERR_SHAPE;
   if (!counts) return KD_ERR_NULL;
@@ -173,13 +166,12 @@ kd_status check_arrays(int32_t n, const void* const* grads, const int64_t* count
 
 // The arrays from `i` on that one launch takes; the next one's first.  Arrays without elements are left out.
 int32_t fill(kd::GradTable& t, uint64_t* out, int32_t i, int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
-             void* const* outs, const int32_t* out_dtypes, uint32_t elements) {
+             void* const* outs, const int32_t* out_dtypes) {
   t.n = 0;
   t.chunks = 0;
-  t.chunk_elements = elements;
   for (; i < n && t.n < kd::kGradsPerLaunch; ++i) {
     if (!counts[i]) continue;
-    const int64_t pieces = (counts[i] + elements - 1) / elements;
+    const int64_t pieces = (counts[i] + kd::kPieceElements - 1) / kd::kPieceElements;
     t.in[t.n] = reinterpret_cast<uint64_t>(grads[i]) | (dtypes[i] == KD_F32);
     t.count[t.n] = (uint64_t)counts[i];
     t.first[t.n] = t.chunks;
@@ -322,12 +314,11 @@ kd_status kd_grad_norm(int32_t n, const void* const* grads, const int64_t* count
   kd_grad_norm_workspace_size(n, counts, &need);
   if (workspace_bytes < need) return KD_ERR_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const uint32_t elements = piece_elements(n, counts);
   double* const partials = static_cast<double*>(workspace);
   int64_t parts = 0;
   for (int32_t i = 0; i < n;) {
     kd::GradTable t{};
-    i = fill(t, nullptr, i, n, grads, counts, dtypes, nullptr, nullptr, elements);
+    i = fill(t, nullptr, i, n, grads, counts, dtypes, nullptr, nullptr);
     if (!t.n) break;
     KD_TRY(kd::launch_grad_norm(t, norm_kind == KD_NORM_MAX, partials + parts, groups_of(t), st));
     parts += groups_of(t);
@@ -352,11 +343,10 @@ kd_status kd_grad_clip(int32_t n, const void* const* grads, const int64_t* count
       if (out[i] == grads[i] && out_dtypes[i] != dtypes[i]) return KD_ERR_PARAM;
     }
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const uint32_t elements = piece_elements(n, counts);
   int32_t i = 0;
   do {
     kd::ClipTable t{};
-    i = fill(t.t, t.out, i, n, grads, counts, dtypes, out, out_dtypes, elements);
+    i = fill(t.t, t.out, i, n, grads, counts, dtypes, out, out_dtypes);
     KD_TRY(kd::launch_grad_clip(t, norm_kind == KD_NORM_MAX, total, max_norm, norm, st));
     norm = nullptr;
   } while (i < n);

@@ -35,9 +35,9 @@ __device__ __forceinline__ Piece piece_of(const GradTable& t, uint32_t piece) {
   const uint64_t a = t.in[p.array];
   p.f32 = (int)(a & 1);
   const int es = p.f32 ? 4 : 2;
-  p.begin = (int64_t)(piece - t.first[p.array]) * t.chunk_elements;
+  p.begin = (int64_t)(piece - t.first[p.array]) * kPieceElements;
   const int64_t left = (int64_t)t.count[p.array] - p.begin;
-  p.n = (int)(left < (int64_t)t.chunk_elements ? left : (int64_t)t.chunk_elements);
+  p.n = (int)(left < (int64_t)kPieceElements ? left : (int64_t)kPieceElements);
   p.in = (global_t)(a & ~1ull) + p.begin * es;
   const int head = (int)((16 - ((uint64_t)p.in & 15)) & 15) / es;
   p.head = head < p.n ? head : p.n;
