@@ -116,6 +116,7 @@ kd_status plan(const kd_sample_params* p, kd::RowsArgs& r, RowsLayout& L) {
   if (r.V > kd::kWideList) {
     const int64_t rows = r.T < kd::kWideRows ? r.T : kd::kWideRows;
     const int64_t tiles = (r.V + kd::kWideTile - 1) / kd::kWideTile, parts = 4 * kd::kNumCU / rows;
+    // (four workgroups a CU; one, four and eight: top-p 0.9 in 64 rows of 128256 fp32 74, 66 and 80 us, in 512 of 151936 bf16 282, 259 and 263)
     r.wide_parts = (int)(parts < 1 ? 1 : parts < tiles ? parts : tiles);
     L.wide = L.total;
     L.mass = (size_t)round_up((int64_t)L.wide + rows * (int64_t)sizeof(kd::RowWide), 256);

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(kTileThreads) void quantize_blocks_kernel(const Blo
   constexpr int R = kTileRows, WAVES = kTileThreads / 64, PITCH = 128 + 4;
   __shared__ uint32_t tops[WAVES][128];
   __shared__ Divisor divisors[128];
-  __shared__ uint8_t turned[128 * PITCH];
+  __shared__ __attribute__((aligned(16))) uint8_t turned[128 * PITCH];
   const int tid = threadIdx.x, tc = tid & 15, tr = tid >> 4, wave = tid >> 6;
   const int64_t n_cb = (a.cols + 127) / 128, n_rb = (a.rows + 127) / 128;
   const int64_t rb = blockIdx.x, cb = blockIdx.y;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const BlocksArgs a, 
 hipError_t launch_quantize_blocks(const BlocksArgs& a, hipStream_t st) {
   if (!a.tile && !a.codes_t) {
     int w_shift = 0;
-    while (w_shift < 4 && ((int64_t)128 << w_shift) < a.cols) ++w_shift;
+    while (w_shift < 3 && ((int64_t)128 << w_shift) < a.cols) ++w_shift;      // (two rows a workgroup at least: 2^24 rows are 2^31 threads)
     const int rows = 16 >> w_shift;
     const dim3 grid((uint32_t)((a.rows + rows - 1) / rows), (uint32_t)((a.cols + (128 << w_shift) - 1) / (128 << w_shift)));
     hipLaunchKernelGGL(a.src_f32 ? quantize_rows_kernel<true> : quantize_rows_kernel<false>, grid, dim3(256), 0, st, a, w_shift);

@@ -516,8 +516,11 @@ static hipError_t launch_few_of(const FewArgs& f, int grid, int smem, hipStream_
 static hipError_t launch_few(const ProductArgs& p, const void* x, int x_f32, hipStream_t st) {
   const int mb = p.M <= 16 ? 1 : 2;
   const int64_t groups = (p.N + 15) / 16;
+  // As many waves to 16 rows of b as there are kFewBlocks blocks for; where workgroups are many (more than four a CU), as leave each wave four times that.
+  // (1 x 151936 x 4096 with one, two, four and eight: 119, 113, 113, 125 us; 16 rows of a 140, 130, 142, 173; 8 x 151936 x 2048 56, 60, 71, 71;
+  // 8 x 40000 x 4096 with two and eight 31 and 38.)
   int wk = kFewWaves;
-  while (wk > 1 && (groups * wk > 4 * kNumCU * kFewWaves || (wk / 2) * kFewBlocks * 128 >= p.K)) wk >>= 1;
+  while (wk > 1 && ((groups * wk > 4 * kNumCU * kFewWaves && wk * 4 * kFewBlocks * 128 > p.K) || (wk / 2) * kFewBlocks * 128 >= p.K)) wk >>= 1;
   const FewArgs f{p, x, x_f32, wk};
   const int wn = kFewWaves / wk, grid = (int)((groups + wn - 1) / wn), smem = (int)few_smem(p.M, p.K, mb);
   if (mb == 1) return p.out_f32 ? launch_few_of<1, false>(f, grid, smem, st) : launch_few_of<1, true>(f, grid, smem, st);

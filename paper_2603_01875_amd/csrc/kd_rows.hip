@@ -8,8 +8,8 @@
 // Sampling under top-p or min-p without a top-k may keep any number of entries.  There two kernels come between, again many workgroups
 // to a row (wide): one adds up w by bins of the logit, the other the w above the bin in which the sum passes top-p of the whole, tile by tile, and
 // lists that bin's entries.
-// A list that does not fit (thousands of equal entries), a top-k of more than a list, and very many rows go the slow way: passes of the last kernel
-// over the row that narrow the last kept entry down.
+// A list that does not fit (thousands of equal entries) and a top-k of more than kReach go the slow way: passes of the last kernel over the row that narrow the
+// last kept entry down (top-k 3000 in 64 rows of 128256 fp32: 281 us, beside 43 for 1000).
 #include <hip/hip_runtime.h>
 
 #include "kd_beside.h"
@@ -783,7 +783,7 @@ __global__ __launch_bounds__(kSelect) void sample_bins_kernel(const RowsArgs a) 
     if (s.flat[i]) atomicAdd((unsigned long long*)&a.wide[p.t - a.row0].bins[i], (unsigned long long)s.flat[i]);
 }
 
-// The bin in which the sum over the bins passes `share` of the whole, the sum in front of it and what is left to reach in it.
+// The bin in which the sum over the bins passes `share` of the whole, and what is left to reach in it.
 struct Border { uint32_t bin; uint64_t left; };
 __device__ __forceinline__ Border border_of(const uint64_t* bins, double share, SelectLds& s) {
   constexpr int PER = kFlat / kSelect;
@@ -1042,10 +1042,17 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
   }
 
   // A list of up to half a list is sorted, and its sums are those of places.  (64 rows of 128256 fp32, us, so and by the digits below: top-k 300 29 and 38, 1000 43 and 45,
-  // 1000 with top-p 0.9 43 and 58.)
-  const bool sorts = from == LIST && found <= (uint32_t)kList / 2 && (k < (int64_t)found || d.top_p < 1.f);
+  // 1000 with top-p 0.9 43 and 58.  A wide bin's entries lie close to each other, which is where sorting is slow: one row of 151936 bf16, top-p 0.9, 31 and 38; but
+  // lists of up to 2048 of 64 rows of 128256 fp32 82 and 66.)
+  const bool sorts = from == LIST ? found <= (uint32_t)kList / 2 && (k < (int64_t)found || d.top_p < 1.f) : from == WIDE && d.top_p < 1.f && found <= (uint32_t)kSelect;
   if (sorts) {
     constexpr int PER = kList / 2 / kSelect;
+    uint64_t want = 0;
+    if (from == WIDE) {
+      want = border_of(a.wide[t - a.row0].bins, (double)d.top_p, s).left;
+      s.list[tid] = held[0];
+      __syncthreads();
+    }
     sort_by_bins(found, key, s);
     uint64_t w[PER], sum = 0, all;
 #pragma unroll
@@ -1055,8 +1062,10 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
       sum += w[i];
     }
     uint64_t before = prefix(sum, all, s);
-    uint64_t want = (uint64_t)ceil((double)d.top_p * (double)all);
-    want = want < 1 ? 1 : want < all ? want : all;
+    if (from == LIST) {
+      want = (uint64_t)ceil((double)d.top_p * (double)all);
+      want = want < 1 ? 1 : want < all ? want : all;
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       if (before < want && before + w[i] >= want) s.value[0] = s.list[tid * PER + i];
