@@ -212,3 +212,10 @@ def test_a_gradient_of_more_than_two_to_the_31_elements():
     assert abs(got.item() - norm) <= 2.0 ** -23 * norm
     f = np.float32(norm / 2) / norm
     assert abs(g[n - 1].item() - 64 * f) <= 2.0 ** -7 * 64 and bool((g[:-1] == g[0]).all()) and abs(g[0].item() - 2.0 ** -10 * f) <= 2.0 ** -18
+
+
+def test_most_rows_that_a_matrix_may_have():
+    rows, cols = 1 << 24, 1040
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(7))
+    q, r = K.quantize_e4m3_blocks(x), K.quantize_e4m3_blocks(x[-300:].clone())
+    assert torch.equal(q.codes[-300:], r.codes) and torch.equal(q.scales[-300:], r.scales)
