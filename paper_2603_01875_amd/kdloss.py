@@ -1055,6 +1055,19 @@ def _grad_list(grads):
     return grads if isinstance(grads, GradList) else GradList(grads)
 
 
+def _norm_call(g, norm_kind, total, workspace, workspace_bytes):
+    _call("kd_grad_norm", g.device, [g.n, g._in[0], g.counts, g._in[1], int(norm_kind), ctypes.c_void_p(total), ctypes.c_void_p(workspace),
+                                     ctypes.c_size_t(workspace_bytes)])
+
+
+def _clip_call(g, total, max_norm, norm_kind):
+    import torch
+    norm = torch.empty((), dtype=torch.float32, device=g.device)
+    _call("kd_grad_clip", g.device, [g.n, g._in[0], g.counts, g._in[1], int(norm_kind), ctypes.c_void_p(total), float(max_norm), g._out[0],
+                                     g._out[1], _ptr(norm)])
+    return norm
+
+
 def kd_grad_norm(grads, norm_kind=NORM_L2, workspace=None):
     """The sum of all squares (NORM_L2) or the largest magnitude (NORM_MAX) over a GradList or a list of tensors, as one float64 on the
     device.  A program with gradients spread over ranks all-reduces it and goes on with kd_grad_clip."""
@@ -1063,8 +1076,7 @@ def kd_grad_norm(grads, norm_kind=NORM_L2, workspace=None):
     total = torch.empty((), dtype=torch.float64, device=g.device)
     ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=g.device) if workspace is None else workspace
     _check_workspace(ws, g.device)
-    _call("kd_grad_norm", g.device, [g.n, g._in[0], g.counts, g._in[1], int(norm_kind), _ptr(total), _ptr(ws),
-                                     ctypes.c_size_t(_nbytes(ws))])
+    _norm_call(g, norm_kind, total.data_ptr(), ws.data_ptr(), _nbytes(ws))
     return total
 
 
@@ -1074,13 +1086,17 @@ def kd_grad_clip(grads, total, max_norm, norm_kind=NORM_L2):
     import torch
     g = _grad_list(grads)
     _check_tensors([("total", total, (torch.float64,), 1, False)], g.device)
-    norm = torch.empty((), dtype=torch.float32, device=g.device)
-    _call("kd_grad_clip", g.device, [g.n, g._in[0], g.counts, g._in[1], int(norm_kind), _ptr(total), float(max_norm), g._out[0],
-                                     g._out[1], _ptr(norm)])
-    return norm
+    return _clip_call(g, total.data_ptr(), max_norm, norm_kind)
 
 
 def kd_clip_grad_norm(grads, max_norm, norm_kind=NORM_L2, workspace=None):
     """kd_grad_norm and kd_grad_clip in one: clips all gradients together to the norm max_norm.  Returns the norm they had."""
+    import torch
     g = _grad_list(grads)
-    return kd_grad_clip(g, kd_grad_norm(g, norm_kind, workspace), max_norm, norm_kind)
+    if workspace is not None:
+        return kd_grad_clip(g, kd_grad_norm(g, norm_kind, workspace), max_norm, norm_kind)
+    # (the total behind the workspace: an allocation costs as much as a launch's arguments)
+    ws = torch.empty(g.workspace_bytes + 256, dtype=torch.uint8, device=g.device)
+    total = ws.data_ptr() + g.workspace_bytes
+    _norm_call(g, norm_kind, total, ws.data_ptr(), g.workspace_bytes)
+    return _clip_call(g, total, max_norm, norm_kind)
