@@ -15,6 +15,7 @@
 #include "kd_beside.h"
 #include "kd_launch.h"
 #include "kd_unaligned.hpp"
+#include "kd_weight.hpp"
 
 namespace kd {
 
@@ -36,40 +37,6 @@ template <bool F32>
 __device__ __forceinline__ const void* row_of(const RowsArgs& a, int64_t t) {
   return (const char*)a.logits + t * a.ld * (F32 ? 4 : 2);
 }
-
-// ------------------------------------------------------------------------------------------------
-// w = 2^t in 64 bits, t <= 0
-//
-// t = n + x with a whole number n and |x| <= 1/2; 2^x is the polynomial of degree 8 that meets it at the Chebyshev nodes of [-1/2, 1/2] (1 at 0; off by
-// 2^-39.7 at most), 2^n is added to its exponent.  n comes out of the low bits of t + 1.5 2^52: no conversion, no table.  13 instructions in 64 bits; an exp
-// in 32 bits would be off by 2^-24 in every sum that a uniform number is compared with: one token in some thousand would be another one.
-// ------------------------------------------------------------------------------------------------
-constexpr double kLog2e = 1.44269504088896340736;
-constexpr int kChunkBits = 48;         // a chunk's sums: 2^14 entries of at most 2^48 (0x1p48 below)
-
-__device__ __forceinline__ double weight(double t) {
-  t = fmax(t, -80.);                                   // (2^-80 and less count as nothing; also for a NaN, where a chunk is empty)
-  const double m = t + 0x1.8p52, x = t - (m - 0x1.8p52);
-  double p = 0x1.63d1363930791p-20;
-  p = fma(p, x, 0x1.00dc4a53395d3p-16);
-  p = fma(p, x, 0x1.4308ac85a7718p-13);
-  p = fma(p, x, 0x1.5d8745a72831bp-10);
-  p = fma(p, x, 0x1.3b2ab7181b778p-7);
-  p = fma(p, x, 0x1.c6b08dd6fd236p-5);
-  p = fma(p, x, 0x1.ebfbdff823cedp-3);
-  p = fma(p, x, 0x1.62e42fef84cf0p-1);
-  p = fma(p, x, 1.);
-  return __hiloint2double(__double2hiint(p) + (__double2loint(m) << 20), __double2loint(p));
-}
-// A weight (or a sum of some) as a whole number of 2^-bits.
-__device__ __forceinline__ uint64_t whole(double w, int bits) { return (uint64_t)rint(ldexp(w, bits)); }
-// The same of a single one (less than 2^52 of them, so that they are the low bits of what 2^52 is added to); scale = 2^bits.
-__device__ __forceinline__ uint64_t whole_one(double w, double scale) {
-  return (uint64_t)(__double_as_longlong(fma(w, scale, 0x1p52)) - __double_as_longlong(0x1p52));
-}
-
-// A chunk's weights are 2^(z scale - zero) with zero = top scale, rounded: off by the same factor 2^offset all of them, offset = top scale - zero.
-__device__ __forceinline__ double chunk_offset(double top, double scale) { return fma(top, scale, -(top * scale)); }
 
 // ------------------------------------------------------------------------------------------------
 // first kernel
@@ -157,10 +124,13 @@ __global__ __launch_bounds__(kRowThreads) void rows_scan_kernel(const RowsArgs a
     const float tau = row_temperature(a, t);
     uint64_t s = 0;
     if (tau > 0.f) {
-      const double scale = kLog2e / (double)tau, zero = (double)top * scale;      // (rounded: see chunk_offset)
+      const Exponents x = exponents_of(top, kLog2e / (double)tau);
+      if (x.base != 0.f)
+#pragma unroll
+        for (int i = 0; i < E; ++i) z[i] -= x.base;
       double w = 0;
 #pragma unroll
-      for (int i = 0; i < E; ++i) w += weight(fma((double)z[i], scale, -zero));
+      for (int i = 0; i < E; ++i) w += weight(fma((double)z[i], x.scale, -x.zero));
       s = whole(w, kChunkBits);
     }
 #pragma unroll
@@ -894,9 +864,9 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
     auto chunk_mass = [&](int c) {
       const RowChunk& q = a.chunk[t * a.chunks + c];
       if (q.key <= kKeyMinusInf) return (uint64_t)0;
-      const double z0 = value_of(q.key);
-      return whole((double)q.sum * exp2((z0 - top) * scale - chunk_offset(z0, scale)), row_bits - kChunkBits);
+      return whole((double)q.sum * rescale(value_of(q.key), top, scale), row_bits - kChunkBits);
     };
+    if (tid == 0) s.value[0] = s.value[1] = 0;      // (a thread's share holds the target, whatever it is; were it not so, chunk 0 would be read)
 #pragma unroll 1
     for (int c = c0; c < c0 + per && c < a.chunks; ++c) part += chunk_mass(c);
     const uint64_t before = prefix(part, row_total, s);
@@ -917,8 +887,9 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
       }
       __syncthreads();
       const int c = (int)s.value[0];
-      const double z0 = value_of(a.chunk[t * a.chunks + c].key), z0_scaled = z0 * scale;
-      const double inner = ldexp((double)s.value[1], kChunkBits - row_bits) * exp2((top - z0) * scale + chunk_offset(z0, scale));
+      const float z0 = value_of(a.chunk[t * a.chunks + c].key);
+      const Exponents ex = exponents_of(z0, scale);
+      const double inner = ldexp((double)s.value[1], kChunkBits - row_bits) * rescale(top, z0, scale);
       // that chunk again, with its own sums; thread i has `each` entries from the i-th on, VE at a time
       constexpr int VE = F32 ? 4 : 8, MOST = 32 / VE;
       const int each = max(VE, a.per_thread * kRowThreads / kSelect), entries = kRowThreads * a.per_thread;
@@ -940,7 +911,7 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
 #pragma unroll
           for (int i = 0; i < VE; ++i) z[i] = here && j * VE < each && at + i < V ? logit<F32>(r.p, at + i) : -__builtin_inff();
       };
-      auto w_of = [&](float v) { return whole_one(weight(fma((double)v, scale, -z0_scaled)), 0x1p48); };
+      auto w_of = [&](float v) { return whole_one(weight(exponent(ex, v)), 0x1p48); };
       float z[MOST][VE];
       uint64_t sums[MOST], mine = 0, all;
 #pragma unroll
@@ -1142,7 +1113,8 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
     }
   }
   __syncthreads();
-  // the tile in which the sum passes the target, and the entry in the tile
+  // the tile in which the sum passes the target (one thread's share holds it; were it not so, tile 0 would be read), and the entry in the tile
+  if (tid == 0) s.value[0] = s.value[1] = 0;
   const int per = (tiles + kSelect - 1) / kSelect, b0 = tid * per;
   uint64_t part = 0, total;
   for (int b = b0; b < b0 + per && b < tiles; ++b) part += s.mass[b];
