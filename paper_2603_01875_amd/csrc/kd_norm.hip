@@ -141,11 +141,15 @@ __device__ __forceinline__ void stream_out(global_t p, const V& v) {
   __builtin_nontemporal_store(v, (KD_GLOBAL Any*)p);
 }
 
+// The factor as f 2^e, f from 1/2 to 1: below 2^-126 it would lose bits in 32 (gradients of 1e10 and a limit of 1e-30), and x f 2^e may be a normal number all the same.
+struct Factor { float f; int e; };
+__device__ __forceinline__ float scaled(float x, const Factor& f) { return ldexpf(x * f.f, f.e); }
+
 template <bool IN32, bool OUT32>
-__device__ __forceinline__ void scale_piece(const Piece& p, global_t out, float f) {
+__device__ __forceinline__ void scale_piece(const Piece& p, global_t out, const Factor& f) {
   constexpr int VE = IN32 ? 4 : 8;
   auto one = [&](int i) {
-    const float y = element(p.in, IN32, i) * f;
+    const float y = scaled(element(p.in, IN32, i), f);
     if (OUT32) ((KD_GLOBAL float*)out)[i] = y;
     else ((KD_GLOBAL uint16_t*)out)[i] = bf16_bits(y);
   };
@@ -157,10 +161,10 @@ __device__ __forceinline__ void scale_piece(const Piece& p, global_t out, float 
     float y[VE];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (IN32) y[k] = __uint_as_float(x[k]) * f;
+      if (IN32) y[k] = scaled(__uint_as_float(x[k]), f);
       else {
-        y[(2 * k) % VE] = __uint_as_float(x[k] << 16) * f;
-        y[(2 * k + 1) % VE] = __uint_as_float(x[k] & 0xffff0000u) * f;
+        y[(2 * k) % VE] = scaled(__uint_as_float(x[k] << 16), f);
+        y[(2 * k + 1) % VE] = scaled(__uint_as_float(x[k] & 0xffff0000u), f);
       }
     }
     if (OUT32) {
@@ -199,7 +203,8 @@ __global__ __launch_bounds__(kNormThreads) void grad_clip_kernel(const ClipTable
   const double sum = *total, norm = max_kind ? sum : sqrt(sum);
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   const bool clips = norm > max_norm && norm < __builtin_inf();
-  const float f = clips ? (float)(max_norm / norm) : 1.f;
+  Factor f{1.f, 0};
+  if (clips) f.f = (float)frexp(max_norm / norm, &f.e);
   for (uint32_t i = blockIdx.x; i < c.t.chunks; i += gridDim.x) {
     const Piece p = piece_of(c.t, c.t.chunks - 1 - i);
     const uint64_t o = c.out[p.array];
