@@ -411,8 +411,9 @@ kd_status kd_top_logits(const kd_top_logits_params* params, const void* logits, 
  *   (1: all, at least one); of those the ones with w >= min_p (0: all).
  *   token[t] = the first kept v, in order of v, where the sum of the kept w up to and with v exceeds u[t] times the sum of all kept
  *   logp[t]  = log of w_token over that sum (may be NULL)
- * w and its sums are held in 64 bits (exp to 2^-39; sums of many threads are whole numbers of 2^-48 to 2^-61 V), so that which token is drawn
- * does not depend on the order of a sum.  temperature 0: the first of the largest logits, logp 0.  A setting may be the
+ * w and its sums are held in 64 bits: exp to 2^-39, and each w as a whole number of 2^-51, or of 2^-62 S where the row's sum S of w is above 2^11, so that which
+ * token is drawn does not depend on the order of a sum, and a sum is off by at most V 2^-52 (or 2^-62 V S) by that; without a filter, where sums of w are rounded, by at most
+ * V 2^-51 + 2^-34.  temperature 0: the first of the largest logits, logp 0.  A setting may be the
  * same for all rows (in params) or an array of one per row (temperature_rows, ... device pointers; NULL: params').  A logit of minus
  * infinity is never drawn.  token is -1 and logp NaN in a row without a finite logit, with a NaN or a logit of plus infinity,
  * and where u or a row's own setting is outside its range. */

@@ -709,10 +709,32 @@ __device__ __forceinline__ Draw draw_of(const RowsArgs& a, int64_t t, uint32_t k
             d.min_p >= 0.f && d.min_p <= 1.f && key > kKeyMinusInf && key < kKeyInf;
   return d;
 }
-// Bits of a weight in sums over a whole row: V entries of at most 2^bits.
+// Bits of a weight in sums of chunks' sums: V entries of at most 2^bits.
 __device__ __forceinline__ int bits_of_row(int64_t V) { return min(kChunkBits, 62 - (64 - __clzll((unsigned long long)V))); }
-__device__ __forceinline__ Row row_for(const void* row, int64_t V, float top, double scale) {
-  return Row{row, V, top, scale, (float)((kFlat - 1) / 44. * scale), ldexp(1., bits_of_row(V))};
+// Bits of a weight in sums over the row's entries, each of them rounded: as many as the row's sum leaves of 62, and no more than whole_one takes.  (As many as V equal
+// entries leave would be 44 at V = 151936 and 37 at 2^24: a tail of small weights, all rounded the same way, would be off by V halves of that.)  The chunks'
+// sums in 32 bits, in a fixed order: whoever asks for a row gets the same bits.
+constexpr int kMostBits = 51;
+__device__ __forceinline__ int bits_of_sum(const RowsArgs& a, int64_t t, float top, double scale, SelectLds& s) {
+  float sum = 0.f;
+  for (int c = threadIdx.x; c < a.chunks; c += kSelect) {
+    const RowChunk& q = a.chunk[t * a.chunks + c];
+    if (q.key > kKeyMinusInf) sum += (float)q.sum * __builtin_amdgcn_exp2f((value_of(q.key) - top) * (float)scale);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+  if ((threadIdx.x & 63) == 0) s.part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  double all = 0;
+#pragma unroll
+  for (int w = 0; w < kSelect / 64; ++w) all += s.part[w];
+  __syncthreads();
+  int e;                               // (the sum is less than 2^e)
+  frexp(fmax(ldexp(all, -kChunkBits), 1.), &e);
+  return min(kMostBits, 62 - e);
+}
+__device__ __forceinline__ Row row_for(const void* row, int64_t V, float top, double scale, int bits) {
+  return Row{row, V, top, scale, (float)((kFlat - 1) / 44. * scale), ldexp(1., bits)};
 }
 
 // The part of a row that a workgroup of the wide kernels has: tiles first .. last - 1.
@@ -743,7 +765,8 @@ __global__ __launch_bounds__(kSelect) void sample_bins_kernel(const RowsArgs a) 
   const uint32_t key = largest_key(a, p.t, s);
   const Draw d = draw_of(a, p.t, key);
   if (!d.wide() || d.top_p == 1.f) return;
-  const Row r = row_for(row_of<F32>(a, p.t), a.V, value_of(key), kLog2e / (double)d.tau);
+  const double scale = kLog2e / (double)d.tau;
+  const Row r = row_for(row_of<F32>(a, p.t), a.V, value_of(key), scale, bits_of_sum(a, p.t, value_of(key), scale, s));
   for (int i = tid; i < kFlat; i += kSelect) s.flat[i] = 0;
   __syncthreads();
   for (int b = p.first; b < p.last; ++b) {
@@ -795,7 +818,8 @@ __global__ __launch_bounds__(kSelect) void sample_tiles_kernel(const RowsArgs a)
   const uint32_t key = largest_key(a, p.t, s);
   const Draw d = draw_of(a, p.t, key);
   if (!d.wide()) return;
-  const Row r = row_for(row_of<F32>(a, p.t), a.V, value_of(key), kLog2e / (double)d.tau);
+  const double scale = kLog2e / (double)d.tau;
+  const Row r = row_for(row_of<F32>(a, p.t), a.V, value_of(key), scale, bits_of_sum(a, p.t, value_of(key), scale, s));
   const uint32_t bin = d.top_p < 1.f ? border_of(a.wide[p.t - a.row0].bins, (double)d.top_p, s).bin : ~0u;
   const uint64_t least = (uint64_t)ceil((double)d.min_p * r.one);
   for (int b = p.first; b < p.last; ++b) {
@@ -850,16 +874,14 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
     return;
   }
   const double top = value_of(key), scale = kLog2e / (d.greedy ? 1. : (double)d.tau);
-  const Row r = row_for(row_of<F32>(a, t), V, (float)top, scale);
-  const int row_bits = bits_of_row(V), tiles = (int)((V + kTile - 1) / kTile);
-  auto log_p = [&](float z, uint64_t total) {
-    return d.greedy ? 0.f : (float)(((double)z - top) / (double)d.tau - log(ldexp((double)total, -row_bits)));
-  };
+  const int tiles = (int)((V + kTile - 1) / kTile);
+  auto log_p = [&](float z, double sum) { return d.greedy ? 0.f : (float)(((double)z - top) / (double)d.tau - log(sum)); };
 
-  uint64_t row_total = 0;
-  if (d.all_k) {
+  if (d.all_k && d.top_p == 1.f && d.min_p == 0.f) {
     // chunks' sums at the row's largest entry
-    uint64_t part = 0;
+    const int row_bits = bits_of_row(V);
+    const void* const row = row_of<F32>(a, t);
+    uint64_t part = 0, row_total;
     const int per = (a.chunks + kSelect - 1) / kSelect, c0 = tid * per;
     auto chunk_mass = [&](int c) {
       const RowChunk& q = a.chunk[t * a.chunks + c];
@@ -870,94 +892,95 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
 #pragma unroll 1
     for (int c = c0; c < c0 + per && c < a.chunks; ++c) part += chunk_mass(c);
     const uint64_t before = prefix(part, row_total, s);
-    if (d.top_p == 1.f && d.min_p == 0.f) {
-      const uint64_t target = target_of(d.u, row_total);
-      if (before <= target && target < before + part) {
-        uint64_t x = before;
+    const uint64_t target = target_of(d.u, row_total);
+    if (before <= target && target < before + part) {
+      uint64_t x = before;
 #pragma unroll 1
-        for (int c = c0; c < c0 + per && c < a.chunks; ++c) {
-          const uint64_t m = chunk_mass(c);
-          if (target < x + m) {
-            s.value[0] = c;
-            s.value[1] = target - x;
-            break;
-          }
-          x += m;
+      for (int c = c0; c < c0 + per && c < a.chunks; ++c) {
+        const uint64_t m = chunk_mass(c);
+        if (target < x + m) {
+          s.value[0] = c;
+          s.value[1] = target - x;
+          break;
+        }
+        x += m;
+      }
+    }
+    __syncthreads();
+    const int c = (int)s.value[0];
+    const float z0 = value_of(a.chunk[t * a.chunks + c].key);
+    const Exponents ex = exponents_of(z0, scale);
+    const double inner = ldexp((double)s.value[1], kChunkBits - row_bits) * rescale(top, z0, scale);
+    // that chunk again, with its own sums; thread i has `each` entries from the i-th on, VE at a time
+    constexpr int VE = F32 ? 4 : 8, MOST = 32 / VE;
+    const int each = max(VE, a.per_thread * kRowThreads / kSelect), entries = kRowThreads * a.per_thread;
+    const int64_t i0 = (int64_t)c * entries + (int64_t)tid * each;
+    const bool here = (tid + 1) * each <= entries;
+    auto load = [&](float (&z)[VE], int j) {
+      const int64_t at = i0 + j * VE;
+      const bool in = here && j * VE < each && at + VE <= V;
+      const u32x4_t v = V >= VE ? load16((const char*)row + (in ? at : 0) * (F32 ? 4 : 2)) : u32x4_t{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (F32) z[i] = __uint_as_float(v[i]);
+        else {
+          z[(2 * i) % VE] = __uint_as_float(v[i] << 16);
+          z[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
         }
       }
-      __syncthreads();
-      const int c = (int)s.value[0];
-      const float z0 = value_of(a.chunk[t * a.chunks + c].key);
-      const Exponents ex = exponents_of(z0, scale);
-      const double inner = ldexp((double)s.value[1], kChunkBits - row_bits) * rescale(top, z0, scale);
-      // that chunk again, with its own sums; thread i has `each` entries from the i-th on, VE at a time
-      constexpr int VE = F32 ? 4 : 8, MOST = 32 / VE;
-      const int each = max(VE, a.per_thread * kRowThreads / kSelect), entries = kRowThreads * a.per_thread;
-      const int64_t i0 = (int64_t)c * entries + (int64_t)tid * each;
-      const bool here = (tid + 1) * each <= entries;
-      auto load = [&](float (&z)[VE], int j) {
-        const int64_t at = i0 + j * VE;
-        const bool in = here && j * VE < each && at + VE <= V;
-        const u32x4_t v = V >= VE ? load16((const char*)r.p + (in ? at : 0) * (F32 ? 4 : 2)) : u32x4_t{0, 0, 0, 0};
+      if (!in)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (F32) z[i] = __uint_as_float(v[i]);
-          else {
-            z[(2 * i) % VE] = __uint_as_float(v[i] << 16);
-            z[(2 * i + 1) % VE] = __uint_as_float(v[i] & 0xffff0000u);
-          }
-        }
-        if (!in)
+        for (int i = 0; i < VE; ++i) z[i] = here && j * VE < each && at + i < V ? logit<F32>(row, at + i) : -__builtin_inff();
+    };
+    auto w_of = [&](float v) { return whole_one(weight(exponent(ex, v)), 0x1p48); };
+    float z[MOST][VE];
+    uint64_t sums[MOST], mine = 0, all;
 #pragma unroll
-          for (int i = 0; i < VE; ++i) z[i] = here && j * VE < each && at + i < V ? logit<F32>(r.p, at + i) : -__builtin_inff();
-      };
-      auto w_of = [&](float v) { return whole_one(weight(exponent(ex, v)), 0x1p48); };
-      float z[MOST][VE];
-      uint64_t sums[MOST], mine = 0, all;
+    for (int j = 0; j < MOST; ++j) load(z[j], j);
 #pragma unroll
-      for (int j = 0; j < MOST; ++j) load(z[j], j);
+    for (int j = 0; j < MOST; ++j) {
+      sums[j] = 0;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) sums[j] += w_of(z[j][i]);
+      mine += sums[j];
+    }
+    uint64_t x = prefix(mine, all, s);
+    const uint64_t want = inner < (double)all ? (uint64_t)inner : all - 1;
+    if (x <= want && want < x + mine) {
+      int at = 0;
+      bool past = false;
 #pragma unroll
       for (int j = 0; j < MOST; ++j) {
-        sums[j] = 0;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) sums[j] += w_of(z[j][i]);
-        mine += sums[j];
-      }
-      uint64_t x = prefix(mine, all, s);
-      const uint64_t want = inner < (double)all ? (uint64_t)inner : all - 1;
-      if (x <= want && want < x + mine) {
-        int at = 0;
-        bool past = false;
-#pragma unroll
-        for (int j = 0; j < MOST; ++j) {
-          past |= want < x + sums[j];
-          if (!past) {
-            x += sums[j];
-            at = j + 1;
-          }
-        }
-        float v[VE];
-        load(v, at);
-        past = false;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) {
-          x += w_of(v[i]);
-          if (x > want && !past) {
-            answer(i0 + at * VE + i, log_p(v[i], row_total));
-            past = true;
-          }
+        past |= want < x + sums[j];
+        if (!past) {
+          x += sums[j];
+          at = j + 1;
         }
       }
-      return;
+      float v[VE];
+      load(v, at);
+      past = false;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        x += w_of(v[i]);
+        if (x > want && !past) {
+          answer(i0 + at * VE + i, log_p(v[i], ldexp((double)row_total, -row_bits)));
+          past = true;
+        }
+      }
     }
+    return;
   }
 
-  const uint64_t least = (uint64_t)ceil((double)d.min_p * r.one);
+  // (the sums of a list: of no more than kList entries)
+  static_assert(kList <= 1 << 12, "62 bits");
+  const bool wide = a.wide && d.wide();
+  Row r = row_for(row_of<F32>(a, t), V, (float)top, scale, wide ? bits_of_sum(a, t, (float)top, scale, s) : 50);
   const int64_t k = d.greedy ? 1 : d.all_k ? V : d.top_k;
   uint64_t held[kHeld], limit = 1;      // entries; the last kept one
   uint32_t found = 0;
   enum { WIDE, LIST, ROW } from = ROW;  // where the kept entries are: above a bin and in its list; in a list of the largest; anywhere
-  if (a.wide && d.wide()) {
+  if (wide) {
     found = d.top_p < 1.f ? a.wide[t - a.row0].count : 0;
     if (found <= (uint32_t)kList) {
       from = WIDE;
@@ -987,6 +1010,7 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
         return;
       }
       if (listed && found <= 128) {
+        const uint64_t least = (uint64_t)ceil((double)d.min_p * r.one);
         // one entry a thread: what is in front of it in descending order, then what is kept in front of it in order of the index
         uint64_t* const w = s.list + 128;
         const uint64_t mine = held[0], my_w = mine ? row_weight(r, entry_value(mine)) : 0;
@@ -1012,7 +1036,7 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
           uint64_t y = 0;
 #pragma unroll 8
           for (uint32_t i = 0; i < found; ++i) y += entry_index(s.list[i]) < entry_index(mine) ? w[i] : 0;
-          if (y <= target && target < y + my_w) answer(entry_index(mine), log_p(entry_value(mine), total));
+          if (y <= target && target < y + my_w) answer(entry_index(mine), log_p(entry_value(mine), (double)total / r.one));
         }
         return;
       }
@@ -1020,6 +1044,8 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
     }
   }
 
+  if (from == ROW && !wide) r.one = ldexp(1., bits_of_sum(a, t, (float)top, scale, s));
+  const uint64_t least = (uint64_t)ceil((double)d.min_p * r.one);
   // A list of up to half a list is sorted, and its sums are those of places.  (64 rows of 128256 fp32, us, so and by the digits below: top-k 300 29 and 38, 1000 43 and 45,
   // 1000 with top-p 0.9 43 and 58.  A wide bin's entries lie close to each other, which is where sorting is slow: one row of 151936 bf16, top-p 0.9, 31 and 38; but
   // lists of up to 2048 of 64 rows of 128256 fp32 82 and 66.)
@@ -1148,7 +1174,7 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
     for (int i = 0; i < kEach; ++i) {
       y += w[i];
       if (y > want && !done) {
-        answer(at + i, log_p(z[i], total));
+        answer(at + i, log_p(z[i], (double)total / r.one));
         done = true;
       }
     }
