@@ -972,10 +972,10 @@ __global__ __launch_bounds__(kSelect, 4) void sample_select_kernel(const RowsArg
     return;
   }
 
-  // (the sums of a list: of no more than kList entries)
-  static_assert(kList <= 1 << 12, "62 bits");
+  // (the sums of a list, of no more than kList entries, have room for all bits that a weight may have)
+  static_assert(kList <= 1 << (63 - kMostBits), "64 bits");
   const bool wide = a.wide && d.wide();
-  Row r = row_for(row_of<F32>(a, t), V, (float)top, scale, wide ? bits_of_sum(a, t, (float)top, scale, s) : 50);
+  Row r = row_for(row_of<F32>(a, t), V, (float)top, scale, wide ? bits_of_sum(a, t, (float)top, scale, s) : kMostBits);
   const int64_t k = d.greedy ? 1 : d.all_k ? V : d.top_k;
   uint64_t held[kHeld], limit = 1;      // entries; the last kept one
   uint32_t found = 0;
