@@ -922,8 +922,9 @@ def make_top_logits_params(T, V, K, ld=None, tau=1.0, in_dtype=BF16, index_dtype
 
 
 def make_sample_params(T, V, ld=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, in_dtype=BF16, index_dtype=I64):
+    # (a top_k that 32 bits do not hold keeps all entries, as any that is no less than V)
     return KdSampleParams(int(T), int(V), int(V if ld is None else ld), int(in_dtype), int(index_dtype), float(temperature),
-                          int(top_k), float(top_p), float(min_p))
+                          max(-1, min(int(top_k), (1 << 31) - 1)), float(top_p), float(min_p))
 
 
 def _check_logits(p, logits):
