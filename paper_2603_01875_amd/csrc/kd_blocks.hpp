@@ -9,9 +9,8 @@ constexpr uint32_t kLeastBlock = 0x04e00000u;        // 448 2^-126
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 __device__ __forceinline__ float scale_of(uint32_t m) { return m < 0x7f800000u ? __uint_as_float(m) / 448.f : __builtin_nanf(""); }
 
-// 448 x / m, rounded once, as a division of the exact 448 x rounds it:  m = 2^e f with 1 <= f < 2, a = (448 2^-e) x, q = a (1 / f), and then the remainder's share,
-// (a - q f) (1 / f), added.  448 x is exact for bf16; for fp32 its own remainder joins q's.  (Of the 5.4 10^8 pairs of significands of fp32 whose quotient lies next to a border between
-// two codes, one, 12170971 / 13631487, is taken for the border itself, half a step of fp32 away.)  A division for every element took
+// 448 x / m, rounded as 448 x and its quotient by m are:  m = 2^e f with 1 <= f < 2, a = (448 2^-e) x, q = a (1 / f), and then the remainder's share,
+// (a - q f) (1 / f), added in one rounding, which gives the quotient that a division gives (448 x is exact for bf16).  A division for every element took
 // three times as many instructions.
 struct Divisor { float c, f, inv; };
 __device__ __forceinline__ Divisor divisor_of(uint32_t m) {
@@ -23,11 +22,8 @@ __device__ __forceinline__ Divisor divisor_of(uint32_t m) {
 }
 template <bool F32>
 __device__ __forceinline__ float quotient(float x, const Divisor& d) {
-#pragma clang fp contract(off)
-  const float a = x * d.c, q = a * d.inv, r = fmaf(-q, d.f, a);
-  if (!F32) return fmaf(r, d.inv, q);
-  const float share = (r + fmaf(x, d.c, -a)) * d.inv;      // (rounded by itself: halfway between two floats the sum then is what it should be)
-  return q + share;
+  const float a = x * d.c, q = a * d.inv, y = fmaf(fmaf(-q, d.f, a), d.inv, q);
+  return F32 ? __builtin_amdgcn_fmed3f(y, -448.f, 448.f) : y;      // (448 x rounded may be one step more than 448 m)
 }
 // codes of quotients (of a block with an infinity or a NaN: anything, its scale is NaN)
 __device__ __forceinline__ uint32_t codes_of4(float a, float b, float c, float d) {
