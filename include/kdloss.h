@@ -352,8 +352,8 @@ typedef struct {
   int32_t reserved[2];        /* must be 0                                                       */
 } kd_blocks_params;
 
-/* Quantises a matrix in blocks:  scale = m / 448 with m = max(largest |src| of the block, 448 2^-126), code = e4m3(448 src / m), the
- * quotient rounded once in fp32, then to nearest even.  A block that holds an infinity or a NaN has the scale NaN.
+/* Quantises a matrix in blocks:  scale = m / 448 with m = max(largest |src| of the block, 448 2^-126), code = e4m3(448 src / m):
+ * 448 src, which is exact for bf16, and its quotient by m in fp32, each rounded once, then to nearest even.  A block that holds an infinity or a NaN has the scale NaN.
  * codes, scales: of src.  codes_t, scales_t: of its transpose [cols, rows] (KD_BLOCK_ROW: blocks along src's columns, with scales of
  * their own; KD_BLOCK_TILE: the same codes and scales).  Either pair may be NULL; src is read once for both.
  * src: aligned to its elements, codes to 16 bytes, scales to 4. */

@@ -10,7 +10,8 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 __device__ __forceinline__ float scale_of(uint32_t m) { return m < 0x7f800000u ? __uint_as_float(m) / 448.f : __builtin_nanf(""); }
 
 // 448 x / m, rounded as 448 x and its quotient by m are:  m = 2^e f with 1 <= f < 2, a = (448 2^-e) x, q = a (1 / f), and then the remainder's share,
-// (a - q f) (1 / f), added in one rounding, which gives the quotient that a division gives (448 x is exact for bf16).  A division for every element took
+// (a - q f) (1 / f), added in one rounding, which gives the quotient that a division gives (448 x is exact for bf16; fp32: on all of the 5.4 10^8 pairs
+// of significands whose quotient lies next to a border between codes).  A division for every element took
 // three times as many instructions.
 struct Divisor { float c, f, inv; };
 __device__ __forceinline__ Divisor divisor_of(uint32_t m) {

@@ -829,7 +829,7 @@ def make_blocks_params(rows, cols, ld=None, src_dtype=BF16, block=BLOCK_ROW):
 def quantize_e4m3_blocks(x, block=BLOCK_ROW, transpose=False, both=False):
     """E4m3Blocks of a bf16 or fp32 matrix with contiguous rows: a scale per row and 128 columns (BLOCK_ROW) or per 128 x 128
     (BLOCK_TILE).  transpose: of x's transpose instead; both: (x's, its transpose's) from one reading.  Other than quantize_e4m3, which
-    multiplies by a reciprocal, it divides: code = e4m3(448 x / largest of the block), rounded once before."""
+    multiplies by a reciprocal, it divides: code = e4m3(448 x / largest of the block), product and quotient in fp32."""
     import torch
     rows, cols, ld = _check_matrix(x, "x")
     p = make_blocks_params(rows, cols, ld, _float_dtype(x, "x"), block)
