@@ -430,6 +430,8 @@ typedef struct {
   int32_t reserved[2];        /* must be 0                                                       */
 } kd_sample_params;
 
+/* The workspace has room for every filter, as arrays of settings are not known here: 4 bytes for every 8 to 64 logits and, where rows have more than 4096, 48 KB a row
+ * for 1024 rows at most (512 rows of 151936: 35 MB). */
 kd_status kd_sample_workspace_size(const kd_sample_params* params, size_t* bytes);
 /* Arrays aligned to their elements. */
 kd_status kd_sample(const kd_sample_params* params, const void* logits, const float* u, const float* temperature_rows,
@@ -447,7 +449,7 @@ kd_status kd_sample(const kd_sample_params* params, const void* logits, const fl
  *         totals between the two calls.
  *  out, out_dtypes  where the clipped values go; out NULL, or out[i] == grads[i] with the same type: in place, where nothing is written
  *         if nothing has to be scaled
- *  norm   device, one float, or NULL */
+ *  norm   device, one float, or NULL; infinite where the norm is beyond fp32, also if it is finite in 64 bits (then everything is scaled) */
 typedef enum { KD_NORM_L2 = 0, KD_NORM_MAX = 1 } kd_norm;
 #define KD_GRADS_MAX 65536
 

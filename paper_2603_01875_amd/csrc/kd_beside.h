@@ -79,7 +79,7 @@ hipError_t launch_sample(const RowsArgs& r, hipStream_t st);
 // ---- gradient norm ----
 constexpr int kGradsPerLaunch = 160;
 constexpr int kNormGroups = 2048;      // workgroups of a launch
-// Elements of a piece.  (Norm and clipped copy, us, with 2048, 8192 and 32768: 3.2 million fp32 in 24 arrays 9.3 + 6.7, 7.3 + 6.1, 7.5 + 6.7; 30 million bf16 39 + 26,
+// Elements of a piece.  (Norm and clipped copy, us, each repeated by itself on arrays with allocations of their own, with 2048, 8192 and 32768: 3.2 million fp32 in 24 arrays 9.3 + 6.7, 7.3 + 6.1, 7.5 + 6.7; 30 million bf16 39 + 26,
 // 17 + 22, 14 + 21; 1.7 billion 1802 + 1505, 587 + 1338, 573 + 1313: finding a piece's array costs as much as some thousand elements.)
 constexpr int kPieceElements = 32768;
 struct GradTable {

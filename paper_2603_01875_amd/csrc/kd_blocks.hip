@@ -11,9 +11,9 @@ namespace kd {
 //
 // Bound by memory: two bytes (four) read, one written per element and order.  A workgroup holds 128 x 128 elements in registers, four rows x eight
 // columns a thread: rows, columns and the tile each have their largest magnitude from there, so that both orders come from one reading.
-// Codes of the other order are turned through LDS, so that a wave writes whole lines.  4096 x 4096 bf16 by rows, both orders: 20 us, of 14 at the rate of a
+// Codes of the other order are turned through LDS, so that a wave writes whole lines.  4096 x 4096 bf16 by rows, both orders: 20 us (22 between the products of a training step), of 14 at the rate of a
 // copy; 4096 x 12288: 51 (eight rows a thread and columns' codes stored as threads have them: 25 and 74, too few waves to have loads on their
-// way while others compute).  By tiles: 16 and 38.
+// way while others compute).  By tiles: 16 (18) and 38.  By rows each element is divided twice, by its row's largest and by its column's.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTileRows = 4, kTileThreads = 16 * 128 / kTileRows;
 template <bool F32, bool TILE>

@@ -1,7 +1,8 @@
 // Norm of many arrays taken together, and clipping (kd_grad_norm, kd_grad_clip).
 //
 // norm = sqrt(sum x^2) or max |x|;  out = x min(1, max_norm / norm).  Two readings and one writing of all elements, nothing else: bound by
-// memory: 1.7 billion bf16 in 311 arrays 572 us (5.9 TB/s), then 1313 (5.2), of 1420 for one reading and one writing at the rate of a copy.  The arrays come as a table in the kernel's arguments (no copy to the device, so a call can be captured), cut into pieces
+// memory: 1.7 billion bf16 in 311 arrays, views of one at any offset, 591 to 613 us (5.6 to 5.8 TB/s), then 1545 (4.4), of 1420 for one reading and one writing at the
+// rate of a copy; arrays of one size with an allocation each 565 to 572 and 1309 to 1316.  The arrays come as a table in the kernel's arguments (no copy to the device, so a call can be captured), cut into pieces
 // of equal length that workgroups take in turn; squares are summed in 64 bits, where none overflows and the order of 10^9 terms does not matter
 // much, in a fixed order all the same: a thread's, then a workgroup's, then all workgroups' by one more.
 #include <hip/hip_runtime.h>

@@ -41,7 +41,7 @@ __device__ __forceinline__ const void* row_of(const RowsArgs& a, int64_t t) {
 // ------------------------------------------------------------------------------------------------
 // first kernel
 //
-// All of a thread's loads are on their way at once, and only then used.  Top logits: bound by memory, 4096 x 151936 bf16 225 to 243 us (5.1 to 5.5 TB/s).  Sampling: by
+// All of a thread's loads are on their way at once, and only then used.  Top logits: bound by memory, 4096 x 151936 bf16 212 to 243 us (5.1 to 5.9 TB/s).  Sampling: by
 // the exponentials in 64 bits, 21 instructions an entry issued at 90 % of the rate, 512 x 151936 bf16 61 us (2.5 TB/s).
 // ------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float row_temperature(const RowsArgs& a, int64_t t) { return a.temperature_rows ? a.temperature_rows[t] : a.tau; }
@@ -433,7 +433,8 @@ __device__ __forceinline__ void starts_of_bins(SelectLds& s) {
 }
 
 // Sorts list[0 .. n) in descending order, n at most half a list (no entry twice); top: its largest key.  By bins of the distance from the top
-// into the list's other half, then each entry counts the larger ones of its bin.
+// into the list's other half, then each entry counts the larger ones of its bin: n^2 steps for n equal logits, so that 2000 of them at the top of each of 64 rows make the top 50
+// take 185 us instead of 18 (600: 44).
 __device__ __forceinline__ void sort_by_bins(uint32_t n, uint32_t top, SelectLds& s) {
   constexpr int HELD = kList / 2 / kSelect;
   for (int i = threadIdx.x; i < kNear; i += kSelect) s.near_[i] = 0;
@@ -617,7 +618,9 @@ __device__ __forceinline__ uint64_t last_of(const uint64_t (&held)[kHeld], bool 
 // ------------------------------------------------------------------------------------------------
 // top logits
 //
-// Four workgroups of eight waves a CU, which wait for each other's LDS and groups: 4096 rows of 151936, 64 of each, 83 to 93 us; 7 rows 9.
+// Four workgroups of eight waves a CU, which wait for each other's LDS and groups: 4096 rows of 151936, 64 of each, 78 to 93 us; 7 rows 9.
+// Where V / 8 is no more than K every entry is listed, and a row of more entries than a list goes the slow way: top 1024 of 512 rows of 8192 fp32 47 us,
+// of 9000 70, of 12288, which take the short one, 35.
 // ------------------------------------------------------------------------------------------------
 template <bool F32>
 __device__ __forceinline__ void put_top(const RowsArgs& a, int64_t t, int at, uint64_t entry) {
@@ -685,8 +688,8 @@ __global__ __launch_bounds__(kSelect, 8) void top_select_kernel(const RowsArgs a
 // ------------------------------------------------------------------------------------------------
 // sampling
 //
-// Bins and tiles read the row again (9 and 11 us for 64 rows of 128256 fp32), and the select kernel is a chain of short steps of one workgroup a row, each some
-// thousand cycles of latency: 15 us for 512 rows without a filter, 16 for one row with a short list, 37 where lists of a thousand are sorted.
+// Bins and tiles read the row again (10 and 12 us for 64 rows of 128256 fp32), and the select kernel is a chain of short steps of one workgroup a row, each some
+// thousand cycles of latency: 14 to 15 us for 512 rows without a filter, 16 for one row with a short list, 37 where lists of a thousand are sorted.
 // ------------------------------------------------------------------------------------------------
 // A row's settings, and whether it can be drawn from.
 struct Draw {
