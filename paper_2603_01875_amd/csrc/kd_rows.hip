@@ -716,13 +716,13 @@ __device__ __forceinline__ Draw draw_of(const RowsArgs& a, int64_t t, uint32_t k
 __device__ __forceinline__ int bits_of_row(int64_t V) { return min(kChunkBits, 62 - (64 - __clzll((unsigned long long)V))); }
 // Bits of a weight in sums over the row's entries, each of them rounded: as many as the row's sum leaves of 62, and no more than whole_one takes.  (As many as V equal
 // entries leave would be 44 at V = 151936 and 37 at 2^24: a tail of small weights, all rounded the same way, would be off by V halves of that.)  The chunks'
-// sums in 32 bits, in a fixed order: whoever asks for a row gets the same bits.
+// sums in 32 bits, in a fixed order and with no operation that a compiler may fuse or not: whichever kernel asks for a row gets the same bits.
 constexpr int kMostBits = 51;
 __device__ __forceinline__ int bits_of_sum(const RowsArgs& a, int64_t t, float top, double scale, SelectLds& s) {
   float sum = 0.f;
   for (int c = threadIdx.x; c < a.chunks; c += kSelect) {
     const RowChunk& q = a.chunk[t * a.chunks + c];
-    if (q.key > kKeyMinusInf) sum += (float)q.sum * __builtin_amdgcn_exp2f((value_of(q.key) - top) * (float)scale);
+    if (q.key > kKeyMinusInf) sum = fmaf((float)q.sum, __builtin_amdgcn_exp2f((value_of(q.key) - top) * (float)scale), sum);
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
